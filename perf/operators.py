@@ -279,8 +279,8 @@ def _handles(s):
 def _run_own(s):
     B, op, n = s["B"], s["op"], s["n"]
     if op == "plan":
-        B.wf_page_plan(s["old"], s["new"], n, s["bs"], s["free"], s["n_free"], s["table"], s["width"], s["offsets"], s["slots"], s["cap"], s["len"],
-                       s["left"], s["err"])
+        B.wf_page_plan(s["old"], s["new"], n, s["bs"], s["free"], s["free"].numel(), s["n_free"], s["table"], s["width"], s["offsets"], s["slots"],
+                       s["cap"], s["len"], s["left"], s["err"])
         return {"table": s["table"], "offsets": s["offsets"], "slots": s["slots"], "len": s["len"], "n_free": s["left"]}
     if op == "store":
         d = s["hkv"] * s["dim"]
