@@ -437,9 +437,9 @@ def _plain_select(s):
     x = torch.where(torch.isnan(x) | (s["suppress"] != 0)[None], -math.inf, x)
     m = x.amax(-1, keepdim=True)
     # the sum in 64 bits: whole numbers come out of its comparison with other beams'
-    lse = m + torch.log(torch.exp(x - m).sum(-1, keepdim=True, dtype=torch.float64)).float()
+    rest = torch.log(torch.exp(x - m).sum(-1, keepdim=True, dtype=torch.float64)).float()
     at = _best(x, 2 * W)
-    total = s["scores"].view(n * W, 1) + (x.gather(1, at) - lse)
+    total = s["scores"].view(n * W, 1) + ((x.gather(1, at) - m) - rest)
     total = torch.where(torch.isnan(total), -math.inf, total).view(n, 2 * W * W)
     top = _best(total, 2 * W)
     score, beam, token = total.gather(1, top), top // (2 * W), at.view(n, -1).gather(1, top)
