@@ -54,6 +54,8 @@ typedef enum wf_status {
 #define WF_DEV_ERR_TOKEN 0x4u    /* a token id outside [0, vocab) was clamped */
 #define WF_DEV_ERR_LAUNCH 0x8u   /* a kernel found its launch inconsistent with its plan
                                     (grid, cluster or shared memory) and did nothing */
+#define WF_DEV_ERR_PAGE 0x10u    /* a paged-cache call met a length, block id or slot out of
+                                    bounds; what it names was skipped */
 
 #define WF_MAX_TAPS 8
 #define WF_MAX_LAYERS 64
@@ -332,6 +334,158 @@ wf_status wf_attention_noalloc(const void *d_q, const void *d_kc, const void *d_
                                const int32_t *d_slot, const int32_t *d_base, int32_t n_seq,
                                int32_t RPS, int32_t n_heads, int32_t ctx, int32_t mode,
                                int32_t rope, float rope_base, void *d_out, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Beam decode over a paged key/value cache held in 4 bits.  The calls below
+ * take no handle: every buffer is the caller's, every call is asynchronous on
+ * its stream, and a step of beam search is
+ *   wf_page_plan      blocks and slots for the step's new tokens,
+ *   wf_kv4_store      the new keys and values of a layer,
+ *   wf_kv4_attention  the layer's attention (self and cross),
+ *   wf_beam_select    the next tokens and their parents,
+ *   wf_beam_reorder   the block tables after the selection.
+ * d_err (nullable) is a device uint32 that the call ORs WF_DEV_ERR_* bits
+ * into; the caller clears it.
+ * ---------------------------------------------------------------------- */
+
+#define WF_BF16 0
+#define WF_F16 1
+#define WF_F32 2
+#define WF_KV4_GROUP 64   /* values that share a scale and an offset */
+#define WF_KV4_RECORD 1152 /* bytes of 16 positions of one group, keys and values */
+#define WF_MAX_BEAMS 16
+
+/* A paged cache in 4 bits.  A block holds block_size positions of every
+ * key/value head; the same block id names that block in each of n_layers
+ * layers, layer l starting at d_base + l * layer_stride bytes.  A row of a
+ * head is cut into groups of 64 values (head_dim 64: one, 128: two).  A value
+ * of a group is s (c - 8) + z: c a code of 4 bits, s and z the group's scale
+ * and offset in `dtype` (WF_BF16 or WF_F16), which is also the type of the
+ * rows stored and of the queries.  From a group's extremes,
+ *   s = round((max - min) / 15), z = round(max - 7 s),
+ *   c = clamp(rint((x - z) / s), -8, 7) + 8   (8 where s is 0),
+ * in fp32, rounded to nearest even; a group with a value that is not finite
+ * reads back as NaN.
+ * Layout: [block][head][group][block_size / 16][1152 bytes].  A record of 16
+ * positions holds 512 bytes of key codes (32 a position, low nibble first),
+ * 512 of value codes in the order the attention's tensor instructions take
+ * them, and 128 of (s, z) pairs: [position % 8][keys, values][position / 8]. */
+typedef struct wf_kv4_pool {
+  void *d_base;         /* 16-byte aligned */
+  int64_t layer_stride; /* bytes, a multiple of 16; 0: n_blocks * wf_kv4_block_bytes() */
+  int32_t n_layers;
+  int32_t n_blocks;     /* block ids are 0 .. n_blocks - 1; n_blocks * block_size < 2^31 */
+  int32_t block_size;   /* 16, 32 or 64 positions */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t dtype;        /* WF_BF16 or WF_F16 */
+} wf_kv4_pool;
+
+/* Bytes of one block in one layer; 0 for a shape that is not supported. */
+size_t wf_kv4_block_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_dim);
+
+/* Block tables and slot maps from request lengths.  Request i (0 <= i < n)
+ * grows from d_old_len[i] to d_new_len[i] positions.  Its table row,
+ * d_table + i * table_stride, names the blocks of its first
+ * ceil(old / block_size) columns; the columns up to ceil(new / block_size) are
+ * filled from the free list, a stack of *d_n_free ids in d_free (capacity
+ * n_blocks): request by request, column by column, from the top.
+ *   d_offsets  int32 [n + 1]      out: request i's new tokens are
+ *                                 [d_offsets[i], d_offsets[i + 1])
+ *   d_slots    int32 [slots_cap]  out: of each new token, block * block_size +
+ *                                 position % block_size; -1 after the last
+ *   d_len      int32 [n]          out: new length if granted, else the old one
+ *   d_n_free_out int32 [1]        out: ids left
+ * Requests are granted in order; the first whose blocks or slots do not fit,
+ * and all after it, are refused whole (WF_DEV_ERR_CAPACITY).  A request with
+ * old < 0, new < old or more than table_stride columns is refused alone
+ * (WF_DEV_ERR_PAGE).  d_len and d_n_free_out are buffers of their own, not
+ * d_old_len, d_new_len or d_n_free: all of the grid reads those. */
+wf_status wf_page_plan(const int32_t *d_old_len, const int32_t *d_new_len, int32_t n,
+                       int32_t block_size, const int32_t *d_free, int32_t n_blocks,
+                       const int32_t *d_n_free, int32_t *d_table, int32_t table_stride,
+                       int32_t *d_offsets, int32_t *d_slots, int32_t slots_cap, int32_t *d_len,
+                       int32_t *d_n_free_out, uint32_t *d_err, void *stream);
+
+/* Quantise n rows of keys and values into one layer of the cache.
+ *   d_k, d_v  dtype [n][n_kv_heads * head_dim], row strides in elements
+ *             (multiples of 8; pointers 16-byte aligned)
+ *   d_slots   int32 [n]: a negative slot skips its row; a slot named twice
+ *             holds either row
+ * wf_kv4_load reads the slots back into rows (zeros for a negative slot). */
+wf_status wf_kv4_store(const wf_kv4_pool *pool, int32_t layer, const void *d_k, int64_t k_stride,
+                       const void *d_v, int64_t v_stride, const int32_t *d_slots, int32_t n,
+                       uint32_t *d_err, void *stream);
+wf_status wf_kv4_load(const wf_kv4_pool *pool, int32_t layer, const int32_t *d_slots, int32_t n,
+                      void *d_k, int64_t k_stride, void *d_v, int64_t v_stride, uint32_t *d_err,
+                      void *stream);
+
+/* Attention of rps query rows per sequence over one layer of the cache:
+ * softmax(scale q K^T) V, n_heads query heads on n_kv_heads (n_heads a
+ * multiple; query head h reads key/value head h / (n_heads / n_kv_heads)).
+ *   d_q     dtype [n_seq * rps][n_heads * head_dim], row r = seq * rps + j
+ *   d_table int32, sequence i's blocks at d_table + i * table_stride (the
+ *           sequences may share blocks, and stride 0 shares one row)
+ *   d_len   int32 [n_seq]  positions held; the rps rows are the last of them
+ *           when causal: row j sees len - (rps - 1 - j) positions, else len
+ *   max_len a bound on d_len; longer sequences are cut to it
+ *           (WF_DEV_ERR_CAPACITY)
+ *   d_out   dtype [n_seq * rps][n_heads * head_dim]
+ * Strides are in elements, multiples of 8, pointers 16-byte aligned.  A row
+ * that sees nothing is zeros; a block id outside the pool is not read and its
+ * positions are not seen (WF_DEV_ERR_PAGE).  Scores, softmax and sums are
+ * fp32; results do not depend on timing.  d_scratch (16-byte aligned) holds
+ * wf_kv4_attention_scratch_bytes() bytes and belongs to the call until it is
+ * done. */
+wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d_q,
+                           int64_t q_stride, const int32_t *d_table, int32_t table_stride,
+                           const int32_t *d_len, int32_t n_seq, int32_t rps, int32_t n_heads,
+                           int32_t causal, float scale, int32_t max_len, void *d_out,
+                           int64_t out_stride, void *d_scratch, size_t scratch_bytes,
+                           uint32_t *d_err, void *stream);
+size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_heads,
+                                      int32_t n_kv_heads, int32_t head_dim, int32_t max_len);
+
+/* One selection of beam search.  Beam w of request i has the logits row
+ * i * beams + w (`dtype` WF_F32, WF_BF16 or WF_F16, ld elements apart) and
+ * the score d_scores[i * beams + w], the sum of its log-probabilities (-inf:
+ * not in use).  A token's score is score + ((logit - max) - log(sum)) in fp32,
+ * max the row's largest logit and sum that of exp(logit - max); ids with a nonzero d_suppress entry (nullable uint8
+ * [vocab]) and NaN logits count as -inf.  Each beam proposes its 2 beams best
+ * tokens (ties: the lower id); of all proposals the 2 beams best are ranked
+ * (ties: the lower beam, then its better token).  Then
+ *   d_token, d_parent int32, d_score fp32 [n_req][beams]  the first `beams`
+ *       that are not eos, best first; past the last one -1, the beam itself
+ *       and -inf
+ *   d_fin_parent int32, d_fin_score fp32 [n_req][beams]  hypotheses that end:
+ *       eos among the first `beams` ranks; past the last one -1 and -inf
+ * eos < 0: none ends.  2 beams <= vocab.  d_score may be d_scores. */
+wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const float *d_scores,
+                         const uint8_t *d_suppress, int32_t n_req, int32_t beams, int32_t vocab,
+                         int32_t eos, int32_t *d_token, int32_t *d_parent, float *d_score,
+                         int32_t *d_fin_parent, float *d_fin_score, void *d_scratch,
+                         size_t scratch_bytes, void *stream);
+size_t wf_beam_select_scratch_bytes(int32_t n_req, int32_t beams, int32_t vocab);
+
+/* The block tables of n_req requests' beams after a selection.  Beam w of
+ * request i has the table row i * beams + w and d_len[i * beams] positions
+ * (equal for the request's beams).  Beams of a request may share full blocks;
+ * a last block that is partly filled belongs to one beam.  New beam w takes
+ * beam d_parent[i * beams + w]'s full blocks; a parent's first child keeps its
+ * last block, each other child gets the last block of a beam without children
+ * and the parent's contents in it, in every layer (by 16 positions).  A parent
+ * of -1 drops the beam's history: its row holds -1 but for a last block of its
+ * own; if all of a request's parents are -1 the request is released.  Blocks
+ * that no beam of the request holds any more are pushed on the free list
+ * (d_free, capacity pool->n_blocks, *d_n_free ids before, *d_n_free_out
+ * after; they may be one), by request, column and beam.  Columns past the length are not written.
+ * d_table_out may be d_table_in. */
+wf_status wf_beam_reorder(const wf_kv4_pool *pool, const int32_t *d_table_in, int32_t *d_table_out,
+                          int32_t table_stride, const int32_t *d_len, const int32_t *d_parent,
+                          int32_t n_req, int32_t beams, int32_t *d_free, const int32_t *d_n_free,
+                          int32_t *d_n_free_out, void *d_scratch, size_t scratch_bytes,
+                          uint32_t *d_err, void *stream);
+size_t wf_beam_reorder_scratch_bytes(int32_t n_req, int32_t beams, int32_t table_stride);
 
 #ifdef __cplusplus
 }

@@ -17,6 +17,9 @@ _lib = None
 
 WF_OK, WF_ERR_INVALID, WF_ERR_CAPACITY, WF_ERR_CUDA, WF_ERR_UNSUPPORTED, WF_ERR_DEVICE = range(6)
 WF_DEV_ERR_TIMEOUT, WF_DEV_ERR_CAPACITY, WF_DEV_ERR_TOKEN, WF_DEV_ERR_LAUNCH = 1, 2, 4, 8
+WF_DEV_ERR_PAGE = 16
+WF_BF16, WF_F16, WF_F32 = 0, 1, 2
+WF_KV4_GROUP, WF_KV4_RECORD, WF_MAX_BEAMS = 64, 1152, 16
 WF_MAX_TAPS = 8
 WF_OPT_KEEP_LOGITS = 1
 WF_OPT_PROFILE = 2
@@ -68,9 +71,17 @@ class WfSampleParams(C.Structure):
                 ("d_suppress", C.c_void_p)]
 
 
+class WfKv4Pool(C.Structure):
+    _fields_ = [("d_base", C.c_void_p), ("layer_stride", C.c_int64), ("n_layers", C.c_int32),
+                ("n_blocks", C.c_int32), ("block_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
 _P = C.c_void_p
 _I = C.c_int32
+_L = C.c_int64
 _SZ = C.c_size_t
+_PL = C.POINTER(WfKv4Pool)
 _SIGS = {
     "wf_workspace_bytes": (_I, [C.POINTER(WfConfig), _I, _I, C.POINTER(_SZ)]),
     "wf_create": (_I, [C.POINTER(WfConfig), C.POINTER(WfTargetWeights), C.POINTER(WfDrafterWeights),
@@ -95,6 +106,17 @@ _SIGS = {
     "wf_attention": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, C.c_float, _P, _P, _SZ, _P]),
     "wf_attention_scratch_bytes": (_SZ, [_I, _I, _I, _I]),
     "wf_attention_noalloc": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, C.c_float, _P, _P]),
+    "wf_kv4_block_bytes": (_SZ, [_I, _I, _I]),
+    "wf_page_plan": (_I, [_P, _P, _I, _I, _P, _I, _P, _P, _I, _P, _P, _I, _P, _P, _P, _P]),
+    "wf_kv4_store": (_I, [_PL, _I, _P, _L, _P, _L, _P, _I, _P, _P]),
+    "wf_kv4_load": (_I, [_PL, _I, _P, _I, _P, _L, _P, _L, _P, _P]),
+    "wf_kv4_attention": (_I, [_PL, _I, _P, _L, _P, _I, _P, _I, _I, _I, _I, C.c_float, _I, _P, _L,
+                              _P, _SZ, _P, _P]),
+    "wf_kv4_attention_scratch_bytes": (_SZ, [_I, _I, _I, _I, _I, _I]),
+    "wf_beam_select": (_I, [_P, _I, _L, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "wf_beam_select_scratch_bytes": (_SZ, [_I, _I, _I]),
+    "wf_beam_reorder": (_I, [_PL, _P, _P, _I, _P, _P, _I, _I, _P, _P, _P, _P, _SZ, _P, _P]),
+    "wf_beam_reorder_scratch_bytes": (_SZ, [_I, _I, _I]),
 }
 EXPORTED = tuple(_SIGS)
 
@@ -306,3 +328,75 @@ def wf_attention_noalloc(q, kc, vc, slot, base, n_seq, rps, n_heads, ctx, mode, 
     _check("wf_attention_noalloc", lib().wf_attention_noalloc(
         _ptr(q), _ptr(kc), _ptr(vc), _ptr(slot), _ptr(base), n_seq, rps, n_heads, ctx, mode,
         int(rope), float(rope_base), _ptr(out), _stream(stream)))
+
+
+# ------------------------------------------- beam decode, paged 4-bit cache --
+def kv4_pool(base, n_layers, n_blocks, block_size, n_kv_heads, head_dim, dtype=WF_BF16,
+             layer_stride=0) -> WfKv4Pool:
+    """Descriptor of a paged 4-bit cache over a device buffer of n_layers *
+    n_blocks * wf_kv4_block_bytes(...) bytes, which it keeps alive."""
+    pool = WfKv4Pool(_ptr(base), layer_stride, n_layers, n_blocks, block_size, n_kv_heads,
+                     head_dim, dtype)
+    pool.buffer = base
+    return pool
+
+
+def wf_kv4_block_bytes(block_size, n_kv_heads, head_dim) -> int:
+    return lib().wf_kv4_block_bytes(block_size, n_kv_heads, head_dim)
+
+
+def wf_page_plan(old_len, new_len, n, block_size, free, n_blocks, n_free, table, table_stride,
+                 offsets, slots, slots_cap, len_out, n_free_out, err=None, stream=None):
+    _check("wf_page_plan", lib().wf_page_plan(
+        _ptr(old_len), _ptr(new_len), n, block_size, _ptr(free), n_blocks, _ptr(n_free),
+        _ptr(table), table_stride, _ptr(offsets), _ptr(slots), slots_cap, _ptr(len_out),
+        _ptr(n_free_out), _ptr(err), _stream(stream)))
+
+
+def wf_kv4_store(pool, layer, k, k_stride, v, v_stride, slots, n, err=None, stream=None):
+    _check("wf_kv4_store", lib().wf_kv4_store(
+        C.byref(pool), layer, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(slots), n, _ptr(err),
+        _stream(stream)))
+
+
+def wf_kv4_load(pool, layer, slots, n, k, k_stride, v, v_stride, err=None, stream=None):
+    _check("wf_kv4_load", lib().wf_kv4_load(
+        C.byref(pool), layer, _ptr(slots), n, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(err),
+        _stream(stream)))
+
+
+def wf_kv4_attention_scratch_bytes(n_seq, rps, n_heads, n_kv_heads, head_dim, max_len) -> int:
+    return lib().wf_kv4_attention_scratch_bytes(n_seq, rps, n_heads, n_kv_heads, head_dim, max_len)
+
+
+def wf_kv4_attention(pool, layer, q, q_stride, table, table_stride, length, n_seq, rps, n_heads,
+                     causal, scale, max_len, out, out_stride, scratch, scratch_bytes, err=None,
+                     stream=None):
+    _check("wf_kv4_attention", lib().wf_kv4_attention(
+        C.byref(pool), layer, _ptr(q), q_stride, _ptr(table), table_stride, _ptr(length), n_seq,
+        rps, n_heads, int(causal), scale, max_len, _ptr(out), out_stride, _ptr(scratch),
+        scratch_bytes, _ptr(err), _stream(stream)))
+
+
+def wf_beam_select_scratch_bytes(n_req, beams, vocab) -> int:
+    return lib().wf_beam_select_scratch_bytes(n_req, beams, vocab)
+
+
+def wf_beam_select(logits, dtype, ld, scores, suppress, n_req, beams, vocab, eos, token, parent,
+                   score, fin_parent, fin_score, scratch, scratch_bytes, stream=None):
+    _check("wf_beam_select", lib().wf_beam_select(
+        _ptr(logits), dtype, ld, _ptr(scores), _ptr(suppress), n_req, beams, vocab, eos,
+        _ptr(token), _ptr(parent), _ptr(score), _ptr(fin_parent), _ptr(fin_score), _ptr(scratch),
+        scratch_bytes, _stream(stream)))
+
+
+def wf_beam_reorder_scratch_bytes(n_req, beams, table_stride) -> int:
+    return lib().wf_beam_reorder_scratch_bytes(n_req, beams, table_stride)
+
+
+def wf_beam_reorder(pool, table_in, table_out, table_stride, length, parent, n_req, beams, free,
+                    n_free, n_free_out, scratch, scratch_bytes, err=None, stream=None):
+    _check("wf_beam_reorder", lib().wf_beam_reorder(
+        C.byref(pool), _ptr(table_in), _ptr(table_out), table_stride, _ptr(length), _ptr(parent),
+        n_req, beams, _ptr(free), _ptr(n_free), _ptr(n_free_out), _ptr(scratch), scratch_bytes,
+        _ptr(err), _stream(stream)))

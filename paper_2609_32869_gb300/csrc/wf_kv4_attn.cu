@@ -1,0 +1,372 @@
+// Attention over the paged 4-bit cache (softmax(scale q K^T) V).
+//
+// A cached value is s (c - 8) + z with one (s, z) per position and group of 64
+// dims, so both products split into exact small-integer tensor products and
+// rank-one terms in fp32:
+//   q . k_j        = sum_g  s_jg (q_g . (c_jg - 8)) + z_jg sum(q_g)
+//   sum_j p_j v_jg = sum_j (p_j s_jg) (c_jg - 8)    + sum_j p_j z_jg
+// The codes enter mma.sync as exact 16-bit integers (a nibble ORed into the
+// mantissa of 128 or 1024, less that constant and 8); only p_j s_jg is rounded.
+//
+// The positions are the M side of both products (A operand: 16 positions of
+// keys, then 16 dims of values), the query rows the N side in tiles of 8, so
+// one dequantisation serves every query row of a key/value head.  K Q^T
+// leaves lane (r, t) with positions r, r + 8 and rows 2t, 2t + 1; an 8x8
+// transpose per tile turns the weights into the B operand of V^T P^T.
+#include <type_traits>
+
+#include "wf_device.cuh"
+#include "wf_kv4.cuh"
+
+namespace wf {
+
+struct Kv4AttnParams {
+  Kv4Pool pool;
+  const void *q;
+  void *out;
+  long long q_stride, out_stride;
+  const int32_t *table, *len;
+  int table_stride, n_seq, rps, n_heads, group, causal, max_len;
+  float scale;
+  uint32_t *err;
+};
+
+constexpr int kAtWarps = 4;
+constexpr int kAtThreads = kAtWarps * 32;
+constexpr int kAtTile = 64;  // positions of a warp's step
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
+  mma_bf16(d, a[0], a[1], a[2], a[3], b0, b1);
+}
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Nibbles i and i + 4 of w as a pair of 16-bit floats c - 8.
+template <int I>
+__device__ __forceinline__ uint32_t codes_of(uint32_t w, __nv_bfloat16) {
+  const uint32_t u = ((w >> (4 * I)) & 0x000f000fu) | 0x43004300u;  // 128 + c
+  const uint32_t eight = 0x43084308u;                            // 136
+  const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&eight));
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <int I>
+__device__ __forceinline__ uint32_t codes_of(uint32_t w, __half) {
+  const uint32_t u = ((w >> (4 * I)) & 0x000f000fu) | 0x64006400u;  // 1024 + c
+  const uint32_t eight = 0x64086408u;                            // 1032
+  const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&eight));
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// One CTA: (sequence, key/value head, NT * 8 query rows).  Its warps take
+// every kAtWarps-th step of 64 positions and keep their own running maximum,
+// sum and weighted values; the CTA merges them in warp order.
+template <typename T, int G, int NT>
+__global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4AttnParams p) {
+  using X = Kv4Type<T>;
+  constexpr int kRows = NT * 8;
+  constexpr bool kSplitP = std::is_same<T, __half>::value;  // see P below
+  __shared__ float sm_o[kAtWarps][kRows][G * 64 + 1];
+  __shared__ float sm_m[kAtWarps][kRows], sm_l[kAtWarps][kRows];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
+  const int head = blockIdx.x % p.pool.heads, seq = blockIdx.x / p.pool.heads;
+  const int row0 = blockIdx.y * kRows, rows = p.rps * p.group;  // rows of this key/value head: j * group + query head
+  int len = p.len[seq];
+  if (len > p.max_len || len < 0) {
+    if (threadIdx.x == 0) set_error(p.err, len < 0 ? WF_DEV_ERR_PAGE : WF_DEV_ERR_CAPACITY);
+    len = len < 0 ? 0 : p.max_len;
+  }
+  const int32_t *table = p.table + static_cast<long long>(seq) * p.table_stride;
+
+  // queries as B operands, and their sums
+  uint32_t qb[NT][G][4][2];
+  float qs[NT][G][2];
+  int lim[NT][2];
+  int end = 0;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int row = row0 + n * 8 + r;
+    const int j = row / p.group, h = head * p.group + row % p.group;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      uint32_t w[8] = {};
+      if (row < rows) {
+        const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + (static_cast<long long>(seq) * p.rps + j) * p.q_stride +
+                                                           h * (G * 64) + g * 64 + t * 16);
+        const uint4 a = src[0], b = src[1];
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += X::lo(w[i]) + X::hi(w[i]);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      // this lane's scores are of rows 2t and 2t + 1
+      qs[n][g][0] = __shfl_sync(0xffffffffu, sum, t * 8);
+      qs[n][g][1] = __shfl_sync(0xffffffffu, sum, t * 8 + 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)  // dims 16t + 8u + k and + 4: the pairing of a code word's nibbles
+          qb[n][g][k][u] = __byte_perm(w[u * 4 + k / 2], w[u * 4 + 2 + k / 2], k % 2 ? 0x7632 : 0x5410);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int rr = row0 + n * 8 + 2 * t + e;
+      int v = rr < rows ? (p.causal ? len - (p.rps - 1 - rr / p.group) : len) : 0;
+      lim[n][e] = max(v, 0);
+      end = max(end, lim[n][e]);
+    }
+  }
+  end = max(end, __shfl_xor_sync(0xffffffffu, end, 1));
+  end = max(end, __shfl_xor_sync(0xffffffffu, end, 2));
+
+  float o[NT][G][4][4] = {}, zacc[NT][G][2] = {}, l[NT][2] = {}, m[NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) m[n][0] = m[n][1] = -INFINITY;
+  const float c = p.scale * 1.4426950408889634f;  // base-2 softmax
+
+  for (int k0 = warp * kAtTile; k0 < end; k0 += kAtWarps * kAtTile) {
+    const unsigned char *rec[4];
+    bool there[4];
+    float x[4][NT][4];
+    float sv[4][2][G], zv[4][2][G];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int pos = k0 + i * 16;
+      there[i] = pos < end;
+      int block = 0;
+      if (there[i]) {
+        block = table[pos >> p.pool.bs_shift];
+        if (block < 0 || block >= p.pool.n_blocks) {
+          if (lane == 0) set_error(p.err, WF_DEV_ERR_PAGE);
+          there[i] = false;
+          block = 0;
+        }
+      }
+      rec[i] = kv4_record(p.pool, block, head, 0, (pos & (p.pool.bs - 1)) >> 4);
+    }
+    const int group_step = (p.pool.bs >> 4) * kKv4Rec;
+    float mx[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) mx[n][0] = m[n][0], mx[n][1] = m[n][1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][n][e] = there[i] ? 0.f : -INFINITY;
+      if (!there[i]) continue;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const unsigned char *rg = rec[i] + g * group_step;
+        const uint2 w0 = *reinterpret_cast<const uint2 *>(rg + r * 32 + t * 8);
+        const uint2 w1 = *reinterpret_cast<const uint2 *>(rg + (r + 8) * 32 + t * 8);
+        const uint4 sz = *reinterpret_cast<const uint4 *>(rg + kKv4ScaleOff + r * 16);
+        float acc[NT][4] = {};
+#define WF_KSTEP(K)                                                                                             \
+  {                                                                                                             \
+    const uint32_t a[4] = {codes_of<K>(w0.x, T()), codes_of<K>(w1.x, T()), codes_of<K>(w0.y, T()),              \
+                           codes_of<K>(w1.y, T())};                                                             \
+    _Pragma("unroll") for (int n = 0; n < NT; ++n) mma16(acc[n], a, qb[n][g][K][0], qb[n][g][K][1], T()); \
+  }
+        WF_KSTEP(0) WF_KSTEP(1) WF_KSTEP(2) WF_KSTEP(3)
+#undef WF_KSTEP
+        const float s0 = X::lo(sz.x) * c, z0 = X::hi(sz.x) * c, s1 = X::lo(sz.y) * c, z1 = X::hi(sz.y) * c;
+        sv[i][0][g] = X::lo(sz.z), zv[i][0][g] = X::hi(sz.z), sv[i][1][g] = X::lo(sz.w), zv[i][1][g] = X::hi(sz.w);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          x[i][n][0] += fmaf(s0, acc[n][0], z0 * qs[n][g][0]);
+          x[i][n][1] += fmaf(s0, acc[n][1], z0 * qs[n][g][1]);
+          x[i][n][2] += fmaf(s1, acc[n][2], z1 * qs[n][g][0]);
+          x[i][n][3] += fmaf(s1, acc[n][3], z1 * qs[n][g][1]);
+        }
+      }
+      const int pos = k0 + i * 16 + r;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (pos + (e >> 1) * 8 >= lim[n][e & 1]) x[i][n][e] = -INFINITY;
+          mx[n][e & 1] = fmaxf(mx[n][e & 1], x[i][n][e]);
+        }
+      }
+      // what lies past the sequence may hold anything
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (pos + u * 8 >= end)
+#pragma unroll
+          for (int g = 0; g < G; ++g) sv[i][u][g] = zv[i][u][g] = 0.f;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xffffffffu, mx[n][e], off));
+        if (mx[n][e] != m[n][e]) {
+          const float corr = ex2(m[n][e] - mx[n][e]);
+          l[n][e] *= corr;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            zacc[n][g][e] *= corr;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[n][g][q][e] *= corr, o[n][g][q][e + 2] *= corr;
+          }
+          m[n][e] = mx[n][e];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (!there[i]) continue;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[i][n][e] = x[i][n][e] == -INFINITY ? 0.f : ex2(x[i][n][e] - m[n][e & 1]);
+          l[n][e & 1] += x[i][n][e];
+        }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        // P in bf16: its range holds any scale.  A cache in fp16 promises 11
+        // bits, so there P goes in as the sum of two.
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float p0 = x[i][n][2 * u], p1 = x[i][n][2 * u + 1];
+            // a weight of 0 stays 0 whatever the position holds
+            const float a = p0 == 0.f ? 0.f : p0 * sv[i][u][g], b = p1 == 0.f ? 0.f : p1 * sv[i][u][g];
+            zacc[n][g][0] += p0 == 0.f ? 0.f : p0 * zv[i][u][g];
+            zacc[n][g][1] += p1 == 0.f ? 0.f : p1 * zv[i][u][g];
+            const uint32_t h = pack_bf16(a, b);
+            ph[n][u] = transpose8x8(h);
+            if (kSplitP)
+              pl[n][u] = transpose8x8(pack_bf16(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u)));
+          }
+        const uint4 w = *reinterpret_cast<const uint4 *>(rec[i] + g * group_step + kKv4ValOff + lane * 16);
+#define WF_VSTEP(Q)                                                                                             \
+  {                                                                                                             \
+    const __nv_bfloat16 b = __nv_bfloat16();                                                                    \
+    const uint32_t a[4] = {codes_of<Q>(w.x, b), codes_of<Q>(w.y, b), codes_of<Q>(w.z, b), codes_of<Q>(w.w, b)};                 \
+    _Pragma("unroll") for (int n = 0; n < NT; ++n) {                                                            \
+      mma16(o[n][g][Q], a, ph[n][0], ph[n][1], b);                                                              \
+      if (kSplitP) mma16(o[n][g][Q], a, pl[n][0], pl[n][1], b);                                                 \
+    }                                                                                                           \
+  }
+        WF_VSTEP(0) WF_VSTEP(1) WF_VSTEP(2) WF_VSTEP(3)
+#undef WF_VSTEP
+      }
+    }
+  }
+
+  // the warp's results: sums over its 8 position lanes, rows 2t and 2t + 1
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) {
+        l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], off);
+#pragma unroll
+        for (int g = 0; g < G; ++g) zacc[n][g][e] += __shfl_xor_sync(0xffffffffu, zacc[n][g][e], off);
+      }
+      const int row = n * 8 + 2 * t + e;
+      if (r == 0) sm_m[warp][row] = m[n][e], sm_l[warp][row] = l[n][e];
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          sm_o[warp][row][g * 64 + r * 8 + q] = o[n][g][q][e] + zacc[n][g][e];
+          sm_o[warp][row][g * 64 + r * 8 + 4 + q] = o[n][g][q][e + 2] + zacc[n][g][e];
+        }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kRows * G * 32; i += kAtThreads) {
+    const int row = i / (G * 32), d = i % (G * 32) * 2;
+    if (row0 + row >= rows) break;
+    float mm = -INFINITY, ll = 0.f, a = 0.f, b = 0.f;
+#pragma unroll
+    for (int w = 0; w < kAtWarps; ++w) mm = fmaxf(mm, sm_m[w][row]);
+#pragma unroll
+    for (int w = 0; w < kAtWarps; ++w) {
+      if (sm_m[w][row] == -INFINITY) continue;
+      const float f = ex2(sm_m[w][row] - mm);
+      ll += f * sm_l[w][row], a += f * sm_o[w][row][d], b += f * sm_o[w][row][d + 1];
+    }
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+    const int j = (row0 + row) / p.group, h = head * p.group + (row0 + row) % p.group;
+    T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + d;
+    *reinterpret_cast<uint32_t *>(dst) = X::pack(a * inv, b * inv);
+  }
+}
+
+}  // namespace wf
+
+using namespace wf;
+
+template <typename T, int G, int NT>
+static cudaError_t launch(const Kv4AttnParams &p, cudaStream_t s) {
+  const int rows = p.rps * p.group;
+  void *args[] = {const_cast<Kv4AttnParams *>(&p)};
+  return launch_pdl(reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>),
+                    dim3(p.n_seq * p.pool.heads, (rows + NT * 8 - 1) / (NT * 8)), kAtThreads, 0, args, s);
+}
+
+extern "C" {
+
+size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                      int32_t max_len) {
+  return 0;
+}
+
+wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d_q, int64_t q_stride, const int32_t *d_table,
+                           int32_t table_stride, const int32_t *d_len, int32_t n_seq, int32_t rps, int32_t n_heads,
+                           int32_t causal, float scale, int32_t max_len, void *d_out, int64_t out_stride, void *d_scratch,
+                           size_t scratch_bytes, uint32_t *d_err, void *stream) {
+  Kv4AttnParams p = {};
+  const wf_status st = kv4_pool_check(pool, layer, &p.pool, nullptr);
+  if (st != WF_OK) return st;
+  const int64_t d = static_cast<int64_t>(n_heads) * pool->head_dim;
+  if (!d_q || !d_table || !d_len || !d_out || n_seq <= 0 || rps <= 0 || n_heads <= 0 || n_heads % pool->n_kv_heads ||
+      max_len <= 0 || table_stride < 0 || !aligned16(d_q) || !aligned16(d_out) || q_stride % 8 || out_stride % 8 ||
+      q_stride < d || out_stride < d || !(scale == scale))
+    return WF_ERR_INVALID;
+  // every position up to max_len needs a table column (stride 0: one row that the caller made long enough)
+  if (table_stride && static_cast<int64_t>(table_stride) * pool->block_size < max_len) return WF_ERR_INVALID;
+  const int64_t rows = static_cast<int64_t>(rps) * (n_heads / pool->n_kv_heads);
+  if (static_cast<int64_t>(n_seq) * pool->n_kv_heads > INT32_MAX || rows > 65535 * 8LL) return WF_ERR_UNSUPPORTED;
+  p.q = d_q, p.out = d_out, p.q_stride = q_stride, p.out_stride = out_stride;
+  p.table = d_table, p.len = d_len, p.table_stride = table_stride;
+  p.n_seq = n_seq, p.rps = rps, p.n_heads = n_heads, p.group = n_heads / pool->n_kv_heads;
+  p.causal = causal != 0, p.max_len = max_len, p.scale = scale, p.err = d_err;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  using B = __nv_bfloat16;
+  const bool f16 = pool->dtype == WF_F16, wide = pool->head_dim == 128, two = rows > 8;
+  cudaError_t e;
+  if (f16)
+    e = wide ? (two ? launch<__half, 2, 2>(p, s) : launch<__half, 2, 1>(p, s)) : (two ? launch<__half, 1, 2>(p, s) : launch<__half, 1, 1>(p, s));
+  else
+    e = wide ? (two ? launch<B, 2, 2>(p, s) : launch<B, 2, 1>(p, s)) : (two ? launch<B, 1, 2>(p, s) : launch<B, 1, 1>(p, s));
+  return e == cudaSuccess ? WF_OK : WF_ERR_CUDA;
+}
+
+}  // extern "C"
