@@ -13,6 +13,8 @@
 // one dequantisation serves every query row of a key/value head.  K Q^T
 // leaves lane (r, t) with positions r, r + 8 and rows 2t, 2t + 1; an 8x8
 // transpose per tile turns the weights into the B operand of V^T P^T.
+#include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "wf_device.cuh"
@@ -28,6 +30,9 @@ struct Kv4AttnParams {
   const int32_t *table, *len;
   int table_stride, n_seq, rps, n_heads, group, causal, max_len;
   float scale;
+  int chunk, chunks;  // positions of a CTA, CTAs along max_len
+  float *part_o;      // [task][chunks][rows][dim] weighted values of a chunk
+  float2 *part_ml;    // [task][chunks][rows] (maximum, sum)
   uint32_t *err;
 };
 
@@ -71,33 +76,94 @@ __device__ __forceinline__ uint32_t codes_of(uint32_t w, __half) {
   return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// One CTA: (sequence, key/value head, NT * 8 query rows).  Its warps take
-// every kAtWarps-th step of 64 positions and keep their own running maximum,
-// sum and weighted values; the CTA merges them in warp order.
+__device__ __forceinline__ void bulk_load(void *smem_dst, const void *src, uint32_t bytes, uint64_t *bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(smem_dst)),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
+template <int G, int NT>
+struct AtShape {
+  static constexpr int kRows = NT * 8;
+  static constexpr int kStages = 3;
+  static constexpr int kStageBytes = 4 * G * kKv4Rec;  // 64 positions of a head
+  static constexpr int kRingBytes = kAtWarps * kStages * kStageBytes;
+  static constexpr int kMergeBytes = kAtWarps * kRows * (G * 64 + 1 + 2) * 4;
+  static constexpr int kBarOff = ((kRingBytes > kMergeBytes ? kRingBytes : kMergeBytes) + 15) / 16 * 16;
+  static constexpr int kSmem = kBarOff + kAtWarps * kStages * 8;
+};
+
+// A row's limit: positions it sees.
+__device__ __forceinline__ int row_limit(const Kv4AttnParams &p, int row, int len) {
+  return max(p.causal ? len - (p.rps - 1 - row / p.group) : len, 0);
+}
+__device__ __forceinline__ int clamp_len(const Kv4AttnParams &p, int len) { return min(max(len, 0), p.max_len); }
+
+// One CTA: (sequence, key/value head, NT * 8 query rows, chunk of positions).
+// Each warp takes every kAtWarps-th step of 64 positions through a ring of
+// its own in shared memory (one bulk copy per record, an mbarrier per stage;
+// no other warp is waited for) and keeps a running maximum, sum and weighted
+// values; the CTA joins them in warp order, a second kernel the chunks.
 template <typename T, int G, int NT>
 __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4AttnParams p) {
   using X = Kv4Type<T>;
-  constexpr int kRows = NT * 8;
+  using S = AtShape<G, NT>;
+  constexpr int kRows = S::kRows, kStages = S::kStages;
   constexpr bool kSplitP = std::is_same<T, __half>::value;  // see P below
-  __shared__ float sm_o[kAtWarps][kRows][G * 64 + 1];
-  __shared__ float sm_m[kAtWarps][kRows], sm_l[kAtWarps][kRows];
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kBarOff) + warp * kStages;
+  unsigned char *ring = smem + warp * kStages * S::kStageBytes;
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(&bars[i], 1);
+    fence_barrier_init();
+  }
+  __syncwarp();
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
   const int head = blockIdx.x % p.pool.heads, seq = blockIdx.x / p.pool.heads;
   const int row0 = blockIdx.y * kRows, rows = p.rps * p.group;  // rows of this key/value head: j * group + query head
-  int len = p.len[seq];
-  if (len > p.max_len || len < 0) {
-    if (threadIdx.x == 0) set_error(p.err, len < 0 ? WF_DEV_ERR_PAGE : WF_DEV_ERR_CAPACITY);
-    len = len < 0 ? 0 : p.max_len;
-  }
   const int32_t *table = p.table + static_cast<long long>(seq) * p.table_stride;
+  const int raw_len = p.len[seq], len = clamp_len(p, raw_len);
+  if (raw_len != len && threadIdx.x == 0) set_error(p.err, raw_len < 0 ? WF_DEV_ERR_PAGE : WF_DEV_ERR_CAPACITY);
+  // positions that any row of this CTA sees, and this CTA's share of them
+  const int seen = row_limit(p, min(row0 + kRows, rows) - 1, len);
+  const int begin = blockIdx.z * p.chunk, end = min(seen, begin + p.chunk);
+  if (begin >= end && blockIdx.z > 0) return;
+
+  // the ring: step i of this warp is positions begin + (warp + i kAtWarps) 64
+  const int first = begin + warp * kAtTile;
+  const int steps = first < end ? (end - first + kAtWarps * kAtTile - 1) / (kAtWarps * kAtTile) : 0;
+  const int my_tile = lane & 3, my_group = lane >> 2;
+  const bool loader = lane < 4 * G;
+  int next_block = -1;
+  uint32_t there_bits = 0;  // 4 bits a stage: tiles that were loaded
+  auto prefetch_block = [&](int i) {
+    const int pos = first + i * (kAtWarps * kAtTile) + my_tile * 16;
+    next_block = loader && i < steps && pos < end ? table[pos >> p.pool.bs_shift] : -2;
+  };
+  auto issue = [&](int i) {
+    const int stage = i % kStages;
+    const bool ok = next_block >= 0 && next_block < p.pool.n_blocks;
+    if (next_block != -2 && !ok) set_error(p.err, WF_DEV_ERR_PAGE);
+    const uint32_t oks = __ballot_sync(0xffffffffu, ok);
+    there_bits = (there_bits & ~(15u << (4 * stage))) | (oks & 15u) << (4 * stage);
+    if (lane == 0) mbar_arrive_expect_tx(&bars[stage], __popc(oks) * kKv4Rec);
+    __syncwarp();
+    if (ok) {
+      const int pos = first + i * (kAtWarps * kAtTile) + my_tile * 16;
+      bulk_load(ring + stage * S::kStageBytes + lane * kKv4Rec,
+                kv4_record(p.pool, next_block, head, my_group, (pos & (p.pool.bs - 1)) >> 4), kKv4Rec, &bars[stage]);
+    }
+    prefetch_block(i + 1);
+  };
+  prefetch_block(0);
+  for (int i = 0; i < kStages && i < steps; ++i) issue(i);
 
   // queries as B operands, and their sums
   uint32_t qb[NT][G][4][2];
   float qs[NT][G][2];
-  int lim[NT][2];
-  int end = 0;
+  int lim[NT][2], least = INT_MAX;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int row = row0 + n * 8 + r;
@@ -128,53 +194,32 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int rr = row0 + n * 8 + 2 * t + e;
-      int v = rr < rows ? (p.causal ? len - (p.rps - 1 - rr / p.group) : len) : 0;
-      lim[n][e] = max(v, 0);
-      end = max(end, lim[n][e]);
+      // a row past the last sees what the last does: its results are not written
+      lim[n][e] = row_limit(p, min(rr, rows - 1), len);
+      least = min(least, lim[n][e]);
     }
   }
-  end = max(end, __shfl_xor_sync(0xffffffffu, end, 1));
-  end = max(end, __shfl_xor_sync(0xffffffffu, end, 2));
+  least = min(least, __shfl_xor_sync(0xffffffffu, least, 1));
+  least = min(least, __shfl_xor_sync(0xffffffffu, least, 2));
 
   float o[NT][G][4][4] = {}, zacc[NT][G][2] = {}, l[NT][2] = {}, m[NT][2];
 #pragma unroll
   for (int n = 0; n < NT; ++n) m[n][0] = m[n][1] = -INFINITY;
   const float c = p.scale * 1.4426950408889634f;  // base-2 softmax
 
-  for (int k0 = warp * kAtTile; k0 < end; k0 += kAtWarps * kAtTile) {
-    const unsigned char *rec[4];
-    bool there[4];
+  // 64 positions from k0; `edge`: some are not seen by some row, or are not there
+  auto step = [&](const unsigned char *buf, int k0, uint32_t there, auto edge_c) {
+    constexpr bool edge = decltype(edge_c)::value;
     float x[4][NT][4];
     float sv[4][2][G], zv[4][2][G];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int pos = k0 + i * 16;
-      there[i] = pos < end;
-      int block = 0;
-      if (there[i]) {
-        block = table[pos >> p.pool.bs_shift];
-        if (block < 0 || block >= p.pool.n_blocks) {
-          if (lane == 0) set_error(p.err, WF_DEV_ERR_PAGE);
-          there[i] = false;
-          block = 0;
-        }
-      }
-      rec[i] = kv4_record(p.pool, block, head, 0, (pos & (p.pool.bs - 1)) >> 4);
-    }
-    const int group_step = (p.pool.bs >> 4) * kKv4Rec;
     float mx[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) mx[n][0] = m[n][0], mx[n][1] = m[n][1];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[i][n][e] = there[i] ? 0.f : -INFINITY;
-      if (!there[i]) continue;
-#pragma unroll
       for (int g = 0; g < G; ++g) {
-        const unsigned char *rg = rec[i] + g * group_step;
+        const unsigned char *rg = buf + (g * 4 + i) * kKv4Rec;
         const uint2 w0 = *reinterpret_cast<const uint2 *>(rg + r * 32 + t * 8);
         const uint2 w1 = *reinterpret_cast<const uint2 *>(rg + (r + 8) * 32 + t * 8);
         const uint4 sz = *reinterpret_cast<const uint4 *>(rg + kKv4ScaleOff + r * 16);
@@ -190,28 +235,21 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
         const float s0 = X::lo(sz.x) * c, z0 = X::hi(sz.x) * c, s1 = X::lo(sz.y) * c, z1 = X::hi(sz.y) * c;
         sv[i][0][g] = X::lo(sz.z), zv[i][0][g] = X::hi(sz.z), sv[i][1][g] = X::lo(sz.w), zv[i][1][g] = X::hi(sz.w);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          x[i][n][0] += fmaf(s0, acc[n][0], z0 * qs[n][g][0]);
-          x[i][n][1] += fmaf(s0, acc[n][1], z0 * qs[n][g][1]);
-          x[i][n][2] += fmaf(s1, acc[n][2], z1 * qs[n][g][0]);
-          x[i][n][3] += fmaf(s1, acc[n][3], z1 * qs[n][g][1]);
-        }
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = fmaf(e < 2 ? s0 : s1, acc[n][e], (e < 2 ? z0 : z1) * qs[n][g][e & 1]);
+            x[i][n][e] = g == 0 ? v : x[i][n][e] + v;
+          }
       }
       const int pos = k0 + i * 16 + r;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (pos + (e >> 1) * 8 >= lim[n][e & 1]) x[i][n][e] = -INFINITY;
+          if (edge && (pos + (e >> 1) * 8 >= lim[n][e & 1] || !(there >> i & 1))) x[i][n][e] = -INFINITY;
           mx[n][e & 1] = fmaxf(mx[n][e & 1], x[i][n][e]);
         }
-      }
-      // what lies past the sequence may hold anything
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (pos + u * 8 >= end)
-#pragma unroll
-          for (int g = 0; g < G; ++g) sv[i][u][g] = zv[i][u][g] = 0.f;
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -234,12 +272,12 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (!there[i]) continue;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[i][n][e] = x[i][n][e] == -INFINITY ? 0.f : ex2(x[i][n][e] - m[n][e & 1]);
+          const float w = ex2(x[i][n][e] - m[n][e & 1]);
+          x[i][n][e] = edge && x[i][n][e] == -INFINITY ? 0.f : w;
           l[n][e & 1] += x[i][n][e];
         }
 #pragma unroll
@@ -252,20 +290,22 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const float p0 = x[i][n][2 * u], p1 = x[i][n][2 * u + 1];
-            // a weight of 0 stays 0 whatever the position holds
-            const float a = p0 == 0.f ? 0.f : p0 * sv[i][u][g], b = p1 == 0.f ? 0.f : p1 * sv[i][u][g];
-            zacc[n][g][0] += p0 == 0.f ? 0.f : p0 * zv[i][u][g];
-            zacc[n][g][1] += p1 == 0.f ? 0.f : p1 * zv[i][u][g];
+            float a = p0 * sv[i][u][g], b = p1 * sv[i][u][g], za = p0 * zv[i][u][g], zb = p1 * zv[i][u][g];
+            if (edge) {  // a weight of 0 stays 0 whatever the position holds
+              a = p0 == 0.f ? 0.f : a, za = p0 == 0.f ? 0.f : za;
+              b = p1 == 0.f ? 0.f : b, zb = p1 == 0.f ? 0.f : zb;
+            }
+            zacc[n][g][0] += za, zacc[n][g][1] += zb;
             const uint32_t h = pack_bf16(a, b);
             ph[n][u] = transpose8x8(h);
             if (kSplitP)
               pl[n][u] = transpose8x8(pack_bf16(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u)));
           }
-        const uint4 w = *reinterpret_cast<const uint4 *>(rec[i] + g * group_step + kKv4ValOff + lane * 16);
+        const uint4 w = *reinterpret_cast<const uint4 *>(buf + (g * 4 + i) * kKv4Rec + kKv4ValOff + lane * 16);
 #define WF_VSTEP(Q)                                                                                             \
   {                                                                                                             \
     const __nv_bfloat16 b = __nv_bfloat16();                                                                    \
-    const uint32_t a[4] = {codes_of<Q>(w.x, b), codes_of<Q>(w.y, b), codes_of<Q>(w.z, b), codes_of<Q>(w.w, b)};                 \
+    const uint32_t a[4] = {codes_of<Q>(w.x, b), codes_of<Q>(w.y, b), codes_of<Q>(w.z, b), codes_of<Q>(w.w, b)}; \
     _Pragma("unroll") for (int n = 0; n < NT; ++n) {                                                            \
       mma16(o[n][g][Q], a, ph[n][0], ph[n][1], b);                                                              \
       if (kSplitP) mma16(o[n][g][Q], a, pl[n][0], pl[n][1], b);                                                 \
@@ -275,9 +315,30 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
 #undef WF_VSTEP
       }
     }
+  };
+
+  for (int i = 0; i < steps; ++i) {
+    const int stage = i % kStages;
+    const bool landed = mbar_wait(&bars[stage], (i / kStages) & 1, p.err, kSpinLimitCycles);
+    if (!__all_sync(0xffffffffu, landed)) {  // the copies in flight still have to land before the CTA ends
+      for (int j = i; j < steps && j < i + kStages; ++j) mbar_drain(&bars[j % kStages], (j / kStages) & 1);
+      break;
+    }
+    const int k0 = first + i * (kAtWarps * kAtTile);
+    const uint32_t there = there_bits >> (4 * stage) & 15u;
+    const unsigned char *buf = ring + stage * S::kStageBytes;
+    if (k0 + kAtTile <= least && there == 15u)
+      step(buf, k0, there, std::false_type());
+    else
+      step(buf, k0, there, std::true_type());
+    __syncwarp();
+    if (i + kStages < steps) issue(i + kStages);
   }
 
   // the warp's results: sums over its 8 position lanes, rows 2t and 2t + 1
+  __syncthreads();
+  float *sm_m = reinterpret_cast<float *>(smem), *sm_l = sm_m + kAtWarps * kRows, *sm_o = sm_l + kAtWarps * kRows;
+  constexpr int kLd = G * 64 + 1;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -288,34 +349,84 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
 #pragma unroll
         for (int g = 0; g < G; ++g) zacc[n][g][e] += __shfl_xor_sync(0xffffffffu, zacc[n][g][e], off);
       }
-      const int row = n * 8 + 2 * t + e;
-      if (r == 0) sm_m[warp][row] = m[n][e], sm_l[warp][row] = l[n][e];
+      const int row = warp * kRows + n * 8 + 2 * t + e;
+      if (r == 0) sm_m[row] = m[n][e], sm_l[row] = l[n][e];
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          sm_o[warp][row][g * 64 + r * 8 + q] = o[n][g][q][e] + zacc[n][g][e];
-          sm_o[warp][row][g * 64 + r * 8 + 4 + q] = o[n][g][q][e + 2] + zacc[n][g][e];
+          sm_o[row * kLd + g * 64 + r * 8 + q] = o[n][g][q][e] + zacc[n][g][e];
+          sm_o[row * kLd + g * 64 + r * 8 + 4 + q] = o[n][g][q][e + 2] + zacc[n][g][e];
         }
     }
   }
   __syncthreads();
+  const bool whole = seen <= p.chunk;  // no other chunk has positions
+  const size_t task = (static_cast<size_t>(blockIdx.x) * gridDim.y + blockIdx.y) * gridDim.z + blockIdx.z;
   for (int i = threadIdx.x; i < kRows * G * 32; i += kAtThreads) {
     const int row = i / (G * 32), d = i % (G * 32) * 2;
     if (row0 + row >= rows) break;
     float mm = -INFINITY, ll = 0.f, a = 0.f, b = 0.f;
 #pragma unroll
-    for (int w = 0; w < kAtWarps; ++w) mm = fmaxf(mm, sm_m[w][row]);
+    for (int w = 0; w < kAtWarps; ++w) mm = fmaxf(mm, sm_m[w * kRows + row]);
 #pragma unroll
     for (int w = 0; w < kAtWarps; ++w) {
-      if (sm_m[w][row] == -INFINITY) continue;
-      const float f = ex2(sm_m[w][row] - mm);
-      ll += f * sm_l[w][row], a += f * sm_o[w][row][d], b += f * sm_o[w][row][d + 1];
+      const int at = w * kRows + row;
+      if (sm_m[at] == -INFINITY) continue;
+      const float f = ex2(sm_m[at] - mm);
+      ll += f * sm_l[at], a += f * sm_o[at * kLd + d], b += f * sm_o[at * kLd + d + 1];
+    }
+    if (whole) {
+      const float inv = ll == 0.f ? 0.f : 1.f / ll;
+      const int j = (row0 + row) / p.group, h = head * p.group + (row0 + row) % p.group;
+      T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + d;
+      *reinterpret_cast<uint32_t *>(dst) = X::pack(a * inv, b * inv);
+    } else {
+      const size_t at = task * kRows + row;
+      *reinterpret_cast<float2 *>(p.part_o + at * (G * 64) + d) = make_float2(a, b);
+      if (d == 0) p.part_ml[at] = make_float2(mm, ll);
+    }
+  }
+}
+
+// Joins the chunks of a row group in order: one warp per row, whose lanes
+// hold 2 G dims each.
+template <typename T, int G, int NT>
+__global__ void __launch_bounds__(kAtThreads) kv4_join_kernel(const Kv4AttnParams p) {
+  using X = Kv4Type<T>;
+  constexpr int kRows = NT * 8;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int head = blockIdx.x % p.pool.heads, seq = blockIdx.x / p.pool.heads;
+  const int row0 = blockIdx.y * kRows, rows = p.rps * p.group;
+  const int seen = row_limit(p, min(row0 + kRows, rows) - 1, clamp_len(p, p.len[seq]));
+  if (seen <= p.chunk) return;
+  const int chunks = (seen + p.chunk - 1) / p.chunk;
+  const size_t task = (static_cast<size_t>(blockIdx.x) * gridDim.y + blockIdx.y) * p.chunks;
+  for (int row = threadIdx.x >> 5; row < kRows && row0 + row < rows; row += kAtWarps) {
+    float mm = -INFINITY;
+    for (int k = lane; k < chunks; k += 32) mm = fmaxf(mm, p.part_ml[(task + k) * kRows + row].x);
+#pragma unroll
+    for (int off = 16; off; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
+    float ll = 0.f, a[G] = {}, b[G] = {};
+    for (int k = 0; k < chunks; ++k) {
+      const size_t at = (task + k) * kRows + row;
+      const float2 ml = p.part_ml[at];
+      const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm);
+      ll += f * ml.y;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const float2 v = *reinterpret_cast<const float2 *>(p.part_o + at * (G * 64) + g * 64 + lane * 2);
+        // a chunk that the row sees nothing of holds zeros
+        a[g] += f * v.x, b[g] += f * v.y;
+      }
     }
     const float inv = ll == 0.f ? 0.f : 1.f / ll;
     const int j = (row0 + row) / p.group, h = head * p.group + (row0 + row) % p.group;
-    T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + d;
-    *reinterpret_cast<uint32_t *>(dst) = X::pack(a * inv, b * inv);
+    T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + lane * 2;
+#pragma unroll
+    for (int g = 0; g < G; ++g) *reinterpret_cast<uint32_t *>(dst + g * 64) = X::pack(a[g] * inv, b[g] * inv);
   }
 }
 
@@ -323,19 +434,45 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
 
 using namespace wf;
 
+// Query rows of a CTA: 8, or 16 where a key/value head has more.
+static int at_tiles(int64_t rows) { return rows > 8 ? 2 : 1; }
+// Positions of a CTA.  Each warp's step is 64, so a CTA takes at least 256;
+// sequences are cut until there are about two CTAs for each of the four that
+// an SM holds, so that SMs whose sequences are short find other work.
+static int at_chunk(int64_t tasks, int max_len) {
+  const int64_t least = kAtWarps * kAtTile, want = 152 * 8;
+  const int64_t per = (tasks * max_len + want - 1) / want;
+  return static_cast<int>(std::min<int64_t>(std::max(least, (per + least - 1) / least * least), 1 << 30));
+}
+
 template <typename T, int G, int NT>
 static cudaError_t launch(const Kv4AttnParams &p, cudaStream_t s) {
+  using S = AtShape<G, NT>;
+  static const cudaError_t ready = [] {
+    const void *fn = reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>);
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  }();
+  if (ready != cudaSuccess) return ready;
   const int rows = p.rps * p.group;
+  const dim3 grid(p.n_seq * p.pool.heads, (rows + NT * 8 - 1) / (NT * 8), p.chunks);
   void *args[] = {const_cast<Kv4AttnParams *>(&p)};
-  return launch_pdl(reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>),
-                    dim3(p.n_seq * p.pool.heads, (rows + NT * 8 - 1) / (NT * 8)), kAtThreads, 0, args, s);
+  cudaError_t e = launch_pdl(reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>), grid, kAtThreads, S::kSmem, args, s);
+  if (e == cudaSuccess && p.chunks > 1)
+    e = launch_pdl(reinterpret_cast<const void *>(kv4_join_kernel<T, G, NT>), dim3(grid.x, grid.y), kAtThreads, 0, args, s);
+  return e;
 }
 
 extern "C" {
 
 size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                       int32_t max_len) {
-  return 0;
+  if (n_seq <= 0 || rps <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || (head_dim != 64 && head_dim != 128))
+    return 0;
+  const int64_t rows = static_cast<int64_t>(rps) * (n_heads / n_kv_heads), group = at_tiles(rows) * 8;
+  const int64_t tasks = static_cast<int64_t>(n_seq) * n_kv_heads * ((rows + group - 1) / group);
+  const int64_t chunks = (max_len + at_chunk(tasks, max_len) - 1) / at_chunk(tasks, max_len);
+  return chunks > 1 ? static_cast<size_t>(tasks * chunks * group) * (head_dim + 2) * sizeof(float) : 0;
 }
 
 wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d_q, int64_t q_stride, const int32_t *d_table,
@@ -358,9 +495,21 @@ wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d
   p.table = d_table, p.len = d_len, p.table_stride = table_stride;
   p.n_seq = n_seq, p.rps = rps, p.n_heads = n_heads, p.group = n_heads / pool->n_kv_heads;
   p.causal = causal != 0, p.max_len = max_len, p.scale = scale, p.err = d_err;
+  const int tiles = at_tiles(rows);
+  const int64_t groups = (rows + tiles * 8 - 1) / (tiles * 8), tasks = static_cast<int64_t>(n_seq) * pool->n_kv_heads * groups;
+  p.chunk = at_chunk(tasks, max_len);
+  p.chunks = (max_len + p.chunk - 1) / p.chunk;
+  if (p.chunks > 65535) return WF_ERR_UNSUPPORTED;
+  if (p.chunks > 1) {
+    if (!d_scratch || !aligned16(d_scratch)) return WF_ERR_INVALID;
+    if (scratch_bytes < wf_kv4_attention_scratch_bytes(n_seq, rps, n_heads, pool->n_kv_heads, pool->head_dim, max_len))
+      return WF_ERR_CAPACITY;
+    p.part_o = static_cast<float *>(d_scratch);
+    p.part_ml = reinterpret_cast<float2 *>(p.part_o + tasks * p.chunks * tiles * 8 * pool->head_dim);
+  }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   using B = __nv_bfloat16;
-  const bool f16 = pool->dtype == WF_F16, wide = pool->head_dim == 128, two = rows > 8;
+  const bool f16 = pool->dtype == WF_F16, wide = pool->head_dim == 128, two = tiles == 2;
   cudaError_t e;
   if (f16)
     e = wide ? (two ? launch<__half, 2, 2>(p, s) : launch<__half, 2, 1>(p, s)) : (two ? launch<__half, 1, 2>(p, s) : launch<__half, 1, 1>(p, s));
