@@ -147,17 +147,35 @@ def _check(name, status):
 
 def _ptr(t):
     """Device pointer of a torch tensor (or an int / None)."""
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return t
-    return t.data_ptr()
+    try:
+        return t.data_ptr()
+    except AttributeError:
+        if t is None or isinstance(t, int):
+            return t
+        raise
+
+
+_current_stream = None
+
+
+def _find_current_stream():
+    """A function that returns the current device's current stream.  The raw
+    query, where torch has it, takes 0.2 us; torch.cuda.current_stream() builds
+    an object in 3 us, as long as the launch it is for."""
+    import torch
+    raw, device = (getattr(torch._C, f, None) for f in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+    if raw is None or device is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    torch.cuda.init()
+    return lambda: raw(device())
 
 
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        global _current_stream
+        if _current_stream is None:
+            _current_stream = _find_current_stream()
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

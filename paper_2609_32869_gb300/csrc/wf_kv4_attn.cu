@@ -60,20 +60,46 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Nibbles i and i + 4 of w as a pair of 16-bit floats c - 8.
-template <int I>
-__device__ __forceinline__ uint32_t codes_of(uint32_t w, __nv_bfloat16) {
-  const uint32_t u = ((w >> (4 * I)) & 0x000f000fu) | 0x43004300u;  // 128 + c
-  const uint32_t eight = 0x43084308u;                            // 136
-  const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&eight));
-  return *reinterpret_cast<const uint32_t *>(&v);
+// Nibbles i and i + 4 of w as a pair of 16-bit floats kBias + c.
+template <typename T>
+struct Codes;
+template <>
+struct Codes<__nv_bfloat16> {
+  static constexpr float kBias = 128.f;
+  template <int I>
+  static __device__ __forceinline__ uint32_t biased(uint32_t w) {
+    return ((w >> (4 * I)) & 0x000f000fu) | 0x43004300u;
+  }
+  template <int I>
+  static __device__ __forceinline__ uint32_t exact(uint32_t w) {  // c - 8
+    const uint32_t u = biased<I>(w), eight = 0x43084308u;         // 136
+    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&eight));
+    return *reinterpret_cast<const uint32_t *>(&v);
+  }
+};
+template <>
+struct Codes<__half> {
+  static constexpr float kBias = 0.f;
+  template <int I>
+  static __device__ __forceinline__ uint32_t biased(uint32_t w) {  // 1024 + c, less 1024
+    const uint32_t u = ((w >> (4 * I)) & 0x000f000fu) | 0x64006400u, bias = 0x64006400u;
+    const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&bias));
+    return *reinterpret_cast<const uint32_t *>(&v);
+  }
+};
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+      : "l"(*reinterpret_cast<const unsigned long long *>(&a)), "l"(*reinterpret_cast<const unsigned long long *>(&b)));
+  return d;
 }
-template <int I>
-__device__ __forceinline__ uint32_t codes_of(uint32_t w, __half) {
-  const uint32_t u = ((w >> (4 * I)) & 0x000f000fu) | 0x64006400u;  // 1024 + c
-  const uint32_t eight = 0x64086408u;                            // 1032
-  const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&eight));
-  return *reinterpret_cast<const uint32_t *>(&v);
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 __device__ __forceinline__ void bulk_load(void *smem_dst, const void *src, uint32_t bytes, uint64_t *bar) {
@@ -202,19 +228,20 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
   least = min(least, __shfl_xor_sync(0xffffffffu, least, 1));
   least = min(least, __shfl_xor_sync(0xffffffffu, least, 2));
 
-  float o[NT][G][4][4] = {}, zacc[NT][G][2] = {}, l[NT][2] = {}, m[NT][2];
+  float o[NT][G][4][4] = {}, zacc[NT][G][2] = {};
+  float2 l[NT], m[NT];  // of rows 2t and 2t + 1; m: what the weights are relative to
 #pragma unroll
-  for (int n = 0; n < NT; ++n) m[n][0] = m[n][1] = -INFINITY;
+  for (int n = 0; n < NT; ++n) l[n] = make_float2(0.f, 0.f), m[n] = make_float2(-INFINITY, -INFINITY);
   const float c = p.scale * 1.4426950408889634f;  // base-2 softmax
 
   // 64 positions from k0; `edge`: some are not seen by some row, or are not there
   auto step = [&](const unsigned char *buf, int k0, uint32_t there, auto edge_c) {
     constexpr bool edge = decltype(edge_c)::value;
-    float x[4][NT][4];
-    float sv[4][2][G], zv[4][2][G];
+    float2 x[4][NT][2];  // [16 positions][rows][position r, r + 8] (row 2t, row 2t + 1)
+    uint2 szv[4][G];
     float mx[NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) mx[n][0] = m[n][0], mx[n][1] = m[n][1];
+    for (int n = 0; n < NT; ++n) mx[n][0] = mx[n][1] = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -226,59 +253,82 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
         float acc[NT][4] = {};
 #define WF_KSTEP(K)                                                                                             \
   {                                                                                                             \
-    const uint32_t a[4] = {codes_of<K>(w0.x, T()), codes_of<K>(w1.x, T()), codes_of<K>(w0.y, T()),              \
-                           codes_of<K>(w1.y, T())};                                                             \
+    const uint32_t a[4] = {Codes<T>::template biased<K>(w0.x), Codes<T>::template biased<K>(w1.x),              \
+                           Codes<T>::template biased<K>(w0.y), Codes<T>::template biased<K>(w1.y)};             \
     _Pragma("unroll") for (int n = 0; n < NT; ++n) mma16(acc[n], a, qb[n][g][K][0], qb[n][g][K][1], T()); \
   }
         WF_KSTEP(0) WF_KSTEP(1) WF_KSTEP(2) WF_KSTEP(3)
 #undef WF_KSTEP
-        const float s0 = X::lo(sz.x) * c, z0 = X::hi(sz.x) * c, s1 = X::lo(sz.y) * c, z1 = X::hi(sz.y) * c;
-        sv[i][0][g] = X::lo(sz.z), zv[i][0][g] = X::hi(sz.z), sv[i][1][g] = X::lo(sz.w), zv[i][1][g] = X::hi(sz.w);
+        // the codes' bias and 8 go into z: a few dozen units on a sum of 64 products in fp32
+        const float s0 = X::lo(sz.x) * c, s1 = X::lo(sz.y) * c;
+        const float z0 = fmaf(X::hi(sz.x), c, -(Codes<T>::kBias + 8.f) * s0), z1 = fmaf(X::hi(sz.y), c, -(Codes<T>::kBias + 8.f) * s1);
+        szv[i][g] = make_uint2(sz.z, sz.w);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = fmaf(e < 2 ? s0 : s1, acc[n][e], (e < 2 ? z0 : z1) * qs[n][g][e & 1]);
-            x[i][n][e] = g == 0 ? v : x[i][n][e] + v;
-          }
+        for (int n = 0; n < NT; ++n) {
+          const float2 a = make_float2(fmaf(s0, acc[n][0], z0 * qs[n][g][0]), fmaf(s0, acc[n][1], z0 * qs[n][g][1]));
+          const float2 b = make_float2(fmaf(s1, acc[n][2], z1 * qs[n][g][0]), fmaf(s1, acc[n][3], z1 * qs[n][g][1]));
+          x[i][n][0] = g == 0 ? a : add2(x[i][n][0], a);
+          x[i][n][1] = g == 0 ? b : add2(x[i][n][1], b);
+        }
       }
       const int pos = k0 + i * 16 + r;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (edge && (pos + (e >> 1) * 8 >= lim[n][e & 1] || !(there >> i & 1))) x[i][n][e] = -INFINITY;
-          mx[n][e & 1] = fmaxf(mx[n][e & 1], x[i][n][e]);
+      for (int n = 0; n < NT; ++n) {
+        if (edge) {
+          const bool here = there >> i & 1;
+          if (!here || pos >= lim[n][0]) x[i][n][0].x = -INFINITY;
+          if (!here || pos >= lim[n][1]) x[i][n][0].y = -INFINITY;
+          if (!here || pos + 8 >= lim[n][0]) x[i][n][1].x = -INFINITY;
+          if (!here || pos + 8 >= lim[n][1]) x[i][n][1].y = -INFINITY;
         }
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xffffffffu, mx[n][e], off));
-        if (mx[n][e] != m[n][e]) {
-          const float corr = ex2(m[n][e] - mx[n][e]);
-          l[n][e] *= corr;
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            zacc[n][g][e] *= corr;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) o[n][g][q][e] *= corr, o[n][g][q][e + 2] *= corr;
-          }
-          m[n][e] = mx[n][e];
-        }
+        mx[n][0] = max3(mx[n][0], x[i][n][0].x, x[i][n][1].x);
+        mx[n][1] = max3(mx[n][1], x[i][n][0].y, x[i][n][1].y);
       }
     }
+    // The reference of the weights moves only when some row's maximum passes
+    // it by 2^8: the sums stay far inside fp32 and most steps rescale nothing.
+    bool moved = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) moved |= mx[n][0] > m[n].x + 8.f || mx[n][1] > m[n].y + 8.f;
+    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float next[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          next[e] = fmaxf(mx[n][e], e ? m[n].y : m[n].x);
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) next[e] = fmaxf(next[e], __shfl_xor_sync(0xffffffffu, next[e], off));
+        }
+        // nothing seen yet: sums are zero, whatever they are scaled by
+        const float c0 = m[n].x == -INFINITY ? 0.f : ex2(m[n].x - next[0]), c1 = m[n].y == -INFINITY ? 0.f : ex2(m[n].y - next[1]);
+        l[n].x *= c0, l[n].y *= c1;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          zacc[n][g][0] *= c0, zacc[n][g][1] *= c1;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) o[n][g][q][0] *= c0, o[n][g][q][1] *= c1, o[n][g][q][2] *= c0, o[n][g][q][3] *= c1;
+        }
+        m[n] = make_float2(next[0], next[1]);
+      }
+    }
+    float2 minus[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) minus[n] = make_float2(-m[n].x, -m[n].y);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float w = ex2(x[i][n][e] - m[n][e & 1]);
-          x[i][n][e] = edge && x[i][n][e] == -INFINITY ? 0.f : w;
-          l[n][e & 1] += x[i][n][e];
+        for (int u = 0; u < 2; ++u) {
+          const float2 y = add2(x[i][n][u], minus[n]);
+          float2 w = make_float2(ex2(y.x), ex2(y.y));
+          if (edge) {
+            if (x[i][n][u].x == -INFINITY) w.x = 0.f;
+            if (x[i][n][u].y == -INFINITY) w.y = 0.f;
+          }
+          x[i][n][u] = w;
+          l[n] = add2(l[n], w);
         }
 #pragma unroll
       for (int g = 0; g < G; ++g) {
@@ -286,29 +336,35 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
         // bits, so there P goes in as the sum of two.
         uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t sz = u ? szv[i][g].y : szv[i][g].x;
+          const float sv = X::lo(sz), zv = X::hi(sz);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float p0 = x[i][n][2 * u], p1 = x[i][n][2 * u + 1];
-            float a = p0 * sv[i][u][g], b = p1 * sv[i][u][g], za = p0 * zv[i][u][g], zb = p1 * zv[i][u][g];
+          for (int n = 0; n < NT; ++n) {
+            const float2 w = x[i][n][u];
+            float a = w.x * sv, b = w.y * sv;
             if (edge) {  // a weight of 0 stays 0 whatever the position holds
-              a = p0 == 0.f ? 0.f : a, za = p0 == 0.f ? 0.f : za;
-              b = p1 == 0.f ? 0.f : b, zb = p1 == 0.f ? 0.f : zb;
+              a = w.x == 0.f ? 0.f : a, b = w.y == 0.f ? 0.f : b;
+              zacc[n][g][0] += w.x == 0.f ? 0.f : w.x * zv;
+              zacc[n][g][1] += w.y == 0.f ? 0.f : w.y * zv;
+            } else {
+              zacc[n][g][0] = fmaf(w.x, zv, zacc[n][g][0]);
+              zacc[n][g][1] = fmaf(w.y, zv, zacc[n][g][1]);
             }
-            zacc[n][g][0] += za, zacc[n][g][1] += zb;
             const uint32_t h = pack_bf16(a, b);
             ph[n][u] = transpose8x8(h);
             if (kSplitP)
               pl[n][u] = transpose8x8(pack_bf16(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u)));
           }
+        }
         const uint4 w = *reinterpret_cast<const uint4 *>(buf + (g * 4 + i) * kKv4Rec + kKv4ValOff + lane * 16);
 #define WF_VSTEP(Q)                                                                                             \
   {                                                                                                             \
-    const __nv_bfloat16 b = __nv_bfloat16();                                                                    \
-    const uint32_t a[4] = {codes_of<Q>(w.x, b), codes_of<Q>(w.y, b), codes_of<Q>(w.z, b), codes_of<Q>(w.w, b)}; \
+    using C = Codes<__nv_bfloat16>;                                                                             \
+    const uint32_t a[4] = {C::exact<Q>(w.x), C::exact<Q>(w.y), C::exact<Q>(w.z), C::exact<Q>(w.w)};             \
     _Pragma("unroll") for (int n = 0; n < NT; ++n) {                                                            \
-      mma16(o[n][g][Q], a, ph[n][0], ph[n][1], b);                                                              \
-      if (kSplitP) mma16(o[n][g][Q], a, pl[n][0], pl[n][1], b);                                                 \
+      mma16(o[n][g][Q], a, ph[n][0], ph[n][1], __nv_bfloat16());                                                \
+      if (kSplitP) mma16(o[n][g][Q], a, pl[n][0], pl[n][1], __nv_bfloat16());                                   \
     }                                                                                                           \
   }
         WF_VSTEP(0) WF_VSTEP(1) WF_VSTEP(2) WF_VSTEP(3)
@@ -343,14 +399,15 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      float le = e ? l[n].y : l[n].x;
 #pragma unroll
       for (int off = 4; off < 32; off <<= 1) {
-        l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], off);
+        le += __shfl_xor_sync(0xffffffffu, le, off);
 #pragma unroll
         for (int g = 0; g < G; ++g) zacc[n][g][e] += __shfl_xor_sync(0xffffffffu, zacc[n][g][e], off);
       }
       const int row = warp * kRows + n * 8 + 2 * t + e;
-      if (r == 0) sm_m[row] = m[n][e], sm_l[row] = l[n][e];
+      if (r == 0) sm_m[row] = e ? m[n].y : m[n].x, sm_l[row] = le;
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
