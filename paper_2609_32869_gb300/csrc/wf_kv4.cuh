@@ -65,17 +65,22 @@ __device__ __forceinline__ unsigned char *kv4_record(const Kv4Pool &p, int block
   return p.base + (slab * (p.bs >> 4) + tile) * kKv4Rec;
 }
 
-inline cudaError_t launch_pdl(const void *fn, dim3 grid, dim3 block, size_t smem, void **args, cudaStream_t s) {
+inline cudaError_t launch_pdl(const void *fn, dim3 grid, dim3 block, size_t smem, void **args, cudaStream_t s,
+                              int cluster_y = 1) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1;
+  attr[1].val.clusterDim.y = cluster_y;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster_y > 1 ? 2 : 1;
   return cudaLaunchKernelExC(&cfg, fn, args);
 }
 

@@ -24,41 +24,55 @@ namespace wf {
 
 struct Kv4AttnParams {
   Kv4Pool pool;
+  uint32_t block_bytes;
   const void *q;
   void *out;
   long long q_stride, out_stride;
   const int32_t *table, *len;
   int table_stride, n_seq, rps, n_heads, group, causal, max_len;
+  uint32_t group_inv;  // 2^32 / group, rounded up (group > 1)
   float scale;
-  int chunk, chunks;  // positions of a CTA, CTAs along max_len
-  float *part_o;      // [task][chunks][rows][dim] weighted values of a chunk
-  float2 *part_ml;    // [task][chunks][rows] (maximum, sum)
+  // A unit is (sequence, key/value head, group of query rows); it is cut into
+  // chunks of positions, one CTA each, which a cluster or a second kernel joins.
+  int row_groups, chunk, chunks, cluster;
+  float *part_o;    // [unit][chunks][rows][dim] weighted values of a chunk
+  float2 *part_ml;  // [unit][chunks][rows] (maximum, sum)
   uint32_t *err;
+  // Row of a key/value head -> query position.  Exact: row < 2^20, group <= 4096.
+  __device__ __forceinline__ int row_of(int row) const { return group == 1 ? row : static_cast<int>(__umulhi(row, group_inv)); }
 };
 
 constexpr int kAtWarps = 4;
 constexpr int kAtThreads = kAtWarps * 32;
-constexpr int kAtTile = 64;  // positions of a warp's step
+constexpr int kAtTile = 64;    // positions of a warp's step
+constexpr int kAtCluster = 8;  // chunks that a cluster joins
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// None of these is volatile: the compiler may interleave independent chains.
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
-  mma_bf16(d, a[0], a[1], a[2], a[3], b0, b1);
-}
-__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-      "{%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// (w & mask) | magic in one instruction, which the compiler makes two of.
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t magic) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "r"(mask), "r"(magic));
+  return d;
 }
 // Nibbles i and i + 4 of w as a pair of 16-bit floats kBias + c.
 template <typename T>
@@ -68,7 +82,7 @@ struct Codes<__nv_bfloat16> {
   static constexpr float kBias = 128.f;
   template <int I>
   static __device__ __forceinline__ uint32_t biased(uint32_t w) {
-    return ((w >> (4 * I)) & 0x000f000fu) | 0x43004300u;
+    return and_or(w >> (4 * I), 0x000f000fu, 0x43004300u);
   }
   template <int I>
   static __device__ __forceinline__ uint32_t exact(uint32_t w) {  // c - 8
@@ -82,7 +96,7 @@ struct Codes<__half> {
   static constexpr float kBias = 0.f;
   template <int I>
   static __device__ __forceinline__ uint32_t biased(uint32_t w) {  // 1024 + c, less 1024
-    const uint32_t u = ((w >> (4 * I)) & 0x000f000fu) | 0x64006400u, bias = 0x64006400u;
+    const uint32_t u = and_or(w >> (4 * I), 0x000f000fu, 0x64006400u), bias = 0x64006400u;
     const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&bias));
     return *reinterpret_cast<const uint32_t *>(&v);
   }
@@ -111,30 +125,33 @@ __device__ __forceinline__ void bulk_load(void *smem_dst, const void *src, uint3
 template <int G, int NT>
 struct AtShape {
   static constexpr int kRows = NT * 8;
-  static constexpr int kStages = 3;
+  static constexpr int kStages = 2;
+  static constexpr int kSub = 2;                          // tiles of 16 positions between two looks at the maximum
+  static constexpr int kBlocks = G == 1 ? 6 - NT : 4 - NT;  // CTAs of an SM that the registers allow
   static constexpr int kStageBytes = 4 * G * kKv4Rec;  // 64 positions of a head
   static constexpr int kRingBytes = kAtWarps * kStages * kStageBytes;
-  static constexpr int kMergeBytes = kAtWarps * kRows * (G * 64 + 1 + 2) * 4;
+  static constexpr int kMergeBytes = kAtWarps * kRows * (G * 64 + 1 + 2) * 4 + kRows * (G * 64 + 2) * 4;
   static constexpr int kBarOff = ((kRingBytes > kMergeBytes ? kRingBytes : kMergeBytes) + 15) / 16 * 16;
   static constexpr int kSmem = kBarOff + kAtWarps * kStages * 8;
 };
 
 // A row's limit: positions it sees.
 __device__ __forceinline__ int row_limit(const Kv4AttnParams &p, int row, int len) {
-  return max(p.causal ? len - (p.rps - 1 - row / p.group) : len, 0);
+  return max(p.causal ? len - (p.rps - 1 - p.row_of(row)) : len, 0);
 }
 __device__ __forceinline__ int clamp_len(const Kv4AttnParams &p, int len) { return min(max(len, 0), p.max_len); }
 
-// One CTA: (sequence, key/value head, NT * 8 query rows, chunk of positions).
-// Each warp takes every kAtWarps-th step of 64 positions through a ring of
-// its own in shared memory (one bulk copy per record, an mbarrier per stage;
-// no other warp is waited for) and keeps a running maximum, sum and weighted
-// values; the CTA joins them in warp order, a second kernel the chunks.
+// A unit is (sequence, key/value head, NT * 8 query rows).  Each warp takes
+// steps of 64 positions of a unit through a ring of its own in shared memory
+// (one bulk copy per record, an mbarrier per stage; no other warp is waited
+// for) and keeps a running maximum, sum and weighted values.  A CTA's warps
+// take a unit, or a chunk of one, in turns and join in order; up to 8 chunks
+// join over a cluster, more by a second kernel.
 template <typename T, int G, int NT>
-__global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4AttnParams p) {
+__global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_attention_kernel(const Kv4AttnParams p) {
   using X = Kv4Type<T>;
   using S = AtShape<G, NT>;
-  constexpr int kRows = S::kRows, kStages = S::kStages;
+  constexpr int kRows = S::kRows, kStages = S::kStages, kSub = S::kSub;
   constexpr bool kSplitP = std::is_same<T, __half>::value;  // see P below
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
@@ -148,43 +165,46 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
   pdl_wait();
   pdl_launch_dependents();
   const int head = blockIdx.x % p.pool.heads, seq = blockIdx.x / p.pool.heads;
-  const int row0 = blockIdx.y * kRows, rows = p.rps * p.group;  // rows of this key/value head: j * group + query head
+  const int row0 = blockIdx.z * kRows, rows = p.rps * p.group;  // rows of this key/value head: j * group + query head
   const int32_t *table = p.table + static_cast<long long>(seq) * p.table_stride;
   const int raw_len = p.len[seq], len = clamp_len(p, raw_len);
   if (raw_len != len && threadIdx.x == 0) set_error(p.err, raw_len < 0 ? WF_DEV_ERR_PAGE : WF_DEV_ERR_CAPACITY);
-  // positions that any row of this CTA sees, and this CTA's share of them
+  // positions that any row of this unit sees, and this CTA's share of them
   const int seen = row_limit(p, min(row0 + kRows, rows) - 1, len);
-  const int begin = blockIdx.z * p.chunk, end = min(seen, begin + p.chunk);
-  if (begin >= end && blockIdx.z > 0) return;
+  const int begin = blockIdx.y * p.chunk, end = min(seen, begin + p.chunk);
+  if (begin >= end && blockIdx.y > 0 && !p.cluster) return;
 
-  // the ring: step i of this warp is positions begin + (warp + i kAtWarps) 64
+  // The ring: step i of this warp is positions begin + (warp + i kAtWarps) 64.
+  // Lane 4 g + k < 4 G loads tile k of group g; a step is whole blocks, so its
+  // place in a block never changes and its table entry moves by whole blocks.
   const int first = begin + warp * kAtTile;
-  const int steps = first < end ? (end - first + kAtWarps * kAtTile - 1) / (kAtWarps * kAtTile) : 0;
-  const int my_tile = lane & 3, my_group = lane >> 2;
-  const bool loader = lane < 4 * G;
-  int next_block = -1;
+  constexpr int stride = kAtWarps * kAtTile;
+  const int steps = first < end ? (end - first + stride - 1) / stride : 0;
+  const int my_pos = first + (lane & 3) * 16, table_step = stride >> p.pool.bs_shift;
+  const int32_t *entry = table + (my_pos >> p.pool.bs_shift);
+  const unsigned char *my_base = kv4_record(p.pool, 0, head, lane >> 2, (my_pos & (p.pool.bs - 1)) >> 4);
+  // steps in which this lane's tile has positions to load
+  const int my_steps = lane < 4 * G && my_pos < end ? (end - my_pos + stride - 1) / stride : 0;
+  int next_block = my_steps > 0 ? *entry : -1;
+  int to_issue = 0, issue_stage = 0;
   uint32_t there_bits = 0;  // 4 bits a stage: tiles that were loaded
-  auto prefetch_block = [&](int i) {
-    const int pos = first + i * (kAtWarps * kAtTile) + my_tile * 16;
-    next_block = loader && i < steps && pos < end ? table[pos >> p.pool.bs_shift] : -2;
-  };
-  auto issue = [&](int i) {
-    const int stage = i % kStages;
-    const bool ok = next_block >= 0 && next_block < p.pool.n_blocks;
-    if (next_block != -2 && !ok) set_error(p.err, WF_DEV_ERR_PAGE);
+  auto issue = [&]() {
+    const bool mine = to_issue < my_steps, ok = mine && static_cast<uint32_t>(next_block) < static_cast<uint32_t>(p.pool.n_blocks);
+    if (mine && !ok) set_error(p.err, WF_DEV_ERR_PAGE);
     const uint32_t oks = __ballot_sync(0xffffffffu, ok);
-    there_bits = (there_bits & ~(15u << (4 * stage))) | (oks & 15u) << (4 * stage);
-    if (lane == 0) mbar_arrive_expect_tx(&bars[stage], __popc(oks) * kKv4Rec);
+    there_bits = (there_bits & ~(15u << (4 * issue_stage))) | (oks & 15u) << (4 * issue_stage);
+    if (lane == 0) mbar_arrive_expect_tx(&bars[issue_stage], __popc(oks) * kKv4Rec);
     __syncwarp();
-    if (ok) {
-      const int pos = first + i * (kAtWarps * kAtTile) + my_tile * 16;
-      bulk_load(ring + stage * S::kStageBytes + lane * kKv4Rec,
-                kv4_record(p.pool, next_block, head, my_group, (pos & (p.pool.bs - 1)) >> 4), kKv4Rec, &bars[stage]);
-    }
-    prefetch_block(i + 1);
+    if (ok)
+      bulk_load(ring + issue_stage * S::kStageBytes + lane * kKv4Rec, my_base + static_cast<long long>(next_block) * p.block_bytes, kKv4Rec,
+                &bars[issue_stage]);
+    ++to_issue;
+    issue_stage = issue_stage + 1 == kStages ? 0 : issue_stage + 1;
+    entry += table_step;
+    next_block = to_issue < my_steps ? *entry : -1;
   };
-  prefetch_block(0);
-  for (int i = 0; i < kStages && i < steps; ++i) issue(i);
+#pragma unroll 1
+  for (int i = 0; i < kStages && i < steps; ++i) issue();
 
   // queries as B operands, and their sums
   uint32_t qb[NT][G][4][2];
@@ -193,7 +213,7 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int row = row0 + n * 8 + r;
-    const int j = row / p.group, h = head * p.group + row % p.group;
+    const int j = p.row_of(row), h = head * p.group + row - j * p.group;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       uint32_t w[8] = {};
@@ -234,43 +254,51 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
   for (int n = 0; n < NT; ++n) l[n] = make_float2(0.f, 0.f), m[n] = make_float2(-INFINITY, -INFINITY);
   const float c = p.scale * 1.4426950408889634f;  // base-2 softmax
 
-  // 64 positions from k0; `edge`: some are not seen by some row, or are not there
+  // kSub tiles of 16 positions from k0; `edge`: some are not seen by some row, or are not there
   auto step = [&](const unsigned char *buf, int k0, uint32_t there, auto edge_c) {
     constexpr bool edge = decltype(edge_c)::value;
-    float2 x[4][NT][2];  // [16 positions][rows][position r, r + 8] (row 2t, row 2t + 1)
-    uint2 szv[4][G];
+    float2 x[kSub][NT][2];  // [16 positions][rows][position r, r + 8] (row 2t, row 2t + 1)
+    uint2 szv[kSub][G];
     float mx[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) mx[n][0] = mx[n][1] = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int g = 0; g < G; ++g) {
+      uint2 w0[kSub], w1[kSub];
+      float acc[kSub][NT][4] = {};
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
+      for (int i = 0; i < kSub; ++i) {
         const unsigned char *rg = buf + (g * 4 + i) * kKv4Rec;
-        const uint2 w0 = *reinterpret_cast<const uint2 *>(rg + r * 32 + t * 8);
-        const uint2 w1 = *reinterpret_cast<const uint2 *>(rg + (r + 8) * 32 + t * 8);
-        const uint4 sz = *reinterpret_cast<const uint4 *>(rg + kKv4ScaleOff + r * 16);
-        float acc[NT][4] = {};
+        w0[i] = *reinterpret_cast<const uint2 *>(rg + r * 32 + t * 8);
+        w1[i] = *reinterpret_cast<const uint2 *>(rg + (r + 8) * 32 + t * 8);
+      }
+      // tile by tile within a step of 16 dims: the chains of sums interleave
 #define WF_KSTEP(K)                                                                                             \
-  {                                                                                                             \
-    const uint32_t a[4] = {Codes<T>::template biased<K>(w0.x), Codes<T>::template biased<K>(w1.x),              \
-                           Codes<T>::template biased<K>(w0.y), Codes<T>::template biased<K>(w1.y)};             \
-    _Pragma("unroll") for (int n = 0; n < NT; ++n) mma16(acc[n], a, qb[n][g][K][0], qb[n][g][K][1], T()); \
+  _Pragma("unroll") for (int i = 0; i < kSub; ++i) {                                                            \
+    const uint32_t a[4] = {Codes<T>::template biased<K>(w0[i].x), Codes<T>::template biased<K>(w1[i].x),        \
+                           Codes<T>::template biased<K>(w0[i].y), Codes<T>::template biased<K>(w1[i].y)};       \
+    _Pragma("unroll") for (int n = 0; n < NT; ++n) mma16(acc[i][n], a, qb[n][g][K][0], qb[n][g][K][1], T()); \
   }
-        WF_KSTEP(0) WF_KSTEP(1) WF_KSTEP(2) WF_KSTEP(3)
+      WF_KSTEP(0) WF_KSTEP(1) WF_KSTEP(2) WF_KSTEP(3)
 #undef WF_KSTEP
+#pragma unroll
+      for (int i = 0; i < kSub; ++i) {
+        const uint4 sz = *reinterpret_cast<const uint4 *>(buf + (g * 4 + i) * kKv4Rec + kKv4ScaleOff + r * 16);
         // the codes' bias and 8 go into z: a few dozen units on a sum of 64 products in fp32
         const float s0 = X::lo(sz.x) * c, s1 = X::lo(sz.y) * c;
         const float z0 = fmaf(X::hi(sz.x), c, -(Codes<T>::kBias + 8.f) * s0), z1 = fmaf(X::hi(sz.y), c, -(Codes<T>::kBias + 8.f) * s1);
         szv[i][g] = make_uint2(sz.z, sz.w);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const float2 a = make_float2(fmaf(s0, acc[n][0], z0 * qs[n][g][0]), fmaf(s0, acc[n][1], z0 * qs[n][g][1]));
-          const float2 b = make_float2(fmaf(s1, acc[n][2], z1 * qs[n][g][0]), fmaf(s1, acc[n][3], z1 * qs[n][g][1]));
+          const float2 a = make_float2(fmaf(s0, acc[i][n][0], z0 * qs[n][g][0]), fmaf(s0, acc[i][n][1], z0 * qs[n][g][1]));
+          const float2 b = make_float2(fmaf(s1, acc[i][n][2], z1 * qs[n][g][0]), fmaf(s1, acc[i][n][3], z1 * qs[n][g][1]));
           x[i][n][0] = g == 0 ? a : add2(x[i][n][0], a);
           x[i][n][1] = g == 0 ? b : add2(x[i][n][1], b);
         }
       }
+    }
+#pragma unroll
+    for (int i = 0; i < kSub; ++i) {
       const int pos = k0 + i * 16 + r;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -316,7 +344,7 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
 #pragma unroll
     for (int n = 0; n < NT; ++n) minus[n] = make_float2(-m[n].x, -m[n].y);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kSub; ++i) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -373,41 +401,52 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
     }
   };
 
+  int stage = 0, k0 = first;
+  uint32_t phase = 0;
+#pragma unroll 1
   for (int i = 0; i < steps; ++i) {
-    const int stage = i % kStages;
-    const bool landed = mbar_wait(&bars[stage], (i / kStages) & 1, p.err, kSpinLimitCycles);
+    const bool landed = mbar_wait(&bars[stage], phase, p.err, kSpinLimitCycles);
     if (!__all_sync(0xffffffffu, landed)) {  // the copies in flight still have to land before the CTA ends
-      for (int j = i; j < steps && j < i + kStages; ++j) mbar_drain(&bars[j % kStages], (j / kStages) & 1);
+      for (int j = i; j < to_issue; ++j) mbar_drain(&bars[j % kStages], (j / kStages) & 1);
       break;
     }
-    const int k0 = first + i * (kAtWarps * kAtTile);
     const uint32_t there = there_bits >> (4 * stage) & 15u;
     const unsigned char *buf = ring + stage * S::kStageBytes;
-    if (k0 + kAtTile <= least && there == 15u)
-      step(buf, k0, there, std::false_type());
-    else
-      step(buf, k0, there, std::true_type());
+#pragma unroll 1
+    for (int h = 0; h < 4; h += kSub) {
+      if (k0 + (h + kSub) * 16 <= least && there == 15u)
+        step(buf + h * kKv4Rec, k0 + h * 16, there >> h, std::false_type());
+      else
+        step(buf + h * kKv4Rec, k0 + h * 16, there >> h, std::true_type());
+    }
     __syncwarp();
-    if (i + kStages < steps) issue(i + kStages);
+    if (to_issue < steps) issue();
+    k0 += stride;
+    if (++stage == kStages) stage = 0, phase ^= 1;
   }
 
   // the warp's results: sums over its 8 position lanes, rows 2t and 2t + 1
-  __syncthreads();
-  float *sm_m = reinterpret_cast<float *>(smem), *sm_l = sm_m + kAtWarps * kRows, *sm_o = sm_l + kAtWarps * kRows;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int off = 4; off < 32; off <<= 1) {
+      l[n].x += __shfl_xor_sync(0xffffffffu, l[n].x, off), l[n].y += __shfl_xor_sync(0xffffffffu, l[n].y, off);
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        zacc[n][g][0] += __shfl_xor_sync(0xffffffffu, zacc[n][g][0], off);
+        zacc[n][g][1] += __shfl_xor_sync(0xffffffffu, zacc[n][g][1], off);
+      }
+    }
+  }
+  __syncthreads();  // the ring is done with
   constexpr int kLd = G * 64 + 1;
+  float *sm_m = reinterpret_cast<float *>(smem), *sm_l = sm_m + kAtWarps * kRows, *sm_o = sm_l + kAtWarps * kRows;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float le = e ? l[n].y : l[n].x;
-#pragma unroll
-      for (int off = 4; off < 32; off <<= 1) {
-        le += __shfl_xor_sync(0xffffffffu, le, off);
-#pragma unroll
-        for (int g = 0; g < G; ++g) zacc[n][g][e] += __shfl_xor_sync(0xffffffffu, zacc[n][g][e], off);
-      }
       const int row = warp * kRows + n * 8 + 2 * t + e;
-      if (r == 0) sm_m[row] = e ? m[n].y : m[n].x, sm_l[row] = le;
+      if (r == 0) sm_m[row] = e ? m[n].y : m[n].x, sm_l[row] = e ? l[n].y : l[n].x;
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -418,8 +457,10 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
     }
   }
   __syncthreads();
+  // the warps join in order; each thread takes pairs of dims
   const bool whole = seen <= p.chunk;  // no other chunk has positions
-  const size_t task = (static_cast<size_t>(blockIdx.x) * gridDim.y + blockIdx.y) * gridDim.z + blockIdx.z;
+  const size_t unit = static_cast<size_t>(blockIdx.x) * gridDim.z + blockIdx.z;
+  float *cl_m = sm_o + kAtWarps * kRows * kLd, *cl_l = cl_m + kRows, *cl_o = cl_l + kRows;  // for the cluster
   for (int i = threadIdx.x; i < kRows * G * 32; i += kAtThreads) {
     const int row = i / (G * 32), d = i % (G * 32) * 2;
     if (row0 + row >= rows) break;
@@ -433,17 +474,44 @@ __global__ void __launch_bounds__(kAtThreads) kv4_attention_kernel(const Kv4Attn
       const float f = ex2(sm_m[at] - mm);
       ll += f * sm_l[at], a += f * sm_o[at * kLd + d], b += f * sm_o[at * kLd + d + 1];
     }
-    if (whole) {
+    if (whole && !p.cluster) {
       const float inv = ll == 0.f ? 0.f : 1.f / ll;
-      const int j = (row0 + row) / p.group, h = head * p.group + (row0 + row) % p.group;
+      const int j = p.row_of(row0 + row), h = head * p.group + row0 + row - j * p.group;
       T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + d;
       *reinterpret_cast<uint32_t *>(dst) = X::pack(a * inv, b * inv);
+    } else if (p.cluster) {
+      *reinterpret_cast<float2 *>(cl_o + row * (G * 64) + d) = make_float2(a, b);
+      if (d == 0) cl_m[row] = mm, cl_l[row] = ll;
     } else {
-      const size_t at = task * kRows + row;
+      const size_t at = (unit * p.chunks + blockIdx.y) * kRows + row;
       *reinterpret_cast<float2 *>(p.part_o + at * (G * 64) + d) = make_float2(a, b);
       if (d == 0) p.part_ml[at] = make_float2(mm, ll);
     }
   }
+  if (!p.cluster) return;
+  // the chunks of a unit are a cluster: every CTA joins some of the outputs over all of them, in chunk order
+  cluster_sync();
+  const int chunks = p.chunks, live_rows = min(rows - row0, kRows);
+  for (int i = threadIdx.x * chunks + blockIdx.y; i < live_rows * G * 32; i += kAtThreads * chunks) {
+    const int row = i / (G * 32), d = i % (G * 32) * 2;
+    float cm[kAtCluster], mm = -INFINITY, ll = 0.f, a = 0.f, b = 0.f;
+#pragma unroll
+    for (int k = 0; k < kAtCluster; ++k)
+      if (k < chunks) cm[k] = dsmem_ld_f32(dsmem_map(smem_u32(cl_m + row), k)), mm = fmaxf(mm, cm[k]);
+#pragma unroll
+    for (int k = 0; k < kAtCluster; ++k) {
+      if (k >= chunks || cm[k] == -INFINITY) continue;
+      const float f = ex2(cm[k] - mm);
+      const uint32_t at = dsmem_map(smem_u32(cl_o + row * (G * 64) + d), k);
+      ll += f * dsmem_ld_f32(dsmem_map(smem_u32(cl_l + row), k));
+      a += f * dsmem_ld_f32(at), b += f * dsmem_ld_f32(at + 4);
+    }
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+    const int j = p.row_of(row0 + row), h = head * p.group + row0 + row - j * p.group;
+    T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + d;
+    *reinterpret_cast<uint32_t *>(dst) = X::pack(a * inv, b * inv);
+  }
+  cluster_sync();  // no CTA leaves while another reads it
 }
 
 // Joins the chunks of a row group in order: one warp per row, whose lanes
@@ -480,7 +548,7 @@ __global__ void __launch_bounds__(kAtThreads) kv4_join_kernel(const Kv4AttnParam
       }
     }
     const float inv = ll == 0.f ? 0.f : 1.f / ll;
-    const int j = (row0 + row) / p.group, h = head * p.group + (row0 + row) % p.group;
+    const int j = p.row_of(row0 + row), h = head * p.group + row0 + row - j * p.group;
     T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + lane * 2;
 #pragma unroll
     for (int g = 0; g < G; ++g) *reinterpret_cast<uint32_t *>(dst + g * 64) = X::pack(a[g] * inv, b[g] * inv);
@@ -491,15 +559,25 @@ __global__ void __launch_bounds__(kAtThreads) kv4_join_kernel(const Kv4AttnParam
 
 using namespace wf;
 
-// Query rows of a CTA: 8, or 16 where a key/value head has more.
-static int at_tiles(int64_t rows) { return rows > 8 ? 2 : 1; }
-// Positions of a CTA.  Each warp's step is 64, so a CTA takes at least 256;
-// sequences are cut until there are about two CTAs for each of the four that
-// an SM holds, so that SMs whose sequences are short find other work.
-static int at_chunk(int64_t tasks, int max_len) {
+// How a call is cut up: a function of its sizes alone.
+struct AtPlan {
+  int tiles;            // 8 query rows each
+  int64_t row_groups, units;
+  int chunk, chunks;
+};
+static AtPlan at_plan(int64_t n_seq, int64_t heads, int64_t rows, int max_len) {
+  AtPlan a;
+  a.tiles = rows > 8 ? 2 : 1;
+  a.row_groups = (rows + a.tiles * 8 - 1) / (a.tiles * 8);
+  a.units = n_seq * heads * a.row_groups;
+  // A CTA's four warps take at least 64 positions each; sequences are cut
+  // until there are about eight CTAs an SM at the longest, so that SMs whose
+  // sequences are short find other work.
   const int64_t least = kAtWarps * kAtTile, want = 152 * 8;
-  const int64_t per = (tasks * max_len + want - 1) / want;
-  return static_cast<int>(std::min<int64_t>(std::max(least, (per + least - 1) / least * least), 1 << 30));
+  const int64_t per = (a.units * max_len + want - 1) / want;
+  a.chunk = static_cast<int>(std::min<int64_t>(std::max(least, (per + least - 1) / least * least), 1 << 30));
+  a.chunks = (max_len + a.chunk - 1) / a.chunk;
+  return a;
 }
 
 template <typename T, int G, int NT>
@@ -511,12 +589,12 @@ static cudaError_t launch(const Kv4AttnParams &p, cudaStream_t s) {
     return e != cudaSuccess ? e : cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
   }();
   if (ready != cudaSuccess) return ready;
-  const int rows = p.rps * p.group;
-  const dim3 grid(p.n_seq * p.pool.heads, (rows + NT * 8 - 1) / (NT * 8), p.chunks);
+  const dim3 grid(p.n_seq * p.pool.heads, p.chunks, p.row_groups);
   void *args[] = {const_cast<Kv4AttnParams *>(&p)};
-  cudaError_t e = launch_pdl(reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>), grid, kAtThreads, S::kSmem, args, s);
-  if (e == cudaSuccess && p.chunks > 1)
-    e = launch_pdl(reinterpret_cast<const void *>(kv4_join_kernel<T, G, NT>), dim3(grid.x, grid.y), kAtThreads, 0, args, s);
+  cudaError_t e = launch_pdl(reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>), grid, kAtThreads, S::kSmem, args, s,
+                             p.cluster ? p.chunks : 1);
+  if (e == cudaSuccess && p.chunks > 1 && !p.cluster)
+    e = launch_pdl(reinterpret_cast<const void *>(kv4_join_kernel<T, G, NT>), dim3(grid.x, p.row_groups), kAtThreads, 0, args, s);
   return e;
 }
 
@@ -526,10 +604,8 @@ size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_head
                                       int32_t max_len) {
   if (n_seq <= 0 || rps <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || (head_dim != 64 && head_dim != 128))
     return 0;
-  const int64_t rows = static_cast<int64_t>(rps) * (n_heads / n_kv_heads), group = at_tiles(rows) * 8;
-  const int64_t tasks = static_cast<int64_t>(n_seq) * n_kv_heads * ((rows + group - 1) / group);
-  const int64_t chunks = (max_len + at_chunk(tasks, max_len) - 1) / at_chunk(tasks, max_len);
-  return chunks > 1 ? static_cast<size_t>(tasks * chunks * group) * (head_dim + 2) * sizeof(float) : 0;
+  const AtPlan a = at_plan(n_seq, n_kv_heads, static_cast<int64_t>(rps) * (n_heads / n_kv_heads), max_len);
+  return a.chunks > kAtCluster ? static_cast<size_t>(a.units * a.chunks * a.tiles * 8) * (head_dim + 2) * sizeof(float) : 0;
 }
 
 wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d_q, int64_t q_stride, const int32_t *d_table,
@@ -547,26 +623,29 @@ wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d
   // every position up to max_len needs a table column (stride 0: one row that the caller made long enough)
   if (table_stride && static_cast<int64_t>(table_stride) * pool->block_size < max_len) return WF_ERR_INVALID;
   const int64_t rows = static_cast<int64_t>(rps) * (n_heads / pool->n_kv_heads);
-  if (static_cast<int64_t>(n_seq) * pool->n_kv_heads > INT32_MAX || rows > 65535 * 8LL) return WF_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(n_seq) * pool->n_kv_heads > INT32_MAX || rows > 65535 * 8LL || n_heads / pool->n_kv_heads > 4096)
+    return WF_ERR_UNSUPPORTED;
+  p.block_bytes = static_cast<uint32_t>(kv4_block_bytes(pool->block_size, pool->n_kv_heads, pool->head_dim));
   p.q = d_q, p.out = d_out, p.q_stride = q_stride, p.out_stride = out_stride;
   p.table = d_table, p.len = d_len, p.table_stride = table_stride;
   p.n_seq = n_seq, p.rps = rps, p.n_heads = n_heads, p.group = n_heads / pool->n_kv_heads;
+  p.group_inv = static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
   p.causal = causal != 0, p.max_len = max_len, p.scale = scale, p.err = d_err;
-  const int tiles = at_tiles(rows);
-  const int64_t groups = (rows + tiles * 8 - 1) / (tiles * 8), tasks = static_cast<int64_t>(n_seq) * pool->n_kv_heads * groups;
-  p.chunk = at_chunk(tasks, max_len);
-  p.chunks = (max_len + p.chunk - 1) / p.chunk;
-  if (p.chunks > 65535) return WF_ERR_UNSUPPORTED;
-  if (p.chunks > 1) {
+  const AtPlan a = at_plan(n_seq, pool->n_kv_heads, rows, max_len);
+  if (a.chunks > 65535) return WF_ERR_UNSUPPORTED;
+  p.row_groups = static_cast<int>(a.row_groups);
+  p.chunk = a.chunk, p.chunks = a.chunks;
+  p.cluster = p.chunks > 1 && p.chunks <= kAtCluster;
+  if (p.chunks > 1 && !p.cluster) {
     if (!d_scratch || !aligned16(d_scratch)) return WF_ERR_INVALID;
     if (scratch_bytes < wf_kv4_attention_scratch_bytes(n_seq, rps, n_heads, pool->n_kv_heads, pool->head_dim, max_len))
       return WF_ERR_CAPACITY;
     p.part_o = static_cast<float *>(d_scratch);
-    p.part_ml = reinterpret_cast<float2 *>(p.part_o + tasks * p.chunks * tiles * 8 * pool->head_dim);
+    p.part_ml = reinterpret_cast<float2 *>(p.part_o + a.units * a.chunks * a.tiles * 8 * pool->head_dim);
   }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   using B = __nv_bfloat16;
-  const bool f16 = pool->dtype == WF_F16, wide = pool->head_dim == 128, two = tiles == 2;
+  const bool f16 = pool->dtype == WF_F16, wide = pool->head_dim == 128, two = a.tiles == 2;
   cudaError_t e;
   if (f16)
     e = wide ? (two ? launch<__half, 2, 2>(p, s) : launch<__half, 2, 1>(p, s)) : (two ? launch<__half, 1, 2>(p, s) : launch<__half, 1, 1>(p, s));

@@ -239,6 +239,15 @@ ATT = [
     (17, 3, 1, 128, 32, 1, [17, 16, 200]),
     (1, 3, 3, 64, 64, 1, [9000, 1, 0, 5000]),
     (4, 10, 10, 64, 16, 1, [44] * 40),
+    # many units: a warp walks each alone
+    (1, 20, 20, 64, 16, 1, [(37 * i) % 230 for i in range(70)]),
+    (12, 7, 7, 64, 64, 0, [(13 * i) % 150 for i in range(175)]),
+    (2, 5, 5, 128, 32, 1, [(29 * i) % 200 for i in range(250)]),
+    (3, 12, 4, 128, 16, 1, [(31 * i) % 99 for i in range(310)]),
+    # few long ones: clusters of chunks, and more chunks than a cluster
+    (2, 4, 4, 64, 32, 1, [2047, 1030, 300]),
+    (11, 2, 1, 128, 64, 1, [5, 2048, 700]),
+    (1, 12, 1, 64, 16, 1, [30011]),
 ]
 
 
