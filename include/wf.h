@@ -447,7 +447,8 @@ size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_head
                                       int32_t n_kv_heads, int32_t head_dim, int32_t max_len);
 
 /* One selection of beam search.  Beam w of request i has the logits row
- * i * beams + w (`dtype` WF_F32, WF_BF16 or WF_F16, ld elements apart) and
+ * i * beams + w (`dtype` WF_F32, WF_BF16 or WF_F16, ld elements apart, at any
+ * alignment of the type) and
  * the score d_scores[i * beams + w], the sum of its log-probabilities (-inf:
  * not in use).  A token's score is score + ((logit - max) - log(sum)) in fp32,
  * max the row's largest logit and sum that of exp(logit - max); ids with a nonzero d_suppress entry (nullable uint8
@@ -459,7 +460,7 @@ size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_head
  *       and -inf
  *   d_fin_parent int32, d_fin_score fp32 [n_req][beams]  hypotheses that end:
  *       eos among the first `beams` ranks; past the last one -1 and -inf
- * eos < 0: none ends.  2 beams <= vocab.  d_score may be d_scores. */
+ * eos < 0: none ends.  2 beams <= vocab <= 2^22.  d_score may be d_scores. */
 wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const float *d_scores,
                          const uint8_t *d_suppress, int32_t n_req, int32_t beams, int32_t vocab,
                          int32_t eos, int32_t *d_token, int32_t *d_parent, float *d_score,

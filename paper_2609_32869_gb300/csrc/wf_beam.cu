@@ -29,8 +29,9 @@ struct SelectParams {
   float *max;                // [rows][chunks]
 };
 constexpr int kSelThreads = 256;
-constexpr int kSelPer = 16;                         // logits of a thread
-constexpr int kSelChunk = kSelThreads * kSelPer;    // of a CTA
+constexpr int kSelPer = 16;                       // logits of a thread
+constexpr int kSelChunk = kSelThreads * kSelPer;  // of a CTA
+constexpr int kSelKeep = 512;                     // candidates of a chunk that are held
 
 // (value descending, index ascending) as one descending unsigned key; 0 is
 // below every key of a value above -inf.
@@ -44,124 +45,246 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
   return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
 }
 __device__ __forceinline__ uint32_t key_index(unsigned long long k) { return 0xffffffffu - static_cast<uint32_t>(k); }
+// The largest key of a warp: its upper word, then the largest lower word under it.
 __device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
-#pragma unroll
-  for (int off = 16; off; off >>= 1) {
-    const unsigned long long v = __shfl_xor_sync(0xffffffffu, k, off);
-    k = v > k ? v : k;
-  }
-  return k;
+  const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(k >> 32));
+  const uint32_t lo = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(k >> 32) == hi ? static_cast<uint32_t>(k) : 0u);
+  return static_cast<unsigned long long>(hi) << 32 | lo;
 }
-__device__ __forceinline__ float as_float(float v) { return v; }
-__device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float as_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int off = 16; off; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+  return v;
+}
+// Sorts a warp's values (keys), largest in lane 0: a bitonic network.
+template <typename K>
+__device__ __forceinline__ K warp_sort(K v, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+    for (int off = size >> 1; off; off >>= 1) {
+      const K w = __shfl_xor_sync(0xffffffffu, v, off);
+      const bool keep_max = ((lane & off) == 0) == ((lane & size) == 0);
+      v = keep_max ? (w > v ? w : v) : (w > v ? v : w);
+    }
+  return v;
+}
 
 template <typename T>
+struct Logits;
+template <>
+struct Logits<float> {
+  static constexpr int kVec = 4;
+  static __device__ __forceinline__ void unpack(uint4 v, float *x) {
+    x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ float one(float v) { return v; }
+};
+template <typename T>
+struct Logits16 {
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ void unpack(uint4 v, float *x) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = Kv4Type<T>::lo(w[i]), x[2 * i + 1] = Kv4Type<T>::hi(w[i]);
+  }
+};
+template <>
+struct Logits<__nv_bfloat16> : Logits16<__nv_bfloat16> {
+  static __device__ __forceinline__ float one(__nv_bfloat16 v) { return __bfloat162float(v); }
+};
+template <>
+struct Logits<__half> : Logits16<__half> {
+  static __device__ __forceinline__ float one(__half v) { return __half2float(v); }
+};
+
+// One CTA: 4096 logits of a row, 16 a thread in registers, by 16-byte loads
+// whatever the row's alignment (a chunk starts up to 15 bytes before a
+// multiple of 4096 logits; what lies outside the row is -inf).
+//
+// The k = 2 beams largest: of the 32 maxima over 128 logits each, the k-th is
+// a value that at least k logits reach and few more do; those are collected
+// and sorted by one warp.  Where many reach it (equal logits), k rounds over
+// the CTA pick them one by one.  The sum of exponentials adds 16 terms a
+// thread in fp32, the threads' in fixed point (2^-40), so it has no order.
+template <typename T>
 __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectParams p) {
-  pdl_wait();
-  pdl_launch_dependents();
-  const int chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  using L = Logits<T>;
+  constexpr int kVec = L::kVec, kVecs = kSelPer / kVec;
+  __shared__ float sm_g[32];
+  __shared__ unsigned long long sm_sum[kSelThreads / 32], sm_k[2][kSelThreads / 32], keep[kSelKeep];
+  __shared__ int kept;
+  __shared__ __align__(16) unsigned char mask[kSelChunk + 32];
+  const int chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = 2 * p.W;
   const long long row = blockIdx.y + static_cast<long long>(blockIdx.z) * 65535;
   if (row >= static_cast<long long>(p.n_req) * p.W) return;
+  if (tid == 0) kept = 0;
+  pdl_wait();
+  pdl_launch_dependents();
   const T *src = static_cast<const T *>(p.logits) + row * p.ld;
-  __shared__ float sm_m[kSelThreads / 32];
-  __shared__ double sm_s[kSelThreads / 32];
-  __shared__ unsigned long long sm_k[2][kSelThreads / 32];
+  const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
+  const int first = chunk * kSelChunk - skew;  // a multiple of 16 bytes from address 0
   float x[kSelPer];
-  float m = -INFINITY;
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) {
+    const int id = first + (v * kSelThreads + tid) * kVec;
+    if (id >= 0 && id + kVec <= p.V) {
+      L::unpack(*reinterpret_cast<const uint4 *>(src + id), x + v * kVec);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) x[v * kVec + e] = id + e >= 0 && id + e < p.V ? L::one(src[id + e]) : -INFINITY;
+    }
+  }
+  if (p.suppress) {  // its bytes by 16, from the multiple of 16 before the chunk; read back at the skew between the two
+    const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(p.suppress) + first) & 15);
+    for (int i = tid; i < kSelChunk / 16 + 1; i += kSelThreads) {
+      const int id = first - lead + i * 16;
+      if (id >= 0 && id + 16 <= p.V) {
+        *reinterpret_cast<uint4 *>(mask + i * 16) = *reinterpret_cast<const uint4 *>(p.suppress + id);
+      } else {
+        for (int e = 0; e < 16; ++e) mask[i * 16 + e] = id + e >= 0 && id + e < p.V ? p.suppress[id + e] : 0;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < kSelPer / 4; ++v) {
+      const int at = lead + ((v * 4 / kVec) * kSelThreads + tid) * kVec + v * 4 % kVec;
+      const uint32_t *word = reinterpret_cast<const uint32_t *>(mask) + (at >> 2);
+      const uint32_t w = __funnelshift_r(word[0], word[1], (at & 3) * 8);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (w & (0xffu << (8 * e))) x[v * 4 + e] = -INFINITY;
+    }
+  }
+  float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kSelPer; ++i) {
-    const int id = chunk * kSelChunk + i * kSelThreads + tid;
-    x[i] = id < p.V ? as_float(src[id]) : -INFINITY;
-    if (x[i] != x[i] || (id < p.V && p.suppress && p.suppress[id])) x[i] = -INFINITY;
-    m = fmaxf(m, x[i]);
+    if (x[i] != x[i]) x[i] = -INFINITY;
+    top = fmaxf(top, x[i]);
   }
-#pragma unroll
-  for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-  if (lane == 0) sm_m[warp] = m;
+  float g = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
+  g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
+  if ((lane & 7) == 0) sm_g[warp * 4 + (lane >> 3)] = g;
   __syncthreads();
-  for (int w = 0; w < kSelThreads / 32; ++w) m = fmaxf(m, sm_m[w]);
+  const float sorted = warp_sort(sm_g[lane], lane);
+  const float m = __shfl_sync(0xffffffffu, sorted, 0), floor_v = __shfl_sync(0xffffffffu, sorted, K - 1);
   float part = 0.f;
 #pragma unroll
-  for (int i = 0; i < kSelPer; ++i) part += x[i] == -INFINITY ? 0.f : expf(x[i] - m);
-  double s = part;
+  for (int i = 0; i < kSelPer; ++i) {
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((x[i] - m) * 1.4426950408889634f));
+    part += e;
+  }
+  // -inf - -inf, or a logit of +inf: the join knows these rows by their maximum
+  unsigned long long s = part == part ? static_cast<unsigned long long>(part * 1099511627776.f) : 0;
 #pragma unroll
   for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  if (lane == 0) sm_s[warp] = s;
-  // the 2W largest, one at a time
-  unsigned long long best = 0;
+  if (lane == 0) sm_sum[warp] = s;
+  const auto id_of = [&](int i) { return first + ((i / kVec) * kSelThreads + tid) * kVec + i % kVec; };
+  if (top >= floor_v && top > -INFINITY) {
 #pragma unroll
-  for (int i = 0; i < kSelPer; ++i) {
-    const unsigned long long k = x[i] == -INFINITY ? 0 : order_key(x[i], chunk * kSelChunk + i * kSelThreads + tid);
-    best = k > best ? k : best;
+    for (int i = 0; i < kSelPer; ++i)
+      if (x[i] >= floor_v && x[i] > -INFINITY) {
+        const int at = atomicAdd(&kept, 1);
+        if (at < kSelKeep) keep[at] = order_key(x[i], id_of(i));
+      }
   }
-  unsigned long long *out = p.keys + (row * p.chunks + chunk) * (2 * p.W);
-  for (int k = 0; k < 2 * p.W; ++k) {
-    const unsigned long long mine = warp_max(best);
-    if (lane == 0) sm_k[k & 1][warp] = mine;
-    __syncthreads();
-    unsigned long long top = 0;
-    for (int w = 0; w < kSelThreads / 32; ++w) top = sm_k[k & 1][w] > top ? sm_k[k & 1][w] : top;
-    if (tid == 0) out[k] = top;
-    if (top == best && top) {
-      best = 0;
+  __syncthreads();
+  const int n = kept;
+  unsigned long long *out = p.keys + (row * p.chunks + chunk) * K;
+  if (n <= 32) {
+    if (warp == 0) {
+      const unsigned long long k = warp_sort(lane < n ? keep[lane] : 0ull, lane);
+      if (lane < K) out[lane] = k;
+    }
+  } else if (n <= kSelKeep) {
+    if (warp == 0) {
+      for (int k = 0; k < K; ++k) {
+        unsigned long long best = 0;
+        for (int i = lane; i < n; i += 32) best = keep[i] > best ? keep[i] : best;
+        best = warp_max(best);
+        if (lane == 0) out[k] = best;
+        for (int i = lane; i < n; i += 32)
+          if (keep[i] == best) keep[i] = 0;
+      }
+    }
+  } else {
+    unsigned long long below = ~0ull;
+    for (int k = 0; k < K; ++k) {
+      unsigned long long best = 0;
 #pragma unroll
       for (int i = 0; i < kSelPer; ++i) {
-        const unsigned long long q = x[i] == -INFINITY ? 0 : order_key(x[i], chunk * kSelChunk + i * kSelThreads + tid);
-        if (q < top && q > best) best = q;
+        const unsigned long long q = x[i] > -INFINITY ? order_key(x[i], id_of(i)) : 0;
+        if (q < below && q > best) best = q;
       }
+      best = warp_max(best);
+      if (lane == 0) sm_k[k & 1][warp] = best;
+      __syncthreads();
+      below = 0;
+      for (int w = 0; w < kSelThreads / 32; ++w) below = sm_k[k & 1][w] > below ? sm_k[k & 1][w] : below;
+      if (tid == 0) out[k] = below;
     }
   }
   if (tid == 0) {
-    double total = 0;
-    for (int w = 0; w < kSelThreads / 32; ++w) total += sm_s[w];
-    p.sum[row * p.chunks + chunk] = total;
+    unsigned long long total = 0;
+    for (int w = 0; w < kSelThreads / 32; ++w) total += sm_sum[w];
+    p.sum[row * p.chunks + chunk] = static_cast<double>(total) * 0x1p-40;
     p.max[row * p.chunks + chunk] = m;
   }
 }
 
 // One CTA per request, one warp per beam.
 __global__ void __launch_bounds__(WF_MAX_BEAMS * 32) beam_join_kernel(const SelectParams p) {
+  const int W = p.W, K = 2 * W, req = blockIdx.x, lane = threadIdx.x & 31, beam = threadIdx.x >> 5;
+  __shared__ unsigned long long best_key[WF_MAX_BEAMS][2 * WF_MAX_BEAMS], cand[WF_MAX_BEAMS][2 * WF_MAX_BEAMS];
+  __shared__ float row_max[WF_MAX_BEAMS], row_log[WF_MAX_BEAMS];
+  __shared__ double row_sum[WF_MAX_BEAMS];
+  extern __shared__ unsigned char next[];  // [W][chunks] keys taken of each sorted list
   pdl_wait();
   pdl_launch_dependents();
-  const int W = p.W, K = 2 * W, req = blockIdx.x, lane = threadIdx.x & 31, beam = threadIdx.x >> 5;
-  __shared__ unsigned long long cand[WF_MAX_BEAMS][2 * WF_MAX_BEAMS];  // (score, place) by beam, best first
-  __shared__ int32_t tok[WF_MAX_BEAMS][2 * WF_MAX_BEAMS];
   const long long row = static_cast<long long>(req) * W + beam;
   const float *cm = p.max + row * p.chunks;
-  const double *cs = p.sum + row * p.chunks;
+  // the row's sum: the chunks' in order of their lanes, relative to its maximum
   float m = -INFINITY;
-  for (int c = lane; c < p.chunks; c += 32) m = fmaxf(m, cm[c]);
-#pragma unroll
-  for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  for (int c = lane; c < p.chunks; c += 32) m = fmaxf(m, cm[c]), next[beam * p.chunks + c] = 0;
+  m = warp_max(m);
   double s = 0;
   for (int c = lane; c < p.chunks; c += 32)
-    if (cm[c] != -INFINITY) s += cs[c] * exp(static_cast<double>(cm[c]) - static_cast<double>(m));
+    if (cm[c] != -INFINITY) s += p.sum[row * p.chunks + c] * exp(static_cast<double>(cm[c]) - static_cast<double>(m));
 #pragma unroll
   for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  const float log_sum = static_cast<float>(log(s));
-  const float base = p.scores[row];
-  // the row's best: each lane walks the sorted lists of its chunks
+  if (lane == 0) row_max[beam] = m, row_sum[beam] = s;
+  // the row's best: each lane offers the largest key that its lists have left
   const unsigned long long *keys = p.keys + row * p.chunks * K;
-  unsigned long long floor_key = ~0ull;
-  for (int k = 0; k < K; ++k) {
-    unsigned long long best = 0;
-    for (int c = lane; c < p.chunks; c += 32)
-      for (int i = 0; i < K; ++i) {
-        const unsigned long long v = keys[c * K + i];
-        if (v < floor_key) {
-          best = v > best ? v : best;
-          break;
-        }
-      }
-    best = warp_max(best);
-    if (lane == 0) {
-      float total = best ? base + ((key_value(best) - m) - log_sum) : -INFINITY;
-      const bool live = total > -INFINITY;  // not NaN either
-      cand[beam][k] = live ? order_key(total, beam * K + k) : 0;
-      tok[beam][k] = live ? static_cast<int32_t>(key_index(best)) : -1;
+  unsigned long long mine = 0;
+  int from = -1;
+  const auto look = [&]() {
+    mine = 0;
+    for (int c = lane; c < p.chunks; c += 32) {
+      const int at = next[beam * p.chunks + c];
+      const unsigned long long v = at < K ? keys[c * K + at] : 0;
+      if (v > mine) mine = v, from = c;
     }
-    floor_key = best;
+  };
+  look();
+  for (int k = 0; k < K; ++k) {
+    const unsigned long long best = warp_max(mine);
+    if (lane == 0) best_key[beam][k] = best;
+    if (best && best == mine) {
+      ++next[beam * p.chunks + from];
+      look();
+    }
+  }
+  __syncthreads();
+  // one warp takes all rows' logarithms
+  if (beam == 0 && lane < W) row_log[lane] = static_cast<float>(log(row_sum[lane]));
+  __syncthreads();
+  if (lane < K) {
+    const unsigned long long k = best_key[beam][lane];
+    const float total = k ? p.scores[row] + ((key_value(k) - row_max[beam]) - row_log[beam]) : -INFINITY;
+    // NaN is no candidate either
+    cand[beam][lane] = total > -INFINITY ? order_key(total, beam * K + lane) : 0;
   }
   __syncthreads();
   if (beam != 0) return;
@@ -169,12 +292,12 @@ __global__ void __launch_bounds__(WF_MAX_BEAMS * 32) beam_join_kernel(const Sele
   int at = 0, n_go = 0, n_fin = 0;
   const size_t o = static_cast<size_t>(req) * W;
   for (int k = 0; k < K; ++k) {
-    const unsigned long long mine = lane < W && at < K ? cand[lane][at] : 0;
-    const unsigned long long best = warp_max(mine);
+    const unsigned long long head = lane < W && at < K ? cand[lane][at] : 0;
+    const unsigned long long best = warp_max(head);
     if (!best) break;
-    if (mine == best) ++at;
+    if (head == best) ++at;
     const uint32_t place = key_index(best);
-    const int b = place / K, t = tok[b][place % K];
+    const int b = place / K, t = static_cast<int>(key_index(best_key[b][place % K]));
     const float v = key_value(best);
     if (t == p.eos) {
       if (k < W) {
@@ -196,12 +319,14 @@ __global__ void __launch_bounds__(WF_MAX_BEAMS * 32) beam_join_kernel(const Sele
 
 using namespace wf;
 
-static int select_chunks(int V) { return (V + kSelChunk - 1) / kSelChunk; }
+// 15 bytes of skew may push a row's end into another chunk.
+static int select_chunks(int V) { return (V + 7 + kSelChunk - 1) / kSelChunk; }
+constexpr int kSelMaxVocab = 1 << 22;  // the join keeps a byte for each of a request's chunks in shared memory
 
 extern "C" {
 
 size_t wf_beam_select_scratch_bytes(int32_t n_req, int32_t beams, int32_t vocab) {
-  if (n_req <= 0 || beams <= 0 || beams > WF_MAX_BEAMS || vocab < 2 * beams) return 0;
+  if (n_req <= 0 || beams <= 0 || beams > WF_MAX_BEAMS || vocab < 2 * beams || vocab > kSelMaxVocab) return 0;
   return static_cast<size_t>(n_req) * beams * select_chunks(vocab) * (2 * beams * 8 + 16);
 }
 
@@ -210,9 +335,11 @@ wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const 
                          float *d_score, int32_t *d_fin_parent, float *d_fin_score, void *d_scratch, size_t scratch_bytes,
                          void *stream) {
   if (!d_logits || !d_scores || !d_token || !d_parent || !d_score || !d_fin_parent || !d_fin_score || !d_scratch || n_req <= 0 ||
-      beams <= 0 || vocab <= 0 || ld < vocab || (reinterpret_cast<uintptr_t>(d_scratch) & 7))
+      beams <= 0 || vocab <= 0 || ld < vocab || (reinterpret_cast<uintptr_t>(d_scratch) & 7) ||
+      (reinterpret_cast<uintptr_t>(d_logits) & (dtype == WF_F32 ? 3 : 1)))
     return WF_ERR_INVALID;
-  if (dtype < WF_BF16 || dtype > WF_F32 || beams > WF_MAX_BEAMS || vocab < 2 * beams) return WF_ERR_UNSUPPORTED;
+  if (dtype < WF_BF16 || dtype > WF_F32 || beams > WF_MAX_BEAMS || vocab < 2 * beams || vocab > kSelMaxVocab)
+    return WF_ERR_UNSUPPORTED;
   const long long rows = static_cast<long long>(n_req) * beams;
   if (rows > INT32_MAX) return WF_ERR_INVALID;
   if (scratch_bytes < wf_beam_select_scratch_bytes(n_req, beams, vocab)) return WF_ERR_CAPACITY;
@@ -230,7 +357,7 @@ wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const 
   void *args[] = {&p};
   const dim3 grid(p.chunks, static_cast<unsigned>(std::min<long long>(rows, 65535)), static_cast<unsigned>((rows + 65534) / 65535));
   if (launch_pdl(fn, grid, kSelThreads, 0, args, s) != cudaSuccess ||
-      launch_pdl(reinterpret_cast<const void *>(beam_join_kernel), n_req, beams * 32, 0, args, s) != cudaSuccess)
+      launch_pdl(reinterpret_cast<const void *>(beam_join_kernel), n_req, beams * 32, beams * p.chunks, args, s) != cudaSuccess)
     return WF_ERR_CUDA;
   return WF_OK;
 }
