@@ -25,7 +25,7 @@ struct SelectParams {
   float *fin_score;
   // scratch: per (row, chunk) the maximum and the sum, and 2W keys
   unsigned long long *keys;  // [rows][chunks][2W]
-  double *sum;               // [rows][chunks]
+  unsigned long long *sum;   // [rows][chunks] in units of 2^-40
   float *max;                // [rows][chunks]
 };
 constexpr int kSelThreads = 256;
@@ -35,10 +35,12 @@ constexpr int kSelKeep = 512;                     // candidates of a chunk that 
 
 // (value descending, index ascending) as one descending unsigned key; 0 is
 // below every key of a value above -inf.
-__device__ __forceinline__ unsigned long long order_key(float v, uint32_t idx) {
+__device__ __forceinline__ uint32_t order_bits(float v) {
   const uint32_t b = __float_as_uint(v + 0.f);  // -0 as 0
-  const uint32_t o = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-  return static_cast<unsigned long long>(o) << 32 | (0xffffffffu - idx);
+  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ unsigned long long order_key(float v, uint32_t idx) {
+  return static_cast<unsigned long long>(order_bits(v)) << 32 | (0xffffffffu - idx);
 }
 __device__ __forceinline__ float key_value(unsigned long long k) {
   const uint32_t o = static_cast<uint32_t>(k >> 32);
@@ -51,10 +53,10 @@ __device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
   const uint32_t lo = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(k >> 32) == hi ? static_cast<uint32_t>(k) : 0u);
   return static_cast<unsigned long long>(hi) << 32 | lo;
 }
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int off = 16; off; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
-  return v;
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 // Sorts a warp's values (keys), largest in lane 0: a bitonic network.
 template <typename K>
@@ -104,14 +106,16 @@ struct Logits<__half> : Logits16<__half> {
 //
 // The k = 2 beams largest: of the 32 maxima over 128 logits each, the k-th is
 // a value that at least k logits reach and few more do; those are collected
-// and sorted by one warp.  Where many reach it (equal logits), k rounds over
+// and ranked by one warp.  Where many reach it (equal logits), k rounds over
 // the CTA pick them one by one.  The sum of exponentials adds 16 terms a
 // thread in fp32, the threads' in fixed point (2^-40), so it has no order.
+// A NaN is never the larger of a comparison, which keeps it out of the maxima
+// and the candidates; only the sum has to look for it.
 template <typename T>
 __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectParams p) {
   using L = Logits<T>;
   constexpr int kVec = L::kVec, kVecs = kSelPer / kVec;
-  __shared__ float sm_g[32];
+  __shared__ float sm_g[32], sm_floor;
   __shared__ unsigned long long sm_sum[kSelThreads / 32], sm_k[2][kSelThreads / 32], keep[kSelKeep];
   __shared__ int kept;
   __shared__ __align__(16) unsigned char mask[kSelChunk + 32];
@@ -151,6 +155,7 @@ __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectPar
       const int at = lead + ((v * 4 / kVec) * kSelThreads + tid) * kVec + v * 4 % kVec;
       const uint32_t *word = reinterpret_cast<const uint32_t *>(mask) + (at >> 2);
       const uint32_t w = __funnelshift_r(word[0], word[1], (at & 3) * 8);
+      if (!w) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (w & (0xffu << (8 * e))) x[v * 4 + e] = -INFINITY;
@@ -158,30 +163,37 @@ __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectPar
   }
   float top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kSelPer; ++i) {
-    if (x[i] != x[i]) x[i] = -INFINITY;
-    top = fmaxf(top, x[i]);
-  }
+  for (int i = 0; i < kSelPer; ++i) top = fmaxf(top, x[i]);
   float g = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
   g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
   g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
   if ((lane & 7) == 0) sm_g[warp * 4 + (lane >> 3)] = g;
   __syncthreads();
-  const float sorted = warp_sort(sm_g[lane], lane);
-  const float m = __shfl_sync(0xffffffffu, sorted, 0), floor_v = __shfl_sync(0xffffffffu, sorted, K - 1);
+  g = sm_g[lane];
+  const float m = key_value(static_cast<unsigned long long>(__reduce_max_sync(0xffffffffu, order_bits(g))) << 32);
+  if (warp == 0) {
+    const float kth = __shfl_sync(0xffffffffu, warp_sort(g, lane), K - 1);
+    if (lane == 0) sm_floor = kth;
+  }
   float part = 0.f;
 #pragma unroll
-  for (int i = 0; i < kSelPer; ++i) {
-    float e;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((x[i] - m) * 1.4426950408889634f));
-    part += e;
+  for (int i = 0; i < kSelPer; ++i) part += ex2((x[i] - m) * 1.4426950408889634f);
+  if (part != part) {  // a NaN; or all -inf, or a +inf: the join knows those rows by their maximum
+    part = 0.f;
+    for (int i = 0; i < kSelPer; ++i) {
+      const float e = ex2((x[i] - m) * 1.4426950408889634f);
+      part += e == e ? e : 0.f;
+    }
   }
-  // -inf - -inf, or a logit of +inf: the join knows these rows by their maximum
-  unsigned long long s = part == part ? static_cast<unsigned long long>(part * 1099511627776.f) : 0;
-#pragma unroll
-  for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  if (lane == 0) sm_sum[warp] = s;
+  {
+    const unsigned long long fixed = static_cast<unsigned long long>(part * 1099511627776.f);  // at most 2^44
+    const unsigned lo = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(fixed & 0x3fffff));
+    const unsigned hi = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(fixed >> 22));
+    if (lane == 0) sm_sum[warp] = (static_cast<unsigned long long>(hi) << 22) + lo;
+  }
   const auto id_of = [&](int i) { return first + ((i / kVec) * kSelThreads + tid) * kVec + i % kVec; };
+  __syncthreads();
+  const float floor_v = sm_floor;
   if (top >= floor_v && top > -INFINITY) {
 #pragma unroll
     for (int i = 0; i < kSelPer; ++i)
@@ -193,21 +205,15 @@ __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectPar
   __syncthreads();
   const int n = kept;
   unsigned long long *out = p.keys + (row * p.chunks + chunk) * K;
-  if (n <= 32) {
-    if (warp == 0) {
-      const unsigned long long k = warp_sort(lane < n ? keep[lane] : 0ull, lane);
-      if (lane < K) out[lane] = k;
-    }
-  } else if (n <= kSelKeep) {
-    if (warp == 0) {
-      for (int k = 0; k < K; ++k) {
-        unsigned long long best = 0;
-        for (int i = lane; i < n; i += 32) best = keep[i] > best ? keep[i] : best;
-        best = warp_max(best);
-        if (lane == 0) out[k] = best;
-        for (int i = lane; i < n; i += 32)
-          if (keep[i] == best) keep[i] = 0;
+  if (n <= kSelKeep) {
+    if (warp == 0) {  // each key's rank is the number of larger ones
+      for (int i = lane; i < n; i += 32) {
+        const unsigned long long k = keep[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += keep[j] > k;
+        if (rank < K) out[rank] = k;
       }
+      if (lane >= n && lane < K) out[lane] = 0;
     }
   } else {
     unsigned long long below = ~0ull;
@@ -229,89 +235,100 @@ __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectPar
   if (tid == 0) {
     unsigned long long total = 0;
     for (int w = 0; w < kSelThreads / 32; ++w) total += sm_sum[w];
-    p.sum[row * p.chunks + chunk] = static_cast<double>(total) * 0x1p-40;
+    p.sum[row * p.chunks + chunk] = total;
     p.max[row * p.chunks + chunk] = m;
   }
 }
 
-// One CTA per request, one warp per beam.
-__global__ void __launch_bounds__(WF_MAX_BEAMS * 32) beam_join_kernel(const SelectParams p) {
-  const int W = p.W, K = 2 * W, req = blockIdx.x, lane = threadIdx.x & 31, beam = threadIdx.x >> 5;
-  __shared__ unsigned long long best_key[WF_MAX_BEAMS][2 * WF_MAX_BEAMS], cand[WF_MAX_BEAMS][2 * WF_MAX_BEAMS];
+// One CTA per request, one warp per beam and one more, which takes the rows'
+// logarithms in 64 bits while the others pick their rows' best keys.
+constexpr int kJoinStage = 40 << 10;  // shared memory for the rows' keys; past it they are read where they lie
+__global__ void __launch_bounds__((WF_MAX_BEAMS + 1) * 32) beam_join_kernel(const SelectParams p, int staged) {
+  const int W = p.W, K = 2 * W, req = blockIdx.x, lane = threadIdx.x & 31, beam = threadIdx.x >> 5, C = p.chunks;
+  __shared__ unsigned long long best_key[WF_MAX_BEAMS * 2 * WF_MAX_BEAMS], cand[WF_MAX_BEAMS * 2 * WF_MAX_BEAMS];
+  __shared__ unsigned long long ranked[2 * WF_MAX_BEAMS], row_sum[WF_MAX_BEAMS];
   __shared__ float row_max[WF_MAX_BEAMS], row_log[WF_MAX_BEAMS];
-  __shared__ double row_sum[WF_MAX_BEAMS];
-  extern __shared__ unsigned char next[];  // [W][chunks] keys taken of each sorted list
+  extern __shared__ unsigned long long dyn[];
+  unsigned char *next = reinterpret_cast<unsigned char *>(dyn + (staged ? W * C * K : 0));  // [W][C] keys taken of each list
   pdl_wait();
   pdl_launch_dependents();
-  const long long row = static_cast<long long>(req) * W + beam;
-  const float *cm = p.max + row * p.chunks;
-  // the row's sum: the chunks' in order of their lanes, relative to its maximum
-  float m = -INFINITY;
-  for (int c = lane; c < p.chunks; c += 32) m = fmaxf(m, cm[c]), next[beam * p.chunks + c] = 0;
-  m = warp_max(m);
-  double s = 0;
-  for (int c = lane; c < p.chunks; c += 32)
-    if (cm[c] != -INFINITY) s += p.sum[row * p.chunks + c] * exp(static_cast<double>(cm[c]) - static_cast<double>(m));
-#pragma unroll
-  for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  if (lane == 0) row_max[beam] = m, row_sum[beam] = s;
-  // the row's best: each lane offers the largest key that its lists have left
-  const unsigned long long *keys = p.keys + row * p.chunks * K;
-  unsigned long long mine = 0;
-  int from = -1;
-  const auto look = [&]() {
-    mine = 0;
-    for (int c = lane; c < p.chunks; c += 32) {
-      const int at = next[beam * p.chunks + c];
-      const unsigned long long v = at < K ? keys[c * K + at] : 0;
-      if (v > mine) mine = v, from = c;
+  const long long row0 = static_cast<long long>(req) * W;
+  const unsigned long long *keys = p.keys + row0 * C * K;
+  if (staged)
+    for (int i = threadIdx.x; i < W * C * K; i += blockDim.x) dyn[i] = keys[i];
+  for (int i = threadIdx.x; i < W * C; i += blockDim.x) next[i] = 0;
+  if (threadIdx.x < K) ranked[threadIdx.x] = 0;
+  if (beam < W) {  // the row's maximum and sum
+    const float *cm = p.max + (row0 + beam) * C;
+    const unsigned long long *cs = p.sum + (row0 + beam) * C;
+    float m = -INFINITY;
+    for (int c = lane; c < C; c += 32) m = fmaxf(m, cm[c]);
+    m = key_value(static_cast<unsigned long long>(__reduce_max_sync(0xffffffffu, order_bits(m))) << 32);
+    unsigned long long s = 0;
+    for (int c = lane; c < C; c += 32) {
+      const float f = expf(cm[c] - m);
+      if (f == f) s += static_cast<unsigned long long>(static_cast<double>(cs[c]) * static_cast<double>(f));
     }
-  };
-  look();
-  for (int k = 0; k < K; ++k) {
-    const unsigned long long best = warp_max(mine);
-    if (lane == 0) best_key[beam][k] = best;
-    if (best && best == mine) {
-      ++next[beam * p.chunks + from];
-      look();
+#pragma unroll
+    for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    if (lane == 0) row_max[beam] = m, row_sum[beam] = s;
+  }
+  __syncthreads();
+  if (beam == W) {
+    if (lane < W) row_log[lane] = static_cast<float>(log(static_cast<double>(row_sum[lane]) * 0x1p-40));
+  } else {
+    // each lane offers the largest key that its sorted lists have left
+    const unsigned long long *mine = (staged ? dyn : keys) + static_cast<size_t>(beam) * C * K;
+    unsigned long long head = 0;
+    int from = -1;
+    const auto look = [&]() {
+      head = 0;
+      for (int c = lane; c < C; c += 32) {
+        const int at = next[beam * C + c];
+        const unsigned long long v = at < K ? mine[c * K + at] : 0;
+        if (v > head) head = v, from = c;
+      }
+    };
+    look();
+    for (int k = 0; k < K; ++k) {
+      const unsigned long long best = warp_max(head);
+      if (lane == 0) best_key[beam * K + k] = best;
+      if (best && best == head) {
+        ++next[beam * C + from];
+        look();
+      }
     }
   }
   __syncthreads();
-  // one warp takes all rows' logarithms
-  if (beam == 0 && lane < W) row_log[lane] = static_cast<float>(log(row_sum[lane]));
+  for (int i = threadIdx.x; i < W * K; i += blockDim.x) {
+    const int w = i / K;
+    const unsigned long long k = best_key[i];
+    // a row whose maximum is infinite has no scores but NaN, which is no candidate
+    const float m = row_max[w], total = k && m < INFINITY ? p.scores[row0 + w] + ((key_value(k) - m) - row_log[w]) : -INFINITY;
+    cand[i] = total > -INFINITY ? order_key(total, i) : 0;
+  }
   __syncthreads();
-  if (lane < K) {
-    const unsigned long long k = best_key[beam][lane];
-    const float total = k ? p.scores[row] + ((key_value(k) - row_max[beam]) - row_log[beam]) : -INFINITY;
-    // NaN is no candidate either
-    cand[beam][lane] = total > -INFINITY ? order_key(total, beam * K + lane) : 0;
+  for (int i = threadIdx.x; i < W * K; i += blockDim.x) {
+    const unsigned long long k = cand[i];
+    int rank = 0;
+    for (int j = 0; j < W * K; ++j) rank += cand[j] > k;
+    if (k && rank < K) ranked[rank] = k;
   }
   __syncthreads();
   if (beam != 0) return;
-  // the request's best: lane w walks beam w's list
-  int at = 0, n_go = 0, n_fin = 0;
+  // lane r has rank r
+  const unsigned long long k = lane < K ? ranked[lane] : 0;
+  const int place = k ? static_cast<int>(key_index(k)) : 0, b = place / K, t = k ? static_cast<int>(key_index(best_key[place])) : -1;
+  const bool ends = k && t == p.eos;
+  const unsigned going = __ballot_sync(0xffffffffu, k && !ends), ending = __ballot_sync(0xffffffffu, ends && lane < W);
+  const unsigned below = (1u << lane) - 1;
   const size_t o = static_cast<size_t>(req) * W;
-  for (int k = 0; k < K; ++k) {
-    const unsigned long long head = lane < W && at < K ? cand[lane][at] : 0;
-    const unsigned long long best = warp_max(head);
-    if (!best) break;
-    if (head == best) ++at;
-    const uint32_t place = key_index(best);
-    const int b = place / K, t = static_cast<int>(key_index(best_key[b][place % K]));
-    const float v = key_value(best);
-    if (t == p.eos) {
-      if (k < W) {
-        if (lane == 0) p.fin_parent[o + n_fin] = b, p.fin_score[o + n_fin] = v;
-        ++n_fin;
-      }
-    } else if (n_go < W) {
-      if (lane == 0) p.token[o + n_go] = t, p.parent[o + n_go] = b, p.score[o + n_go] = v;
-      ++n_go;
-    }
-  }
+  const int at = __popc(going & below), fin = __popc(ending & below);
+  if (k && !ends && at < W) p.token[o + at] = t, p.parent[o + at] = b, p.score[o + at] = key_value(k);
+  if (ends && lane < W) p.fin_parent[o + fin] = b, p.fin_score[o + fin] = key_value(k);
   if (lane < W) {
-    if (lane >= n_go) p.token[o + lane] = -1, p.parent[o + lane] = lane, p.score[o + lane] = -INFINITY;
-    if (lane >= n_fin) p.fin_parent[o + lane] = -1, p.fin_score[o + lane] = -INFINITY;
+    if (lane >= __popc(going)) p.token[o + lane] = -1, p.parent[o + lane] = lane, p.score[o + lane] = -INFINITY;
+    if (lane >= __popc(ending)) p.fin_parent[o + lane] = -1, p.fin_score[o + lane] = -INFINITY;
   }
 }
 
@@ -348,16 +365,19 @@ wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const 
   p.n_req = n_req, p.W = beams, p.V = vocab, p.eos = eos < 0 ? -2 : eos, p.chunks = select_chunks(vocab);
   p.token = d_token, p.parent = d_parent, p.score = d_score, p.fin_parent = d_fin_parent, p.fin_score = d_fin_score;
   p.keys = static_cast<unsigned long long *>(d_scratch);
-  p.sum = reinterpret_cast<double *>(p.keys + rows * p.chunks * 2 * beams);
+  p.sum = reinterpret_cast<unsigned long long *>(p.keys + rows * p.chunks * 2 * beams);
   p.max = reinterpret_cast<float *>(p.sum + rows * p.chunks);
   const void *fn = dtype == WF_F32 ? reinterpret_cast<const void *>(beam_chunk_kernel<float>)
                    : dtype == WF_F16 ? reinterpret_cast<const void *>(beam_chunk_kernel<__half>)
                                      : reinterpret_cast<const void *>(beam_chunk_kernel<__nv_bfloat16>);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  void *args[] = {&p};
+  const size_t lists = static_cast<size_t>(beams) * p.chunks;
+  int staged = lists * 2 * beams * 8 <= kJoinStage;
+  void *args[] = {&p}, *join_args[] = {&p, &staged};
   const dim3 grid(p.chunks, static_cast<unsigned>(std::min<long long>(rows, 65535)), static_cast<unsigned>((rows + 65534) / 65535));
   if (launch_pdl(fn, grid, kSelThreads, 0, args, s) != cudaSuccess ||
-      launch_pdl(reinterpret_cast<const void *>(beam_join_kernel), n_req, beams * 32, beams * p.chunks, args, s) != cudaSuccess)
+      launch_pdl(reinterpret_cast<const void *>(beam_join_kernel), n_req, (beams + 1) * 32, lists + (staged ? lists * 2 * beams * 8 : 0),
+                 join_args, s) != cudaSuccess)
     return WF_ERR_CUDA;
   return WF_OK;
 }
