@@ -29,7 +29,7 @@ struct SelectParams {
   float *max;                // [rows][chunks]
 };
 constexpr int kSelThreads = 256;
-constexpr int kSelPer = 16;                       // logits of a thread
+constexpr int kSelPer = 32;                       // logits of a thread
 constexpr int kSelChunk = kSelThreads * kSelPer;  // of a CTA
 constexpr int kSelKeep = 512;                     // candidates of a chunk that are held
 
@@ -47,16 +47,13 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
   return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
 }
 __device__ __forceinline__ uint32_t key_index(unsigned long long k) { return 0xffffffffu - static_cast<uint32_t>(k); }
-// The largest key of a warp: its upper word, then the largest lower word under it.
+// The largest key of a warp: its upper word, then the largest lower word under it (if there are several).
 __device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
   const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(k >> 32));
-  const uint32_t lo = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(k >> 32) == hi ? static_cast<uint32_t>(k) : 0u);
+  const unsigned have = __ballot_sync(0xffffffffu, static_cast<uint32_t>(k >> 32) == hi);
+  const uint32_t lo = (have & (have - 1)) ? __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(k >> 32) == hi ? static_cast<uint32_t>(k) : 0u)
+                                          : __shfl_sync(0xffffffffu, static_cast<uint32_t>(k), __ffs(have) - 1);
   return static_cast<unsigned long long>(hi) << 32 | lo;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 // Sorts a warp's values (keys), largest in lane 0: a bitonic network.
 template <typename K>
@@ -100,19 +97,19 @@ struct Logits<__half> : Logits16<__half> {
   static __device__ __forceinline__ float one(__half v) { return __half2float(v); }
 };
 
-// One CTA: 4096 logits of a row, 16 a thread in registers, by 16-byte loads
+// One CTA: 8192 logits of a row, 32 a thread in registers, by 16-byte loads
 // whatever the row's alignment (a chunk starts up to 15 bytes before a
-// multiple of 4096 logits; what lies outside the row is -inf).
+// multiple of 8192 logits; what lies outside the row is -inf).
 //
-// The k = 2 beams largest: of the 32 maxima over 128 logits each, the k-th is
+// The k = 2 beams largest: of the 32 maxima over 256 logits each, the k-th is
 // a value that at least k logits reach and few more do; those are collected
 // and ranked by one warp.  Where many reach it (equal logits), k rounds over
-// the CTA pick them one by one.  The sum of exponentials adds 16 terms a
+// the CTA pick them one by one.  The sum of exponentials adds 32 terms a
 // thread in fp32, the threads' in fixed point (2^-40), so it has no order.
 // A NaN is never the larger of a comparison, which keeps it out of the maxima
 // and the candidates; only the sum has to look for it.
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectParams p) {
+__global__ void __launch_bounds__(kSelThreads, 4) beam_chunk_kernel(const SelectParams p) {
   using L = Logits<T>;
   constexpr int kVec = L::kVec, kVecs = kSelPer / kVec;
   __shared__ float sm_g[32], sm_floor;
@@ -128,17 +125,30 @@ __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectPar
   const T *src = static_cast<const T *>(p.logits) + row * p.ld;
   const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
   const int first = chunk * kSelChunk - skew;  // a multiple of 16 bytes from address 0
+  const auto id_of = [&](int i) { return first + ((i / kVec) * kSelThreads + tid) * kVec + i % kVec; };
   float x[kSelPer];
+  const bool inside = first >= 0 && first + kSelChunk <= p.V;
+  if (inside) {
+    const uint4 *at = reinterpret_cast<const uint4 *>(src + first) + tid;
+    uint4 raw[kVecs];
 #pragma unroll
-  for (int v = 0; v < kVecs; ++v) {
-    const int id = first + (v * kSelThreads + tid) * kVec;
-    if (id >= 0 && id + kVec <= p.V) {
-      L::unpack(*reinterpret_cast<const uint4 *>(src + id), x + v * kVec);
-    } else {
+    for (int v = 0; v < kVecs; ++v) raw[v] = at[v * kSelThreads];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) x[v * kVec + e] = id + e >= 0 && id + e < p.V ? L::one(src[id + e]) : -INFINITY;
+    for (int v = 0; v < kVecs; ++v) L::unpack(raw[v], x + v * kVec);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kSelPer; ++i) {
+      const int id = id_of(i);
+      const float v = L::one(src[min(max(id, 0), p.V - 1)]);
+      x[i] = id >= 0 && id < p.V ? v : -INFINITY;
     }
   }
+  // a logit again, from memory, for the rare paths that would keep registers from the others
+  const auto again = [&](int i) {
+    const int id = id_of(i);
+    if (id < 0 || id >= p.V || (p.suppress && p.suppress[id])) return -INFINITY;
+    return L::one(src[id]);
+  };
   if (p.suppress) {  // its bytes by 16, from the multiple of 16 before the chunk; read back at the skew between the two
     const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(p.suppress) + first) & 15);
     for (int i = tid; i < kSelChunk / 16 + 1; i += kSelThreads) {
@@ -175,32 +185,40 @@ __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectPar
     const float kth = __shfl_sync(0xffffffffu, warp_sort(g, lane), K - 1);
     if (lane == 0) sm_floor = kth;
   }
-  float part = 0.f;
+  float2 part2 = {0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < kSelPer; ++i) part += ex2((x[i] - m) * 1.4426950408889634f);
+  for (int i = 0; i < kSelPer; i += 2) {  // the difference first: its rounding does not grow with the logits
+    const float2 y = mul2(add2(make_float2(x[i], x[i + 1]), make_float2(-m, -m)), make_float2(1.4426950408889634f, 1.4426950408889634f));
+    part2 = add2(part2, make_float2(ex2(y.x), ex2(y.y)));
+  }
+  float part = part2.x + part2.y;
   if (part != part) {  // a NaN; or all -inf, or a +inf: the join knows those rows by their maximum
     part = 0.f;
+#pragma unroll 1
     for (int i = 0; i < kSelPer; ++i) {
-      const float e = ex2((x[i] - m) * 1.4426950408889634f);
+      const float e = ex2((again(i) - m) * 1.4426950408889634f);
       part += e == e ? e : 0.f;
     }
   }
   {
-    const unsigned long long fixed = static_cast<unsigned long long>(part * 1099511627776.f);  // at most 2^44
+    const unsigned long long fixed = static_cast<unsigned long long>(part * 1099511627776.f);  // at most 2^45
     const unsigned lo = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(fixed & 0x3fffff));
     const unsigned hi = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(fixed >> 22));
     if (lane == 0) sm_sum[warp] = (static_cast<unsigned long long>(hi) << 22) + lo;
   }
-  const auto id_of = [&](int i) { return first + ((i / kVec) * kSelThreads + tid) * kVec + i % kVec; };
   __syncthreads();
   const float floor_v = sm_floor;
   if (top >= floor_v && top > -INFINITY) {
+    uint32_t hits = 0;
 #pragma unroll
-    for (int i = 0; i < kSelPer; ++i)
-      if (x[i] >= floor_v && x[i] > -INFINITY) {
-        const int at = atomicAdd(&kept, 1);
-        if (at < kSelKeep) keep[at] = order_key(x[i], id_of(i));
-      }
+    for (int i = 0; i < kSelPer; ++i) hits |= x[i] >= floor_v ? 1u << i : 0u;
+    for (; hits; hits &= hits - 1) {
+      const int i = __ffs(hits) - 1;
+      const float v = again(i);
+      if (!(v > -INFINITY)) continue;
+      const int at = atomicAdd(&kept, 1);
+      if (at < kSelKeep) keep[at] = order_key(v, id_of(i));
+    }
   }
   __syncthreads();
   const int n = kept;
@@ -210,6 +228,7 @@ __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectPar
       for (int i = lane; i < n; i += 32) {
         const unsigned long long k = keep[i];
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) rank += keep[j] > k;
         if (rank < K) out[rank] = k;
       }
@@ -219,9 +238,10 @@ __global__ void __launch_bounds__(kSelThreads) beam_chunk_kernel(const SelectPar
     unsigned long long below = ~0ull;
     for (int k = 0; k < K; ++k) {
       unsigned long long best = 0;
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < kSelPer; ++i) {
-        const unsigned long long q = x[i] > -INFINITY ? order_key(x[i], id_of(i)) : 0;
+        const float v = again(i);
+        const unsigned long long q = v > -INFINITY ? order_key(v, id_of(i)) : 0;
         if (q < below && q > best) best = q;
       }
       best = warp_max(best);
@@ -256,19 +276,23 @@ __global__ void __launch_bounds__((WF_MAX_BEAMS + 1) * 32) beam_join_kernel(cons
   const unsigned long long *keys = p.keys + row0 * C * K;
   if (staged)
     for (int i = threadIdx.x; i < W * C * K; i += blockDim.x) dyn[i] = keys[i];
-  for (int i = threadIdx.x; i < W * C; i += blockDim.x) next[i] = 0;
+  if (C > 32)
+    for (int i = threadIdx.x; i < W * C; i += blockDim.x) next[i] = 0;
   if (threadIdx.x < K) ranked[threadIdx.x] = 0;
   if (beam < W) {  // the row's maximum and sum
     const float *cm = p.max + (row0 + beam) * C;
     const unsigned long long *cs = p.sum + (row0 + beam) * C;
-    float m = -INFINITY;
-    for (int c = lane; c < C; c += 32) m = fmaxf(m, cm[c]);
+    const float m0 = lane < C ? cm[lane] : -INFINITY;
+    const unsigned long long s0 = lane < C ? cs[lane] : 0;
+    float m = m0;
+    for (int c = lane + 32; c < C; c += 32) m = fmaxf(m, cm[c]);
     m = key_value(static_cast<unsigned long long>(__reduce_max_sync(0xffffffffu, order_bits(m))) << 32);
-    unsigned long long s = 0;
-    for (int c = lane; c < C; c += 32) {
-      const float f = expf(cm[c] - m);
-      if (f == f) s += static_cast<unsigned long long>(static_cast<double>(cs[c]) * static_cast<double>(f));
-    }
+    const auto scaled = [&](unsigned long long v, float at) -> unsigned long long {
+      const float f = expf(at - m);
+      return f == f ? static_cast<unsigned long long>(static_cast<double>(v) * static_cast<double>(f)) : 0;
+    };
+    unsigned long long s = scaled(s0, m0);
+    for (int c = lane + 32; c < C; c += 32) s += scaled(cs[c], cm[c]);
 #pragma unroll
     for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
     if (lane == 0) row_max[beam] = m, row_sum[beam] = s;
@@ -279,23 +303,37 @@ __global__ void __launch_bounds__((WF_MAX_BEAMS + 1) * 32) beam_join_kernel(cons
   } else {
     // each lane offers the largest key that its sorted lists have left
     const unsigned long long *mine = (staged ? dyn : keys) + static_cast<size_t>(beam) * C * K;
-    unsigned long long head = 0;
-    int from = -1;
-    const auto look = [&]() {
-      head = 0;
-      for (int c = lane; c < C; c += 32) {
-        const int at = next[beam * C + c];
-        const unsigned long long v = at < K ? mine[c * K + at] : 0;
-        if (v > head) head = v, from = c;
+    if (C <= 32) {  // one list a lane, whose next key is at hand
+      const unsigned long long *list = mine + lane * K;
+      unsigned long long head = lane < C ? list[0] : 0, after = lane < C ? list[1] : 0;
+      int at = 1;
+      for (int k = 0; k < K; ++k) {
+        const unsigned long long best = warp_max(head);
+        if (lane == 0) best_key[beam * K + k] = best;
+        if (best && best == head) {
+          head = after;
+          after = ++at < K ? list[at] : 0;
+        }
       }
-    };
-    look();
-    for (int k = 0; k < K; ++k) {
-      const unsigned long long best = warp_max(head);
-      if (lane == 0) best_key[beam * K + k] = best;
-      if (best && best == head) {
-        ++next[beam * C + from];
-        look();
+    } else {
+      unsigned long long head = 0;
+      int from = -1;
+      const auto look = [&]() {
+        head = 0;
+        for (int c = lane; c < C; c += 32) {
+          const int at = next[beam * C + c];
+          const unsigned long long v = at < K ? mine[c * K + at] : 0;
+          if (v > head) head = v, from = c;
+        }
+      };
+      look();
+      for (int k = 0; k < K; ++k) {
+        const unsigned long long best = warp_max(head);
+        if (lane == 0) best_key[beam * K + k] = best;
+        if (best && best == head) {
+          ++next[beam * C + from];
+          look();
+        }
       }
     }
   }
@@ -311,6 +349,7 @@ __global__ void __launch_bounds__((WF_MAX_BEAMS + 1) * 32) beam_join_kernel(cons
   for (int i = threadIdx.x; i < W * K; i += blockDim.x) {
     const unsigned long long k = cand[i];
     int rank = 0;
+#pragma unroll 10
     for (int j = 0; j < W * K; ++j) rank += cand[j] > k;
     if (k && rank < K) ranked[rank] = k;
   }

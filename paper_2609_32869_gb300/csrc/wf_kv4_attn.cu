@@ -47,11 +47,6 @@ constexpr int kAtThreads = kAtWarps * 32;
 constexpr int kAtTile = 64;    // positions of a warp's step
 constexpr int kAtCluster = 8;  // chunks that a cluster joins
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // None of these is volatile: the compiler may interleave independent chains.
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
@@ -102,14 +97,6 @@ struct Codes<__half> {
   }
 };
 
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("add.rn.f32x2 %0, %1, %2;"
-      : "=l"(*reinterpret_cast<unsigned long long *>(&d))
-      : "l"(*reinterpret_cast<const unsigned long long *>(&a)), "l"(*reinterpret_cast<const unsigned long long *>(&b)));
-  return d;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
