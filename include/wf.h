@@ -460,7 +460,7 @@ size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_head
  *       and -inf
  *   d_fin_parent int32, d_fin_score fp32 [n_req][beams]  hypotheses that end:
  *       eos among the first `beams` ranks; past the last one -1 and -inf
- * eos < 0: none ends.  2 beams <= vocab <= 2^22.  d_score may be d_scores. */
+ * eos < 0: none ends.  2 beams <= vocab <= 2^24.  d_score may be d_scores. */
 wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const float *d_scores,
                          const uint8_t *d_suppress, int32_t n_req, int32_t beams, int32_t vocab,
                          int32_t eos, int32_t *d_token, int32_t *d_parent, float *d_score,

@@ -1,12 +1,14 @@
 // Beam search's selection over beams and vocabulary.
 //
 // Within a row the order of the scores, score + ((logit - max) - log(sum)), is
-// the order of the logits,
-// so the vocabulary is read once: each CTA takes a chunk of a row, keeps the
-// chunk's running maximum and sum of exponentials and its 2 beams largest
-// logits.  A second kernel joins the chunks of a request's rows, turns the
-// survivors into scores and ranks them.
+// the order of the logits.  The vocabulary is read once, for the row's maximum,
+// its sum of exponentials and the maxima of groups of 128 logits (256 of 16
+// bits).  A value that k = 2 beams of those maxima reach bounds the k largest
+// logits from below, so a second kernel reads only the groups that reach it
+// again, turns the k largest logits of each of a request's rows into scores
+// and ranks them.
 #include <algorithm>
+#include <cfloat>
 
 #include "wf_device.cuh"
 #include "wf_kv4.cuh"
@@ -18,20 +20,22 @@ struct SelectParams {
   long long ld;
   const float *scores;
   const uint8_t *suppress;
-  int n_req, W, V, eos, chunks;
+  int n_req, W, V, eos;
+  int tiles, segments, groups;  // tiles of a warp's segment; segments and groups of a row
   int32_t *token, *parent;
   float *score;
   int32_t *fin_parent;
   float *fin_score;
-  // scratch: per (row, chunk) the maximum and the sum, and 2W keys
-  unsigned long long *keys;  // [rows][chunks][2W]
-  unsigned long long *sum;   // [rows][chunks] in units of 2^-40
-  float *max;                // [rows][chunks]
+  // scratch
+  unsigned long long *sum;  // [rows][segments] in units of 2^-40, relative to
+  float *max;               // [rows][segments]
+  float *group_max;         // [rows][groups]
 };
 constexpr int kSelThreads = 256;
-constexpr int kSelPer = 32;                       // logits of a thread
-constexpr int kSelChunk = kSelThreads * kSelPer;  // of a CTA
-constexpr int kSelKeep = 512;                     // candidates of a chunk that are held
+constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kSelPer = 32;             // logits of a lane and tile
+constexpr int kSelTile = 32 * kSelPer;  // of a warp's step
+constexpr int kSelKeep = 128;           // candidates of a row that the join holds
 
 // (value descending, index ascending) as one descending unsigned key; 0 is
 // below every key of a value above -inf.
@@ -42,10 +46,10 @@ __device__ __forceinline__ uint32_t order_bits(float v) {
 __device__ __forceinline__ unsigned long long order_key(float v, uint32_t idx) {
   return static_cast<unsigned long long>(order_bits(v)) << 32 | (0xffffffffu - idx);
 }
-__device__ __forceinline__ float key_value(unsigned long long k) {
-  const uint32_t o = static_cast<uint32_t>(k >> 32);
+__device__ __forceinline__ float order_value(uint32_t o) {
   return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
 }
+__device__ __forceinline__ float key_value(unsigned long long k) { return order_value(static_cast<uint32_t>(k >> 32)); }
 __device__ __forceinline__ uint32_t key_index(unsigned long long k) { return 0xffffffffu - static_cast<uint32_t>(k); }
 // The largest key of a warp: its upper word, then the largest lower word under it (if there are several).
 __device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
@@ -55,16 +59,19 @@ __device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
                                           : __shfl_sync(0xffffffffu, static_cast<uint32_t>(k), __ffs(have) - 1);
   return static_cast<unsigned long long>(hi) << 32 | lo;
 }
-// Sorts a warp's values (keys), largest in lane 0: a bitonic network.
-template <typename K>
-__device__ __forceinline__ K warp_sort(K v, int lane) {
+__device__ __forceinline__ float warp_max(float v) {
+  float m;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+  return m;
+}
+// Sorts a warp's values, largest in lane 0: a bitonic network.
+__device__ __forceinline__ float warp_sort(float v, int lane) {
 #pragma unroll
   for (int size = 2; size <= 32; size <<= 1)
 #pragma unroll
     for (int off = size >> 1; off; off >>= 1) {
-      const K w = __shfl_xor_sync(0xffffffffu, v, off);
-      const bool keep_max = ((lane & off) == 0) == ((lane & size) == 0);
-      v = keep_max ? (w > v ? w : v) : (w > v ? v : w);
+      const float w = __shfl_xor_sync(0xffffffffu, v, off);
+      v = ((lane & off) == 0) == ((lane & size) == 0) ? fmaxf(v, w) : fminf(v, w);
     }
   return v;
 }
@@ -73,14 +80,15 @@ template <typename T>
 struct Logits;
 template <>
 struct Logits<float> {
+  using Half = __half;  // unused
   static constexpr int kVec = 4;
   static __device__ __forceinline__ void unpack(uint4 v, float *x) {
     x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
   }
-  static __device__ __forceinline__ float one(float v) { return v; }
 };
 template <typename T>
 struct Logits16 {
+  using Half = T;
   static constexpr int kVec = 8;
   static __device__ __forceinline__ void unpack(uint4 v, float *x) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -89,251 +97,333 @@ struct Logits16 {
   }
 };
 template <>
-struct Logits<__nv_bfloat16> : Logits16<__nv_bfloat16> {
-  static __device__ __forceinline__ float one(__nv_bfloat16 v) { return __bfloat162float(v); }
-};
+struct Logits<__nv_bfloat16> : Logits16<__nv_bfloat16> {};
 template <>
-struct Logits<__half> : Logits16<__half> {
-  static __device__ __forceinline__ float one(__half v) { return __half2float(v); }
+struct Logits<__half> : Logits16<__half> {};
+
+// kVec logits from id on, those outside [0, V) as -inf.
+template <typename T>
+__device__ __noinline__ uint4 edge_vector(const T *src, int id, int V) {
+  constexpr int kVec = Logits<T>::kVec, kBits = 128 / kVec;
+  uint32_t w[4];
+  const float low = -INFINITY;
+  const uint32_t none = kBits == 32 ? 0xff800000u : Kv4Type<typename Logits<T>::Half>::pack(low, low) & 0xffffu;
+  for (int i = 0; i < 4; ++i) {
+    w[i] = 0;
+    for (int e = 0; e < kVec / 4; ++e) {
+      const int at = id + i * (kVec / 4) + e;
+      uint32_t bits = none;
+      if (at >= 0 && at < V) bits = kBits == 32 ? reinterpret_cast<const uint32_t *>(src)[at] : reinterpret_cast<const uint16_t *>(src)[at];
+      w[i] |= bits << (kBits * e & 31);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __noinline__ uint4 edge_bytes(const uint8_t *src, int id, int V) {
+  uint32_t w[4] = {};
+  for (int i = 0; i < 16; ++i)
+    if (id + i >= 0 && id + i < V) w[i >> 2] |= static_cast<uint32_t>(src[id + i]) << (8 * (i & 3));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Logits of a row by 16-byte vectors from the multiple of 16 bytes at or before
+// its first one, whatever its alignment.
+template <typename T>
+struct RowOf {
+  const T *src;
+  int V, skew;
+  __device__ __forceinline__ RowOf(const SelectParams &p, long long row)
+      : src(static_cast<const T *>(p.logits) + row * p.ld), V(p.V), skew(static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T))) {}
+  __device__ __forceinline__ uint4 vector(int id) const {
+    return id >= 0 && id + Logits<T>::kVec <= V ? *reinterpret_cast<const uint4 *>(src + id) : edge_vector<T>(src, id, V);
+  }
 };
 
-// One CTA: 8192 logits of a row, 32 a thread in registers, by 16-byte loads
-// whatever the row's alignment (a chunk starts up to 15 bytes before a
-// multiple of 8192 logits; what lies outside the row is -inf).
-//
-// The k = 2 beams largest: of the 32 maxima over 256 logits each, the k-th is
-// a value that at least k logits reach and few more do; those are collected
-// and ranked by one warp.  Where many reach it (equal logits), k rounds over
-// the CTA pick them one by one.  The sum of exponentials adds 32 terms a
-// thread in fp32, the threads' in fixed point (2^-40), so it has no order.
-// A NaN is never the larger of a comparison, which keeps it out of the maxima
-// and the candidates; only the sum has to look for it.
+// A warp walks `tiles` tiles of 1024 logits of a row; no warp waits for
+// another.  The sum adds a tile's 32 terms a lane in fp32 and the tiles with
+// the rounding carried along; lanes and segments add in fixed point (2^-40),
+// without order.  A NaN is never the larger of a comparison, which keeps it out
+// of the maxima and the candidates; only the sum has to look for it.
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads, 4) beam_chunk_kernel(const SelectParams p) {
+__global__ void __launch_bounds__(kSelThreads, 4) beam_segment_kernel(const SelectParams p) {
   using L = Logits<T>;
   constexpr int kVec = L::kVec, kVecs = kSelPer / kVec;
-  __shared__ float sm_g[32], sm_floor;
-  __shared__ unsigned long long sm_sum[kSelThreads / 32], sm_k[2][kSelThreads / 32], keep[kSelKeep];
-  __shared__ int kept;
-  __shared__ __align__(16) unsigned char mask[kSelChunk + 32];
-  const int chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = 2 * p.W;
-  const long long row = blockIdx.y + static_cast<long long>(blockIdx.z) * 65535;
+  __shared__ __align__(16) unsigned char masks[kSelWarps][kSelTile + 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long unit = static_cast<long long>(blockIdx.x) * kSelWarps + warp, row = unit / p.segments;
+  const int segment = static_cast<int>(unit - row * p.segments);
   if (row >= static_cast<long long>(p.n_req) * p.W) return;
-  if (tid == 0) kept = 0;
+  unsigned char *mask = masks[warp];
   pdl_wait();
-  pdl_launch_dependents();
-  const T *src = static_cast<const T *>(p.logits) + row * p.ld;
-  const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
-  const int first = chunk * kSelChunk - skew;  // a multiple of 16 bytes from address 0
-  const auto id_of = [&](int i) { return first + ((i / kVec) * kSelThreads + tid) * kVec + i % kVec; };
-  float x[kSelPer];
-  const bool inside = first >= 0 && first + kSelChunk <= p.V;
-  if (inside) {
-    const uint4 *at = reinterpret_cast<const uint4 *>(src + first) + tid;
-    uint4 raw[kVecs];
+  const RowOf<T> in(p, row);
+  const int start = segment * p.tiles * kSelTile - in.skew, end = min(start + p.tiles * kSelTile, p.V);
+  float *group = p.group_max + row * p.groups + segment * p.tiles * kVecs;
+  float m = -INFINITY, sum = 0.f, carry = 0.f;
+  for (int first = start; first < end; first += kSelTile, group += kVecs) {
+    float x[kSelPer];
+    {
+      uint4 raw[kVecs];
+      if (first >= 0 && first + kSelTile <= p.V) {
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v) raw[v] = at[v * kSelThreads];
-#pragma unroll
-    for (int v = 0; v < kVecs; ++v) L::unpack(raw[v], x + v * kVec);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kSelPer; ++i) {
-      const int id = id_of(i);
-      const float v = L::one(src[min(max(id, 0), p.V - 1)]);
-      x[i] = id >= 0 && id < p.V ? v : -INFINITY;
-    }
-  }
-  // a logit again, from memory, for the rare paths that would keep registers from the others
-  const auto again = [&](int i) {
-    const int id = id_of(i);
-    if (id < 0 || id >= p.V || (p.suppress && p.suppress[id])) return -INFINITY;
-    return L::one(src[id]);
-  };
-  if (p.suppress) {  // its bytes by 16, from the multiple of 16 before the chunk; read back at the skew between the two
-    const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(p.suppress) + first) & 15);
-    for (int i = tid; i < kSelChunk / 16 + 1; i += kSelThreads) {
-      const int id = first - lead + i * 16;
-      if (id >= 0 && id + 16 <= p.V) {
-        *reinterpret_cast<uint4 *>(mask + i * 16) = *reinterpret_cast<const uint4 *>(p.suppress + id);
+        for (int v = 0; v < kVecs; ++v) raw[v] = *reinterpret_cast<const uint4 *>(in.src + first + (v * 32 + lane) * kVec);
       } else {
-        for (int e = 0; e < 16; ++e) mask[i * 16 + e] = id + e >= 0 && id + e < p.V ? p.suppress[id + e] : 0;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) raw[v] = in.vector(first + (v * 32 + lane) * kVec);
+      }
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) L::unpack(raw[v], x + v * kVec);
+    }
+    if (p.suppress) {  // the tile's bytes by 16, from the multiple of 16 before it; read back at the skew between the two
+      const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(p.suppress) + first) & 15), from = first - lead;
+      uint4 w[3] = {};
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int id = from + (i * 32 + lane) * 16;
+        if (i == 2 && lane > 0) continue;
+        if (id >= 0 && id + 16 <= p.V) {
+          w[i] = *reinterpret_cast<const uint4 *>(p.suppress + id);
+        } else if (id + 16 > 0 && id < p.V) {
+          w[i] = edge_bytes(p.suppress, id, p.V);
+        }
+      }
+      const uint32_t some = w[0].x | w[0].y | w[0].z | w[0].w | w[1].x | w[1].y | w[1].z | w[1].w | w[2].x | w[2].y | w[2].z | w[2].w;
+      if (__any_sync(0xffffffffu, some != 0)) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (i < 2 || lane == 0) *reinterpret_cast<uint4 *>(mask + (i * 32 + lane) * 16) = w[i];
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < kSelPer / 4; ++q) {
+          const int at = lead + ((q * 4 / kVec) * 32 + lane) * kVec + q * 4 % kVec;
+          const uint32_t *word = reinterpret_cast<const uint32_t *>(mask) + (at >> 2);
+          const uint32_t b = __funnelshift_r(word[0], word[1], (at & 3) * 8);
+          if (!b) continue;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (b & (0xffu << (8 * e))) x[q * 4 + e] = -INFINITY;
+        }
       }
     }
-    __syncthreads();
+    // the groups' maxima, lane v that of vector v
+    float tops = 0.f, tile_top = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < kSelPer / 4; ++v) {
-      const int at = lead + ((v * 4 / kVec) * kSelThreads + tid) * kVec + v * 4 % kVec;
-      const uint32_t *word = reinterpret_cast<const uint32_t *>(mask) + (at >> 2);
-      const uint32_t w = __funnelshift_r(word[0], word[1], (at & 3) * 8);
-      if (!w) continue;
+    for (int v = 0; v < kVecs; ++v) {
+      float t = fmaxf(x[v * kVec], x[v * kVec + 1]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (w & (0xffu << (8 * e))) x[v * 4 + e] = -INFINITY;
+      for (int e = 2; e < kVec; e += 2) t = max3(t, x[v * kVec + e], x[v * kVec + e + 1]);
+      const float g = warp_max(t);
+      tops = lane == v ? g : tops;
+      tile_top = fmaxf(tile_top, g);
     }
-  }
-  float top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kSelPer; ++i) top = fmaxf(top, x[i]);
-  float g = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
-  g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
-  if ((lane & 7) == 0) sm_g[warp * 4 + (lane >> 3)] = g;
-  __syncthreads();
-  g = sm_g[lane];
-  const float m = key_value(static_cast<unsigned long long>(__reduce_max_sync(0xffffffffu, order_bits(g))) << 32);
-  if (warp == 0) {
-    const float kth = __shfl_sync(0xffffffffu, warp_sort(g, lane), K - 1);
-    if (lane == 0) sm_floor = kth;
-  }
-  float2 part2 = {0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < kSelPer; i += 2) {  // the difference first: its rounding does not grow with the logits
-    const float2 y = mul2(add2(make_float2(x[i], x[i + 1]), make_float2(-m, -m)), make_float2(1.4426950408889634f, 1.4426950408889634f));
-    part2 = add2(part2, make_float2(ex2(y.x), ex2(y.y)));
-  }
-  float part = part2.x + part2.y;
-  if (part != part) {  // a NaN; or all -inf, or a +inf: the join knows those rows by their maximum
-    part = 0.f;
-#pragma unroll 1
-    for (int i = 0; i < kSelPer; ++i) {
-      const float e = ex2((again(i) - m) * 1.4426950408889634f);
-      part += e == e ? e : 0.f;
+    if (lane < kVecs) group[lane] = tops;
+    if (tile_top == -INFINITY) continue;
+    if (tile_top > m) {
+      const float f = expf(m - tile_top);
+      sum *= f, carry *= f;
+      m = tile_top;
     }
-  }
-  {
-    const unsigned long long fixed = static_cast<unsigned long long>(part * 1099511627776.f);  // at most 2^45
-    const unsigned lo = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(fixed & 0x3fffff));
-    const unsigned hi = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(fixed >> 22));
-    if (lane == 0) sm_sum[warp] = (static_cast<unsigned long long>(hi) << 22) + lo;
-  }
-  __syncthreads();
-  const float floor_v = sm_floor;
-  if (top >= floor_v && top > -INFINITY) {
-    uint32_t hits = 0;
+    float2 part2 = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kSelPer; ++i) hits |= x[i] >= floor_v ? 1u << i : 0u;
-    for (; hits; hits &= hits - 1) {
-      const int i = __ffs(hits) - 1;
-      const float v = again(i);
-      if (!(v > -INFINITY)) continue;
-      const int at = atomicAdd(&kept, 1);
-      if (at < kSelKeep) keep[at] = order_key(v, id_of(i));
+    for (int i = 0; i < kSelPer; i += 2) {  // the difference first: its rounding does not grow with the logits
+      const float2 y = mul2(add2(make_float2(x[i], x[i + 1]), make_float2(-m, -m)), make_float2(1.4426950408889634f, 1.4426950408889634f));
+      part2 = add2(part2, make_float2(ex2(y.x), ex2(y.y)));
     }
-  }
-  __syncthreads();
-  const int n = kept;
-  unsigned long long *out = p.keys + (row * p.chunks + chunk) * K;
-  if (n <= kSelKeep) {
-    if (warp == 0) {  // each key's rank is the number of larger ones
-      for (int i = lane; i < n; i += 32) {
-        const unsigned long long k = keep[i];
-        int rank = 0;
-#pragma unroll 8
-        for (int j = 0; j < n; ++j) rank += keep[j] > k;
-        if (rank < K) out[rank] = k;
-      }
-      if (lane >= n && lane < K) out[lane] = 0;
-    }
-  } else {
-    unsigned long long below = ~0ull;
-    for (int k = 0; k < K; ++k) {
-      unsigned long long best = 0;
-#pragma unroll 1
+    float part = part2.x + part2.y;
+    if (part != part) {  // a NaN; or a +inf, whose row the join knows by its maximum
+      part = 0.f;
+#pragma unroll
       for (int i = 0; i < kSelPer; ++i) {
-        const float v = again(i);
-        const unsigned long long q = v > -INFINITY ? order_key(v, id_of(i)) : 0;
-        if (q < below && q > best) best = q;
+        const float e = ex2((x[i] - m) * 1.4426950408889634f);
+        part += e == e ? e : 0.f;
       }
-      best = warp_max(best);
-      if (lane == 0) sm_k[k & 1][warp] = best;
-      __syncthreads();
-      below = 0;
-      for (int w = 0; w < kSelThreads / 32; ++w) below = sm_k[k & 1][w] > below ? sm_k[k & 1][w] : below;
-      if (tid == 0) out[k] = below;
     }
+    const float y = part - carry, t = sum + y;
+    carry = (t - sum) - y;
+    sum = t;
   }
-  if (tid == 0) {
-    unsigned long long total = 0;
-    for (int w = 0; w < kSelThreads / 32; ++w) total += sm_sum[w];
-    p.sum[row * p.chunks + chunk] = total;
-    p.max[row * p.chunks + chunk] = m;
+  pdl_launch_dependents();  // not before: the join's CTAs would take the room of this kernel's
+  // tiles of the last segment that lie past the row
+  for (int i = static_cast<int>(group - p.group_max - row * p.groups) + lane; i < min((segment + 1) * p.tiles * kVecs, p.groups); i += 32)
+    p.group_max[row * p.groups + i] = -INFINITY;
+  unsigned long long fixed = static_cast<unsigned long long>(static_cast<double>(sum) * 0x1p40);
+#pragma unroll
+  for (int off = 16; off; off >>= 1) fixed += __shfl_xor_sync(0xffffffffu, fixed, off);
+  if (lane == 0) p.sum[unit] = fixed, p.max[unit] = m;
+}
+
+// 512 groups' maxima, 16 a lane, all loads in flight; -inf past the last.
+__device__ __forceinline__ void load_groups(const float *tops, int base, int groups, int lane, float (&t)[16]) {
+#pragma unroll
+  for (int u = 0; u < 16; ++u) {
+    const int i = base + u * 32 + lane;
+    t[u] = i < groups ? tops[i] : -INFINITY;
   }
 }
 
-// One CTA per request, one warp per beam and one more, which takes the rows'
-// logarithms in 64 bits while the others pick their rows' best keys.
-constexpr int kJoinStage = 40 << 10;  // shared memory for the rows' keys; past it they are read where they lie
-__global__ void __launch_bounds__((WF_MAX_BEAMS + 1) * 32) beam_join_kernel(const SelectParams p, int staged) {
-  const int W = p.W, K = 2 * W, req = blockIdx.x, lane = threadIdx.x & 31, beam = threadIdx.x >> 5, C = p.chunks;
-  __shared__ unsigned long long best_key[WF_MAX_BEAMS * 2 * WF_MAX_BEAMS], cand[WF_MAX_BEAMS * 2 * WF_MAX_BEAMS];
-  __shared__ unsigned long long ranked[2 * WF_MAX_BEAMS], row_sum[WF_MAX_BEAMS];
-  __shared__ float row_max[WF_MAX_BEAMS], row_log[WF_MAX_BEAMS];
-  extern __shared__ unsigned long long dyn[];
-  unsigned char *next = reinterpret_cast<unsigned char *>(dyn + (staged ? W * C * K : 0));  // [W][C] keys taken of each list
+__device__ __forceinline__ void copy16_async(void *smem_dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem_dst)), "l"(src) : "memory");
+}
+
+// One CTA per request, two warps per beam: one picks the row's best logits,
+// one takes its maximum, sum and (in 64 bits) logarithm meanwhile.  Most of
+// its time is the latency of a few dependent reads, so each is issued at once:
+// the maxima into registers, the groups into shared memory.
+constexpr int kJoinGroups = 64;  // groups of a row that are looked through
+constexpr int kJoinAhead = 8;    // of them in shared memory at a time
+template <typename T>
+__global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32) beam_join_kernel(const SelectParams p) {
+  using L = Logits<T>;
+  constexpr int kVec = L::kVec;
+  const int W = p.W, K = 2 * W, req = blockIdx.x, lane = threadIdx.x & 31, beam = threadIdx.x >> 5;
+  __shared__ unsigned long long keeps[WF_MAX_BEAMS][kSelKeep], best_key[WF_MAX_BEAMS * 2 * WF_MAX_BEAMS], cand[WF_MAX_BEAMS * 2 * WF_MAX_BEAMS];
+  __shared__ unsigned long long ranked[2 * WF_MAX_BEAMS];
+  __shared__ float row_max[WF_MAX_BEAMS], row_log[WF_MAX_BEAMS], row_score[WF_MAX_BEAMS];
+  __shared__ int counts[WF_MAX_BEAMS], chosen[WF_MAX_BEAMS][kJoinGroups];
+  extern __shared__ uint4 vectors[];  // [W][kJoinAhead][32]
   pdl_wait();
   pdl_launch_dependents();
   const long long row0 = static_cast<long long>(req) * W;
-  const unsigned long long *keys = p.keys + row0 * C * K;
-  if (staged)
-    for (int i = threadIdx.x; i < W * C * K; i += blockDim.x) dyn[i] = keys[i];
-  if (C > 32)
-    for (int i = threadIdx.x; i < W * C; i += blockDim.x) next[i] = 0;
-  if (threadIdx.x < K) ranked[threadIdx.x] = 0;
-  if (beam < W) {  // the row's maximum and sum
-    const float *cm = p.max + (row0 + beam) * C;
-    const unsigned long long *cs = p.sum + (row0 + beam) * C;
-    const float m0 = lane < C ? cm[lane] : -INFINITY;
-    const unsigned long long s0 = lane < C ? cs[lane] : 0;
+  if (beam >= W) {
+    const int w = beam - W;
+    const float *sm = p.max + (row0 + w) * p.segments;
+    const unsigned long long *ss = p.sum + (row0 + w) * p.segments;
+    const float m0 = lane < p.segments ? sm[lane] : -INFINITY;
+    const unsigned long long s0 = lane < p.segments ? ss[lane] : 0;
+    if (lane == 0) row_score[w] = p.scores[row0 + w];
+    if (w == 0 && lane < K) ranked[lane] = 0;
     float m = m0;
-    for (int c = lane + 32; c < C; c += 32) m = fmaxf(m, cm[c]);
-    m = key_value(static_cast<unsigned long long>(__reduce_max_sync(0xffffffffu, order_bits(m))) << 32);
+    for (int c = lane + 32; c < p.segments; c += 32) m = fmaxf(m, sm[c]);
+    m = warp_max(m);
     const auto scaled = [&](unsigned long long v, float at) -> unsigned long long {
       const float f = expf(at - m);
       return f == f ? static_cast<unsigned long long>(static_cast<double>(v) * static_cast<double>(f)) : 0;
     };
     unsigned long long s = scaled(s0, m0);
-    for (int c = lane + 32; c < C; c += 32) s += scaled(cs[c], cm[c]);
+    for (int c = lane + 32; c < p.segments; c += 32) s += scaled(ss[c], sm[c]);
 #pragma unroll
     for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    if (lane == 0) row_max[beam] = m, row_sum[beam] = s;
-  }
-  __syncthreads();
-  if (beam == W) {
-    if (lane < W) row_log[lane] = static_cast<float>(log(static_cast<double>(row_sum[lane]) * 0x1p-40));
+    if (lane == 0) row_max[w] = m, row_log[w] = static_cast<float>(log(static_cast<double>(s) * 0x1p-40));
   } else {
-    // each lane offers the largest key that its sorted lists have left
-    const unsigned long long *mine = (staged ? dyn : keys) + static_cast<size_t>(beam) * C * K;
-    if (C <= 32) {  // one list a lane, whose next key is at hand
-      const unsigned long long *list = mine + lane * K;
-      unsigned long long head = lane < C ? list[0] : 0, after = lane < C ? list[1] : 0;
-      int at = 1;
-      for (int k = 0; k < K; ++k) {
-        const unsigned long long best = warp_max(head);
-        if (lane == 0) best_key[beam * K + k] = best;
-        if (best && best == head) {
-          head = after;
-          after = ++at < K ? list[at] : 0;
+    const long long row = row0 + beam;
+    float *tops = p.group_max + row * p.groups;
+    float lane_top = -INFINITY;
+    if (lane == 0) counts[beam] = 0;
+    for (int i = lane; i < K; i += 32) best_key[beam * K + i] = 0;
+    for (int base = 0; base < p.groups; base += 512) {
+      float t[16];
+      load_groups(tops, base, p.groups, lane, t);
+#pragma unroll
+      for (int u = 0; u < 16; ++u) lane_top = fmaxf(lane_top, t[u]);
+    }
+    __syncwarp();
+    // Of 32 maxima over the lanes' groups the K-th is reached by K groups and
+    // few more (all, below K finite ones).  For K up to 16; more beams, or
+    // more groups than can be held, pick the K groups one by one.
+    float floor_v = __shfl_sync(0xffffffffu, warp_sort(lane_top, lane), min(K, 32) - 1);
+    if (floor_v == -INFINITY) floor_v = -FLT_MAX;
+    int n_groups = kJoinGroups + 1;
+    if (K <= 16) {
+      for (int base = 0; base < p.groups; base += 512) {
+        float t[16];
+        load_groups(tops, base, p.groups, lane, t);
+        uint32_t hits = 0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) hits |= t[u] >= floor_v ? 1u << u : 0u;
+        for (; hits; hits &= hits - 1) {
+          const int at = atomicAdd(&counts[beam], 1);
+          if (at < kJoinGroups) chosen[beam][at] = base + (__ffs(hits) - 1) * 32 + lane;
         }
       }
-    } else {
-      unsigned long long head = 0;
-      int from = -1;
+      __syncwarp();
+      n_groups = counts[beam];
+    }
+    if (n_groups > kJoinGroups) {
+      unsigned long long last = 0, mine = 0;
       const auto look = [&]() {
-        head = 0;
-        for (int c = lane; c < C; c += 32) {
-          const int at = next[beam * C + c];
-          const unsigned long long v = at < K ? mine[c * K + at] : 0;
-          if (v > head) head = v, from = c;
+        float v = -INFINITY;
+        int g = -1;
+        for (int i = lane; i < p.groups; i += 32) {
+          const float t = tops[i];
+          if (t > v) v = t, g = i;
         }
+        mine = g < 0 ? 0 : order_key(v, g);
       };
       look();
-      for (int k = 0; k < K; ++k) {
-        const unsigned long long best = warp_max(head);
-        if (lane == 0) best_key[beam * K + k] = best;
-        if (best && best == head) {
-          ++next[beam * C + from];
+      for (n_groups = 0; n_groups < K; ++n_groups) {  // ties: the first groups, whose ids are lower
+        const unsigned long long best = warp_max(mine);
+        if (!best) break;
+        last = best;
+        if (lane == 0) chosen[beam][n_groups] = static_cast<int>(key_index(best));
+        if (mine == best) {
+          tops[key_index(best)] = -INFINITY;
           look();
         }
+      }
+      floor_v = n_groups == K ? key_value(last) : -FLT_MAX;
+    }
+    __syncwarp();
+    // every logit of theirs that reaches the bound
+    const RowOf<T> in(p, row);
+    const auto id_of = [&](int k) { return chosen[beam][k] * (32 * kVec) - in.skew + lane * kVec; };
+    unsigned long long *keep = keeps[beam];
+    uint4 *mine = vectors + beam * (kJoinAhead * 32) + lane;
+    int n = 0;
+    for (int k0 = 0; k0 < n_groups; k0 += kJoinAhead) {
+      const int here = min(kJoinAhead, n_groups - k0);
+      for (int u = 0; u < here; ++u) {
+        const int id = id_of(k0 + u);
+        if (id >= 0 && id + kVec <= p.V)
+          copy16_async(mine + u * 32, in.src + id);
+        else
+          mine[u * 32] = edge_vector<T>(in.src, id, p.V);
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      for (int u = 0; u < here; ++u) {
+        float y[kVec];
+        L::unpack(mine[u * 32], y);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const unsigned have = __ballot_sync(0xffffffffu, y[e] >= floor_v);
+          if (!have) continue;
+          const int at = n + __popc(have & ((1u << lane) - 1));
+          if (y[e] >= floor_v && at < kSelKeep) keep[at] = order_key(y[e], id_of(k0 + u) + e);
+          n += __popc(have);
+        }
+      }
+    }
+    __syncwarp();
+    if (n <= kSelKeep) {  // each one's rank is the number of larger ones
+      if (p.suppress)
+        for (int i = lane; i < n; i += 32)
+          if (p.suppress[key_index(keep[i])]) keep[i] = 0;
+      __syncwarp();
+      for (int i = lane; i < n; i += 32) {
+        const unsigned long long key = keep[i];
+        if (!key) continue;
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) rank += keep[j] > key;
+        if (rank < K) best_key[beam * K + rank] = key;
+      }
+    } else {  // many equal ones: round by round over the groups
+      unsigned long long below = ~0ull;
+      for (int k = 0; k < K; ++k) {
+        unsigned long long best = 0;
+#pragma unroll 1
+        for (int g = 0; g < n_groups; ++g) {
+          const int id = id_of(g);
+          float y[kVec];
+          L::unpack(in.vector(id), y);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const unsigned long long key = y[e] >= floor_v && !(p.suppress && p.suppress[id + e]) ? order_key(y[e], id + e) : 0;
+            if (key < below && key > best) best = key;
+          }
+        }
+        below = warp_max(best);
+        if (lane == 0) best_key[beam * K + k] = below;
       }
     }
   }
@@ -342,14 +432,14 @@ __global__ void __launch_bounds__((WF_MAX_BEAMS + 1) * 32) beam_join_kernel(cons
     const int w = i / K;
     const unsigned long long k = best_key[i];
     // a row whose maximum is infinite has no scores but NaN, which is no candidate
-    const float m = row_max[w], total = k && m < INFINITY ? p.scores[row0 + w] + ((key_value(k) - m) - row_log[w]) : -INFINITY;
+    const float m = row_max[w], total = k && m < INFINITY ? row_score[w] + ((key_value(k) - m) - row_log[w]) : -INFINITY;
     cand[i] = total > -INFINITY ? order_key(total, i) : 0;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < W * K; i += blockDim.x) {
     const unsigned long long k = cand[i];
     int rank = 0;
-#pragma unroll 10
+#pragma unroll 5
     for (int j = 0; j < W * K; ++j) rank += cand[j] > k;
     if (k && rank < K) ranked[rank] = k;
   }
@@ -375,15 +465,38 @@ __global__ void __launch_bounds__((WF_MAX_BEAMS + 1) * 32) beam_join_kernel(cons
 
 using namespace wf;
 
-// 15 bytes of skew may push a row's end into another chunk.
-static int select_chunks(int V) { return (V + 7 + kSelChunk - 1) / kSelChunk; }
-constexpr int kSelMaxVocab = 1 << 22;  // the join keeps a byte for each of a request's chunks in shared memory
+// The kernels of a call.  The segments keep the L1 that the suppressed ids are
+// read through: with the largest shared-memory carveout 96 requests x 5 beams
+// took 38 us instead of 31.
+template <typename T>
+static bool select_ready(const void **segment, const void **join) {
+  *segment = reinterpret_cast<const void *>(beam_segment_kernel<T>), *join = reinterpret_cast<const void *>(beam_join_kernel<T>);
+  static const bool ok = [](const void *b) {
+    return cudaFuncSetAttribute(b, cudaFuncAttributeMaxDynamicSharedMemorySize, WF_MAX_BEAMS * kJoinAhead * 512) == cudaSuccess;
+  }(*join);
+  return ok;
+}
+constexpr int kSelMaxVocab = 1 << 24;
+// Segments of a row: as many as the GPU's warps take at once (32 an SM).
+struct SelectPlan {
+  int tiles, segments, groups;
+};
+static SelectPlan select_plan(long long rows, int V, bool wide) {
+  const int all = (V + 7 + kSelTile - 1) / kSelTile;  // 15 bytes of skew may push a row's end into another tile
+  SelectPlan a;
+  const long long most = std::min<long long>(all, std::max<long long>(1, 152 * 32 / rows));
+  a.tiles = static_cast<int>((all + most - 1) / most);
+  a.segments = (all + a.tiles - 1) / a.tiles;
+  a.groups = all * (wide ? 8 : 4);
+  return a;
+}
 
 extern "C" {
 
 size_t wf_beam_select_scratch_bytes(int32_t n_req, int32_t beams, int32_t vocab) {
   if (n_req <= 0 || beams <= 0 || beams > WF_MAX_BEAMS || vocab < 2 * beams || vocab > kSelMaxVocab) return 0;
-  return static_cast<size_t>(n_req) * beams * select_chunks(vocab) * (2 * beams * 8 + 16);
+  const SelectPlan a = select_plan(static_cast<long long>(n_req) * beams, vocab, true);
+  return static_cast<size_t>(n_req) * beams * (a.segments * 12 + a.groups * 4);
 }
 
 wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const float *d_scores, const uint8_t *d_suppress,
@@ -401,22 +514,22 @@ wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const 
   if (scratch_bytes < wf_beam_select_scratch_bytes(n_req, beams, vocab)) return WF_ERR_CAPACITY;
   SelectParams p = {};
   p.logits = d_logits, p.ld = ld, p.scores = d_scores, p.suppress = d_suppress;
-  p.n_req = n_req, p.W = beams, p.V = vocab, p.eos = eos < 0 ? -2 : eos, p.chunks = select_chunks(vocab);
+  p.n_req = n_req, p.W = beams, p.V = vocab, p.eos = eos < 0 ? -2 : eos;
+  const SelectPlan plan = select_plan(rows, vocab, dtype == WF_F32);
+  p.tiles = plan.tiles, p.segments = plan.segments, p.groups = plan.groups;
   p.token = d_token, p.parent = d_parent, p.score = d_score, p.fin_parent = d_fin_parent, p.fin_score = d_fin_score;
-  p.keys = static_cast<unsigned long long *>(d_scratch);
-  p.sum = reinterpret_cast<unsigned long long *>(p.keys + rows * p.chunks * 2 * beams);
-  p.max = reinterpret_cast<float *>(p.sum + rows * p.chunks);
-  const void *fn = dtype == WF_F32 ? reinterpret_cast<const void *>(beam_chunk_kernel<float>)
-                   : dtype == WF_F16 ? reinterpret_cast<const void *>(beam_chunk_kernel<__half>)
-                                     : reinterpret_cast<const void *>(beam_chunk_kernel<__nv_bfloat16>);
+  p.sum = static_cast<unsigned long long *>(d_scratch);
+  p.max = reinterpret_cast<float *>(p.sum + rows * p.segments);
+  p.group_max = p.max + rows * p.segments;
+  const void *fn, *join;
+  if (!(dtype == WF_F32 ? select_ready<float>(&fn, &join) : dtype == WF_F16 ? select_ready<__half>(&fn, &join) : select_ready<__nv_bfloat16>(&fn, &join)))
+    return WF_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const size_t lists = static_cast<size_t>(beams) * p.chunks;
-  int staged = lists * 2 * beams * 8 <= kJoinStage;
-  void *args[] = {&p}, *join_args[] = {&p, &staged};
-  const dim3 grid(p.chunks, static_cast<unsigned>(std::min<long long>(rows, 65535)), static_cast<unsigned>((rows + 65534) / 65535));
-  if (launch_pdl(fn, grid, kSelThreads, 0, args, s) != cudaSuccess ||
-      launch_pdl(reinterpret_cast<const void *>(beam_join_kernel), n_req, (beams + 1) * 32, lists + (staged ? lists * 2 * beams * 8 : 0),
-                 join_args, s) != cudaSuccess)
+  void *args[] = {&p};
+  const long long grid = (rows * p.segments + kSelWarps - 1) / kSelWarps;
+  if (grid > INT32_MAX) return WF_ERR_UNSUPPORTED;
+  if (launch_pdl(fn, static_cast<unsigned>(grid), kSelThreads, 0, args, s) != cudaSuccess ||
+      launch_pdl(join, n_req, beams * 64, static_cast<size_t>(beams) * kJoinAhead * 512, args, s) != cudaSuccess)
     return WF_ERR_CUDA;
   return WF_OK;
 }

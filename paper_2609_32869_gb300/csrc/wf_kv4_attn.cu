@@ -97,12 +97,6 @@ struct Codes<__half> {
   }
 };
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-
 __device__ __forceinline__ void bulk_load(void *smem_dst, const void *src, uint32_t bytes, uint64_t *bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(smem_dst)),
                "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
@@ -573,7 +567,7 @@ static cudaError_t launch(const Kv4AttnParams &p, cudaStream_t s) {
   static const cudaError_t ready = [] {
     const void *fn = reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>);
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    return e != cudaSuccess ? e : prefer_shared(fn);
   }();
   if (ready != cudaSuccess) return ready;
   const dim3 grid(p.n_seq * p.pool.heads, p.chunks, p.row_groups);

@@ -450,7 +450,9 @@ def _exact(x):
 
 @pytest.mark.parametrize("n,W,V,dtype", [(1, 1, 2, "f32"), (3, 1, 1000, "bf16"), (2, 2, 4, "f32"), (4, 5, 33, "f16"), (2, 5, 51866, "f32"),
                                          (3, 4, 51865, "bf16"), (2, 16, 40, "f32"), (1, 16, 9001, "f16"), (40, 3, 513, "f32"),
-                                         (1, 3, 200001, "f32"), (2, 8, 4096, "f32"), (2, 8, 4097, "bf16")])
+                                         (1, 3, 200001, "f32"), (2, 8, 4096, "f32"), (2, 8, 4097, "bf16"),
+                                         # segments of 3 and of 8 tiles, and more than 32 lists' worth of vocabulary
+                                         (70, 5, 20011, "f32"), (200, 4, 9000, "f16"), (1, 2, 600007, "bf16")])
 def test_select_random(n, W, V, dtype):
     import torch
     from paper_2609_32869_gb300 import binding as B
@@ -481,6 +483,9 @@ def test_select_ties_go_to_the_lowest_beam_and_id():
     assert got["token"][0].tolist() == [V - 1, V - 3, V - 4] and got["fin_parent"][0].tolist() == [0, -1, -1]
     got, x = _select(torch, B, -np.repeat(up, 3, 1), np.array([[-100, 0, -100.0]]), None, V - 2, "f32")
     assert got["token"][0].tolist() == [0, 1, 2] and got["parent"][0].tolist() == [1, 1, 1]
+    # every logit larger than all before it, in every beam: each tile displaces all that came before
+    got, x = _select(torch, B, np.repeat(np.arange(60000, dtype=np.float64)[None, None] / 256, 16, 1), np.zeros((1, 16)), None, -1, "f32")
+    assert got["token"][0].tolist() == [59999] * 16 and got["parent"][0].tolist() == list(range(16))
     # minus zero equals zero
     z = np.zeros((1, 1, 8))
     z[0, 0, ::2] = -0.0
