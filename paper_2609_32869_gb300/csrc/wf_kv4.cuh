@@ -117,6 +117,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+// (w & mask) | magic in one instruction, which the compiler makes two of.
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t magic) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "r"(mask), "r"(magic));
+  return d;
+}
+
 template <typename T>
 struct Kv4Type;
 template <>

@@ -134,106 +134,269 @@ struct StoreParams {
   uint32_t *err;
 };
 constexpr int kRowThreads = 256;
+constexpr int kRowWarps = kRowThreads / 32;
 
-// Eight lanes quantise one group of a row: 8 values each, the extremes by
-// three exchanges.
+// A warp's unit is one group of 16 rows, keys and values.  Where 16
+// consecutive rows fill a record (a prefill's do, but seldom from a multiple
+// of 16 rows on), the warp of their first row takes them as a whole: the record
+// is put together in shared memory and written, or read, 16 bytes a lane.  All
+// other rows go one by one, to the same places.
+struct RowUnit {
+  int slab;
+  int whole;        // first row of a record that begins in this unit's rows; -1: none
+  uint32_t single;  // of the unit's 16 rows, those outside whole records
+};
+__device__ __forceinline__ RowUnit row_unit(const StoreParams &p, long long unit, int slabs, int lane, int &slot) {
+  RowUnit r;
+  const int tile = static_cast<int>(unit / slabs);
+  r.slab = static_cast<int>(unit - static_cast<long long>(tile) * slabs);
+  // lane j holds the slots of rows 16 (tile - 1) + j and 16 (tile + 1) + j
+  const int r0 = (tile - 1) * 16 + lane, r1 = r0 + 32;
+  const int s0 = r0 >= 0 && r0 < p.n ? p.slots[r0] : -2, s1 = r1 < p.n ? p.slots[r1] : -2;
+  const int up0 = __shfl_up_sync(0xffffffffu, s0, 1), up1 = __shfl_up_sync(0xffffffffu, s1, 1), last0 = __shfl_sync(0xffffffffu, s0, 31);
+  // bit j: row 16 (tile - 1) + j goes on from the one before it
+  const unsigned long long next =
+      __ballot_sync(0xffffffffu, lane > 0 && s0 == up0 + 1) | static_cast<unsigned long long>(__ballot_sync(0xffffffffu, s1 == (lane ? up1 : last0) + 1)) << 32;
+  const unsigned long long first = __ballot_sync(0xffffffffu, s0 >= 0 && (s0 & 15) == 0);
+  // a record starts at bit j: its slot is a multiple of 16 and 15 rows go on
+  const auto starts = [&](int j) { return j >= 0 && (first >> j & 1) && (next >> (j + 1) & 0x7fff) == 0x7fff; };
+  const int j = lane & 15;
+  const int mine = __shfl_sync(0xffffffffu, s0, 16 + j);  // of row 16 tile + j
+  const uint32_t begins = __ballot_sync(0xffffffffu, lane < 16 && starts(16 + j)) & 0xffff;
+  r.single = __ballot_sync(0xffffffffu, lane < 16 && mine >= 0 && !starts(16 + j - (mine & 15))) & 0xffff;
+  r.whole = begins ? tile * 16 + __ffs(begins) - 1 : -1;
+  slot = mine;
+  return r;
+}
+
+// Codes of 8 values x against (s, z), the first in the lowest nibble:
+// clamp(rint((x - z) / s), -8, 7) + 8 with the quotient rounded to fp32.  By
+// the reciprocal, but for scales near the ends of fp32's range and for
+// quotients that the reciprocal's rounding might take across a half.
+__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], float s, float z) {
+  uint32_t codes = 0;
+  if (!(s > 0.f)) return 0x88888888u;
+  const float inv = 1.f / s;
+  bool near = !(s > 1e-30f && s < 1e30f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = fminf(fmaxf((x[i] - z) * inv, -8.f), 7.f), f = t + 12582920.f;  // 1.5 * 2^23 + 8
+    near |= fabsf(fabsf(t - (f - 12582920.f)) - 0.5f) < 1e-4f;
+    codes |= (__float_as_uint(f) & 15u) << (4 * i);
+  }
+  if (near) {
+    codes = 0;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+      float v = x[0];
+#pragma unroll
+      for (int q = 1; q < 8; ++q) v = i == q ? x[q] : v;
+      codes |= static_cast<uint32_t>(static_cast<int>(fminf(fmaxf(rintf((v - z) / s), -8.f), 7.f)) + 8) << (4 * i);
+    }
+  }
+  return codes;
+}
+
+// Quantises one group of a row held by 8 lanes, 8 values each; all lanes call.
+template <typename T>
+__device__ __forceinline__ uint32_t quantise_row(uint4 w, int lane, uint32_t &sz) {
+  using X = Kv4Type<T>;
+  const float x[8] = {X::lo(w.x), X::hi(w.x), X::lo(w.y), X::hi(w.y), X::lo(w.z), X::hi(w.z), X::lo(w.w), X::hi(w.w)};
+  float hi = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+  float lo = -max3(max3(-x[0], -x[1], -x[2]), max3(-x[3], -x[4], -x[5]), fmaxf(-x[6], -x[7]));
+  float bad = 0.f;  // NaN where a value is not finite
+#pragma unroll
+  for (int i = 0; i < 8; ++i) bad = fmaf(x[i], 0.f, bad);
+#pragma unroll
+  for (int off = 1; off < 8; off <<= 1) {
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, off));
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, off));
+  }
+  const bool fine = ((__ballot_sync(0xffffffffu, bad == 0.f) >> (lane & 24)) & 0xffu) == 0xffu;
+  // halves first: max - min may pass the type's range
+  const float s = fine ? X::round((0.5f * hi - 0.5f * lo) / 7.5f) : NAN;
+  const float z = fine ? X::round(hi - 7.f * s) : NAN;  // 7 s is exact in fp32
+  sz = X::pack(s, z);
+  return quantise8(x, s, z);
+}
+
+// 8 codes against (s, z), rounded once: s (c - 8) has at most 15 bits, and the
+// sum that the fused operation rounds is what fp32 would hold first.
+__device__ __forceinline__ uint4 dequantise8(uint32_t w, uint32_t sz, __nv_bfloat16) {
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = and_or(w >> (4 * i), 0x000f000fu, 0x43004300u), eight = 0x43084308u;  // 128 + c, 136
+    const uint32_t s2 = __byte_perm(sz, 0, 0x1010), z2 = __byte_perm(sz, 0, 0x3232);
+    const __nv_bfloat162 c = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&eight));
+    const __nv_bfloat162 v = __hfma2(c, *reinterpret_cast<const __nv_bfloat162 *>(&s2), *reinterpret_cast<const __nv_bfloat162 *>(&z2));
+    r[i] = *reinterpret_cast<const uint32_t *>(&v);
+  }
+  return make_uint4(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410), __byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632));
+}
+__device__ __forceinline__ uint4 dequantise8(uint32_t w, uint32_t sz, __half) {
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = and_or(w >> (4 * i), 0x000f000fu, 0x64006400u), eight = 0x64086408u;  // 1024 + c, 1032
+    const uint32_t s2 = __byte_perm(sz, 0, 0x1010), z2 = __byte_perm(sz, 0, 0x3232);
+    const __half2 c = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&eight));
+    const __half2 v = __hfma2(c, *reinterpret_cast<const __half2 *>(&s2), *reinterpret_cast<const __half2 *>(&z2));
+    r[i] = *reinterpret_cast<const uint32_t *>(&v);
+  }
+  return make_uint4(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410), __byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632));
+}
+
+// The places of a row's 8 codes from dim 8 j on in a record.
+__device__ __forceinline__ void put_codes(unsigned char *rec, int at, int j, int is_v, uint32_t codes) {
+  if (is_v) {
+    *reinterpret_cast<uint16_t *>(rec + kv4_val_offset(at, j, 0)) = static_cast<uint16_t>(codes);
+    *reinterpret_cast<uint16_t *>(rec + kv4_val_offset(at, j, 1)) = static_cast<uint16_t>(codes >> 16);
+  } else {
+    *reinterpret_cast<uint32_t *>(rec + at * 32 + j * 4) = codes;
+  }
+}
+__device__ __forceinline__ uint32_t get_codes(const unsigned char *rec, int at, int j, int is_v) {
+  if (is_v)
+    return *reinterpret_cast<const uint16_t *>(rec + kv4_val_offset(at, j, 0)) |
+           static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(rec + kv4_val_offset(at, j, 1))) << 16;
+  return *reinterpret_cast<const uint32_t *>(rec + at * 32 + j * 4);
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) kv4_store_kernel(const StoreParams p) {
+  __shared__ __align__(16) unsigned char records[kRowWarps][kKv4Rec];
   pdl_wait();
   pdl_launch_dependents();
-  using X = Kv4Type<T>;
+  const int lane = threadIdx.x & 31, j = lane & 7, sub = lane >> 3;
+  unsigned char *rec = records[threadIdx.x >> 5];
   const int slabs = p.pool.heads * p.pool.groups;
-  const long long units = static_cast<long long>(p.n) * slabs * 2;
-  const int j = threadIdx.x & 7;
-  const long long step = static_cast<long long>(gridDim.x) * (kRowThreads / 8);
-  // whole warps iterate together: the exchanges below need all their lanes
-  const long long first = static_cast<long long>(blockIdx.x) * (kRowThreads / 8) + (threadIdx.x >> 3);
-  for (long long u = first; u - (first & 3) < units; u += step) {
-    const bool in = u < units;
-    const long long uu = in ? u : units - 1;
-    const int slab = static_cast<int>(uu % slabs);
-    const int is_v = static_cast<int>(uu / slabs % 2);
-    const int row = static_cast<int>(uu / slabs / 2);
-    const int slot = p.slots[row];
-    const T *src = static_cast<const T *>(is_v ? p.v : p.k) + row * (is_v ? p.v_stride : p.k_stride) + slab * 64 + j * 8;
-    const uint4 w = *reinterpret_cast<const uint4 *>(src);
-    float x[8] = {X::lo(w.x), X::hi(w.x), X::lo(w.y), X::hi(w.y), X::lo(w.z), X::hi(w.z), X::lo(w.w), X::hi(w.w)};
-    float hi = x[0], lo = x[0];
-    bool fine = true;
+  const long long units = (static_cast<long long>(p.n) + 15) / 16 * slabs;
+  for (long long unit = static_cast<long long>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5); unit < units;
+       unit += static_cast<long long>(gridDim.x) * kRowWarps) {
+    int slot;
+    const RowUnit u = row_unit(p, unit, slabs, lane, slot);
+    const int tile = static_cast<int>(unit / slabs);
+    const T *k = static_cast<const T *>(p.k) + u.slab * 64 + j * 8, *v = static_cast<const T *>(p.v) + u.slab * 64 + j * 8;
+    if (u.whole >= 0) {
+      const int at = p.slots[u.whole], block = at >> p.pool.bs_shift;
+      uint4 w[2][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      hi = fmaxf(hi, x[i]), lo = fminf(lo, x[i]);
-      fine &= isfinite(x[i]);
-    }
+      for (int i = 0; i < 4; ++i) {
+        const long long row = u.whole + i * 4 + sub;
+        w[0][i] = *reinterpret_cast<const uint4 *>(k + row * p.k_stride);
+        w[1][i] = *reinterpret_cast<const uint4 *>(v + row * p.v_stride);
+      }
+      __syncwarp();
 #pragma unroll
-    for (int off = 1; off < 8; off <<= 1) {
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, off));
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, off));
-    }
-    fine = ((__ballot_sync(0xffffffffu, fine) >> (threadIdx.x & 24)) & 0xffu) == 0xffu;
-    // halves first: max - min may pass the type's range
-    const float s = fine ? X::round((0.5f * hi - 0.5f * lo) / 7.5f) : NAN;
-    const float z = fine ? X::round(hi - 7.f * s) : NAN;  // 7 s is exact in fp32
-    uint32_t codes = 0;
+      for (int is_v = 0; is_v < 2; ++is_v)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float c = s > 0.f ? fminf(fmaxf(rintf((x[i] - z) / s), -8.f), 7.f) : 0.f;
-      codes |= static_cast<uint32_t>(static_cast<int>(c) + 8) << (4 * i);
+        for (int i = 0; i < 4; ++i) {
+          uint32_t sz;
+          const uint32_t codes = quantise_row<T>(w[is_v][i], lane, sz);
+          put_codes(rec, i * 4 + sub, j, is_v, codes);
+          if (j == 0) *reinterpret_cast<uint32_t *>(rec + kv4_scale_offset(i * 4 + sub, is_v)) = sz;
+        }
+      __syncwarp();
+      if (block < p.pool.n_blocks) {
+        uint4 *dst = reinterpret_cast<uint4 *>(kv4_record(p.pool, block, 0, u.slab, (at & (p.pool.bs - 1)) >> 4));
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (i * 32 + lane < kKv4Rec / 16) dst[i * 32 + lane] = reinterpret_cast<const uint4 *>(rec)[i * 32 + lane];
+      } else if (lane == 0) {
+        set_error(p.err, WF_DEV_ERR_PAGE);
+      }
     }
-    if (!in || slot < 0) continue;
-    const int block = slot >> p.pool.bs_shift;
-    if (block >= p.pool.n_blocks) {
-      if (j == 0) set_error(p.err, WF_DEV_ERR_PAGE);
-      continue;
+    if (u.single) {
+      uint4 w[2][4];
+      int at[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = i * 4 + sub;
+        at[i] = __shfl_sync(0xffffffffu, slot, r);
+        if (!(u.single >> r & 1)) at[i] = -1;
+        if (at[i] >= 0 && at[i] >> p.pool.bs_shift >= p.pool.n_blocks) {
+          if (j == 0) set_error(p.err, WF_DEV_ERR_PAGE);
+          at[i] = -1;
+        }
+        w[0][i] = w[1][i] = make_uint4(0, 0, 0, 0);
+        if (at[i] >= 0) {
+          const long long row = static_cast<long long>(tile) * 16 + r;
+          w[0][i] = *reinterpret_cast<const uint4 *>(k + row * p.k_stride);
+          w[1][i] = *reinterpret_cast<const uint4 *>(v + row * p.v_stride);
+        }
+      }
+#pragma unroll
+      for (int is_v = 0; is_v < 2; ++is_v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t sz;
+          const uint32_t codes = quantise_row<T>(w[is_v][i], lane, sz);
+          if (at[i] < 0) continue;
+          const int pos = at[i] & (p.pool.bs - 1);
+          unsigned char *dst = kv4_record(p.pool, at[i] >> p.pool.bs_shift, 0, u.slab, pos >> 4);
+          put_codes(dst, pos & 15, j, is_v, codes);
+          if (j == 0) *reinterpret_cast<uint32_t *>(dst + kv4_scale_offset(pos & 15, is_v)) = sz;
+        }
     }
-    const int pos = slot & (p.pool.bs - 1), at = pos & 15;
-    unsigned char *rec = kv4_record(p.pool, block, 0, slab, pos >> 4);
-    if (is_v) {
-      *reinterpret_cast<uint16_t *>(rec + kv4_val_offset(at, j, 0)) = static_cast<uint16_t>(codes);
-      *reinterpret_cast<uint16_t *>(rec + kv4_val_offset(at, j, 1)) = static_cast<uint16_t>(codes >> 16);
-    } else {
-      *reinterpret_cast<uint32_t *>(rec + at * 32 + j * 4) = codes;
-    }
-    if (j == 0) *reinterpret_cast<uint32_t *>(rec + kv4_scale_offset(at, is_v)) = X::pack(s, z);
   }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) kv4_load_kernel(const StoreParams p) {
+  __shared__ __align__(16) unsigned char records[kRowWarps][kKv4Rec];
   pdl_wait();
   pdl_launch_dependents();
-  using X = Kv4Type<T>;
+  const int lane = threadIdx.x & 31, j = lane & 7, sub = lane >> 3;
+  unsigned char *rec = records[threadIdx.x >> 5];
   const int slabs = p.pool.heads * p.pool.groups;
-  const long long units = static_cast<long long>(p.n) * slabs * 2;
-  const int j = threadIdx.x & 7;
-  for (long long u = static_cast<long long>(blockIdx.x) * (kRowThreads / 8) + (threadIdx.x >> 3); u < units;
-       u += static_cast<long long>(gridDim.x) * (kRowThreads / 8)) {
-    const int slab = static_cast<int>(u % slabs);
-    const int is_v = static_cast<int>(u / slabs % 2);
-    const int row = static_cast<int>(u / slabs / 2);
-    const int slot = p.slots[row];
-    uint4 out = {0, 0, 0, 0};
-    const int block = slot >> p.pool.bs_shift;
-    if (slot >= 0 && block < p.pool.n_blocks) {
-      const int pos = slot & (p.pool.bs - 1), at = pos & 15;
-      const unsigned char *rec = kv4_record(p.pool, block, 0, slab, pos >> 4);
-      uint32_t codes;
-      if (is_v)
-        codes = *reinterpret_cast<const uint16_t *>(rec + kv4_val_offset(at, j, 0)) |
-                static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(rec + kv4_val_offset(at, j, 1))) << 16;
-      else
-        codes = *reinterpret_cast<const uint32_t *>(rec + at * 32 + j * 4);
-      const uint32_t sz = *reinterpret_cast<const uint32_t *>(rec + kv4_scale_offset(at, is_v));
-      const float s = X::lo(sz), z = X::hi(sz);
-      float x[8];
+  const long long units = (static_cast<long long>(p.n) + 15) / 16 * slabs;
+  for (long long unit = static_cast<long long>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5); unit < units;
+       unit += static_cast<long long>(gridDim.x) * kRowWarps) {
+    int slot;
+    const RowUnit u = row_unit(p, unit, slabs, lane, slot);
+    const int tile = static_cast<int>(unit / slabs);
+    T *k = static_cast<T *>(p.k_out) + u.slab * 64 + j * 8, *v = static_cast<T *>(p.v_out) + u.slab * 64 + j * 8;
+    if (u.whole >= 0) {
+      const int at = p.slots[u.whole], block = at >> p.pool.bs_shift;
+      const bool in = block < p.pool.n_blocks;
+      if (!in && lane == 0) set_error(p.err, WF_DEV_ERR_PAGE);
+      __syncwarp();
+      const uint4 *src = reinterpret_cast<const uint4 *>(kv4_record(p.pool, in ? block : 0, 0, u.slab, (at & (p.pool.bs - 1)) >> 4));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fmaf(s, static_cast<float>(static_cast<int>(codes >> (4 * i) & 15) - 8), z);
-      out = {X::pack(x[0], x[1]), X::pack(x[2], x[3]), X::pack(x[4], x[5]), X::pack(x[6], x[7])};
-    } else if (slot >= 0 && j == 0) {
-      set_error(p.err, WF_DEV_ERR_PAGE);
+      for (int i = 0; i < 3; ++i)
+        if (i * 32 + lane < kKv4Rec / 16) reinterpret_cast<uint4 *>(rec)[i * 32 + lane] = src[i * 32 + lane];
+      __syncwarp();
+#pragma unroll
+      for (int is_v = 0; is_v < 2; ++is_v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = i * 4 + sub;
+          uint4 x = dequantise8(get_codes(rec, r, j, is_v), *reinterpret_cast<const uint32_t *>(rec + kv4_scale_offset(r, is_v)), T());
+          if (!in) x = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4 *>((is_v ? v : k) + (u.whole + r) * (is_v ? p.v_stride : p.k_stride)) = x;
+        }
     }
-    T *dst = static_cast<T *>(is_v ? p.v_out : p.k_out) + row * (is_v ? p.v_stride : p.k_stride) + slab * 64 + j * 8;
-    *reinterpret_cast<uint4 *>(dst) = out;
+    // rows outside whole records, and those without a slot, which read as zeros
+    const uint32_t rest = u.single | (__ballot_sync(0xffffffffu, lane < 16 && tile * 16 + lane < p.n && slot < 0) & 0xffff);
+    if (rest) {
+#pragma unroll
+      for (int is_v = 0; is_v < 2; ++is_v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = i * 4 + sub, at = __shfl_sync(0xffffffffu, slot, r);
+          if (!(rest >> r & 1)) continue;
+          uint4 x = {0, 0, 0, 0};
+          if (at >= 0 && at >> p.pool.bs_shift < p.pool.n_blocks) {
+            const int pos = at & (p.pool.bs - 1);
+            const unsigned char *src = kv4_record(p.pool, at >> p.pool.bs_shift, 0, u.slab, pos >> 4);
+            x = dequantise8(get_codes(src, pos & 15, j, is_v), *reinterpret_cast<const uint32_t *>(src + kv4_scale_offset(pos & 15, is_v)), T());
+          } else if (at >= 0 && j == 0) {
+            set_error(p.err, WF_DEV_ERR_PAGE);
+          }
+          *reinterpret_cast<uint4 *>((is_v ? v : k) + (static_cast<long long>(tile) * 16 + r) * (is_v ? p.v_stride : p.k_stride)) = x;
+        }
+    }
   }
 }
 
@@ -476,8 +639,8 @@ static wf_status rows_launch(const void *fn, StoreParams *p, void *stream) {
   if (p->n == 0) return WF_OK;
   const int sms = sm_count();
   if (!sms) return WF_ERR_CUDA;
-  const long long units = static_cast<long long>(p->n) * p->pool.heads * p->pool.groups * 2;
-  const long long want = (units + kRowThreads / 8 - 1) / (kRowThreads / 8);
+  const long long units = (static_cast<long long>(p->n) + 15) / 16 * p->pool.heads * p->pool.groups;
+  const long long want = (units + kRowWarps - 1) / kRowWarps;
   void *args[] = {p};
   return launch_pdl(fn, static_cast<unsigned>(std::min<long long>(want, 32LL * sms)), kRowThreads, 0, args,
                     static_cast<cudaStream_t>(stream)) == cudaSuccess

@@ -123,12 +123,13 @@ def test_page_plan_many(n, bs, most):
 # -------------------------------------------------------------- store, load --
 @pytest.mark.parametrize("n,bs,heads,dim,dtype,pad", [
     (1, 16, 1, 64, "bf16", 0), (5, 16, 3, 64, "bf16", 64), (33, 32, 2, 128, "f16", 8), (64, 64, 6, 64, "f16", 0),
-    (130, 64, 1, 128, "bf16", 0), (48, 16, 2, 64, "bf16", 0),
+    (130, 64, 1, 128, "bf16", 0), (48, 16, 2, 64, "bf16", 0), (17, 16, 5, 64, "f16", 0), (95, 32, 3, 64, "bf16", 8),
 ])
-@pytest.mark.parametrize("order", ["runs", "mixed"])
+@pytest.mark.parametrize("order", ["runs", "mixed", "requests"])
 def test_store_and_load(n, bs, heads, dim, dtype, pad, order):
     """Bytes equal the oracle's: the quantiser is fp32 arithmetic with every rounding named.
-    "runs": consecutive slots from an odd start, the order of a prefill; "mixed": any order, skipped rows."""
+    "runs": consecutive slots from an odd start, the order of a prefill; "mixed": any order, skipped rows;
+    "requests": runs that begin at a block, end anywhere and leave rows out, whole records from odd rows on."""
     import torch
     from paper_2609_32869_gb300 import binding as B
     rng = np.random.default_rng(n)
@@ -141,6 +142,14 @@ def test_store_and_load(n, bs, heads, dim, dtype, pad, order):
     big = 3.0e38 if dtype == "bf16" else 65504.0
     k[n // 2, -64:] = ob.round16(np.linspace(-big, big, 64), dtype)   # the range's ends
     slots = np.arange(n) + bs - 3 if order == "runs" else rng.permutation(blocks * bs)[:n]
+    if order == "requests":
+        slots, at, b = np.full(n, -1), n % 3, 0
+        while at < n:
+            m = min(int(rng.integers(1, 3 * bs)), n - at, (blocks - b) * bs)
+            slots[at:at + m] = b * bs + np.arange(m)
+            at, b = at + m + int(rng.integers(0, 3)), b + -(-m // bs)
+            if b >= blocks:
+                break
     slots = slots.astype(np.int32)
     if order == "mixed" and n > 4:
         slots[1] = -1
