@@ -103,6 +103,14 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "l"(*reinterpret_cast<const unsigned long long *>(&a)), "l"(*reinterpret_cast<const unsigned long long *>(&b)));
   return d;
 }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+      : "l"(*reinterpret_cast<const unsigned long long *>(&a)), "l"(*reinterpret_cast<const unsigned long long *>(&b)),
+        "l"(*reinterpret_cast<const unsigned long long *>(&c)));
+  return d;
+}
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   float2 d;
   asm("mul.rn.f32x2 %0, %1, %2;"

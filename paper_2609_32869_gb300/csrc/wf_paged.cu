@@ -169,55 +169,98 @@ __device__ __forceinline__ RowUnit row_unit(const StoreParams &p, long long unit
   return r;
 }
 
-// Codes of 8 values x against (s, z), the first in the lowest nibble:
-// clamp(rint((x - z) / s), -8, 7) + 8 with the quotient rounded to fp32.  By
-// the reciprocal, but for scales near the ends of fp32's range and for
-// quotients that the reciprocal's rounding might take across a half.
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], float s, float z) {
-  uint32_t codes = 0;
-  if (!(s > 0.f)) return 0x88888888u;
-  const float inv = 1.f / s;
-  bool near = !(s > 1e-30f && s < 1e30f);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = fminf(fmaxf((x[i] - z) * inv, -8.f), 7.f), f = t + 12582920.f;  // 1.5 * 2^23 + 8
-    near |= fabsf(fabsf(t - (f - 12582920.f)) - 0.5f) < 1e-4f;
-    codes |= (__float_as_uint(f) & 15u) << (4 * i);
-  }
-  if (near) {
-    codes = 0;
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-      float v = x[0];
-#pragma unroll
-      for (int q = 1; q < 8; ++q) v = i == q ? x[q] : v;
-      codes |= static_cast<uint32_t>(static_cast<int>(fminf(fmaxf(rintf((v - z) / s), -8.f), 7.f)) + 8) << (4 * i);
-    }
-  }
-  return codes;
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float min3_nan(float a, float b, float c) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
-// Quantises one group of a row held by 8 lanes, 8 values each; all lanes call.
+// Eight values for each of 8 lanes' 8 rows: lane j gets row j's over the lanes.
+template <typename F>
+__device__ __forceinline__ float rows_over_lanes(const float (&v)[8], int j, F op) {
+  float a[4], b[2];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) a[q] = op(j & 4 ? v[q + 4] : v[q], __shfl_xor_sync(0xffffffffu, j & 4 ? v[q] : v[q + 4], 4));
+#pragma unroll
+  for (int q = 0; q < 2; ++q) b[q] = op(j & 2 ? a[q + 2] : a[q], __shfl_xor_sync(0xffffffffu, j & 2 ? a[q] : a[q + 2], 2));
+  return op(j & 1 ? b[1] : b[0], __shfl_xor_sync(0xffffffffu, j & 1 ? b[0] : b[1], 1));
+}
+
+// Quantises one group of 8 rows held by 8 lanes, row c's values 8j .. 8j + 7
+// in lane j's w[c]: code = clamp(rint((x - z) / s), -8, 7) + 8, the quotient
+// rounded to fp32.  Lane j works out row j's (s, z).  A quotient is the
+// numerator times the rounded reciprocal, corrected once by its exact remainder,
+// which rounds it correctly (P. Markstein, IBM J. Res. Dev. 34 (1990) 111); it
+// has to, for exact halves are common among 16-bit values.  Rows where a
+// quotient needs the clamp or s is far from 1 are divided one by one.  All
+// lanes call.
 template <typename T>
-__device__ __forceinline__ uint32_t quantise_row(uint4 w, int lane, uint32_t &sz) {
+__device__ __forceinline__ void quantise_rows(const uint4 (&w)[8], int lane, uint32_t (&codes)[8], uint32_t (&sz)[8]) {
   using X = Kv4Type<T>;
-  const float x[8] = {X::lo(w.x), X::hi(w.x), X::lo(w.y), X::hi(w.y), X::lo(w.z), X::hi(w.z), X::lo(w.w), X::hi(w.w)};
-  float hi = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
-  float lo = -max3(max3(-x[0], -x[1], -x[2]), max3(-x[3], -x[4], -x[5]), fmaxf(-x[6], -x[7]));
-  float bad = 0.f;  // NaN where a value is not finite
+  const int j = lane & 7;
+  float hi[8], lo[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) bad = fmaf(x[i], 0.f, bad);
-#pragma unroll
-  for (int off = 1; off < 8; off <<= 1) {
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, off));
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, off));
+  for (int c = 0; c < 8; ++c) {
+    const float x[8] = {X::lo(w[c].x), X::hi(w[c].x), X::lo(w[c].y), X::hi(w[c].y), X::lo(w[c].z), X::hi(w[c].z), X::lo(w[c].w), X::hi(w[c].w)};
+    hi[c] = max3_nan(max3_nan(x[0], x[1], x[2]), max3_nan(x[3], x[4], x[5]), max_nan(x[6], x[7]));
+    lo[c] = min3_nan(min3_nan(x[0], x[1], x[2]), min3_nan(x[3], x[4], x[5]), min_nan(x[6], x[7]));
   }
-  const bool fine = ((__ballot_sync(0xffffffffu, bad == 0.f) >> (lane & 24)) & 0xffu) == 0xffu;
+  const float top = rows_over_lanes(hi, j, max_nan), low = rows_over_lanes(lo, j, min_nan);
+  const bool fine = isfinite(top) && isfinite(low);
   // halves first: max - min may pass the type's range
-  const float s = fine ? X::round((0.5f * hi - 0.5f * lo) / 7.5f) : NAN;
-  const float z = fine ? X::round(hi - 7.f * s) : NAN;  // 7 s is exact in fp32
-  sz = X::pack(s, z);
-  return quantise8(x, s, z);
+  const float s = fine ? X::round((0.5f * top - 0.5f * low) / 7.5f) : NAN;
+  const float z = fine ? X::round(top - 7.f * s) : NAN;  // 7 s is exact in fp32
+  const bool none = !(s > 0.f);  // all codes 8
+  const float inv = none ? 0.f : 1.f / s;
+  const bool plain = none || (s > 1e-20f && s < 1e20f && (top - z) * inv < 7.49f && (low - z) * inv > -8.49f);
+  const uint32_t pair = X::pack(s, z);
+  const unsigned slow = __ballot_sync(0xffffffffu, !plain), flat = __ballot_sync(0xffffffffu, none);
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const int from = (lane & 24) + c;
+    sz[c] = __shfl_sync(0xffffffffu, pair, from);
+    const float r = __shfl_sync(0xffffffffu, inv, from);
+    const bool zero = flat >> from & 1;
+    const float zc = zero ? 0.f : X::hi(sz[c]);
+    const float2 mz = {-zc, -zc}, rr = {r, r}, magic = {12582920.f, 12582920.f};  // 1.5 * 2^23 + 8
+    const uint32_t raw[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+    const float minus_s = -X::lo(sz[c]);
+    const float2 ms = {minus_s, minus_s};
+    uint32_t sum = 0;  // the codes sit in the low bits of magic's; its own share is taken off below
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 d = add2(make_float2(X::lo(raw[i]), X::hi(raw[i])), mz), t = mul2(d, rr);
+      const float2 f = add2(fma2(fma2(t, ms, d), rr, t), magic);
+      sum += __float_as_uint(f.x) * (1u << (8 * i));
+      sum += __float_as_uint(f.y) * (1u << (8 * i + 4));
+    }
+    codes[c] = zero ? 0x88888888u : sum - 0x4b400000u * 0x11111111u;
+    if (slow >> from & 1) {
+      uint32_t exact = 0;
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t u = i < 2 ? raw[0] : i < 4 ? raw[1] : i < 6 ? raw[2] : raw[3];
+        const float v = i & 1 ? X::hi(u) : X::lo(u);
+        exact |= static_cast<uint32_t>(static_cast<int>(fminf(fmaxf(rintf((zc - v) / minus_s), -8.f), 7.f)) + 8) << (4 * i);
+      }
+      codes[c] = exact;
+    }
+  }
 }
 
 // 8 codes against (s, z), rounded once: s (c - 8) has at most 15 bits, and the
@@ -280,23 +323,22 @@ __global__ void __launch_bounds__(kRowThreads) kv4_store_kernel(const StoreParam
     const T *k = static_cast<const T *>(p.k) + u.slab * 64 + j * 8, *v = static_cast<const T *>(p.v) + u.slab * 64 + j * 8;
     if (u.whole >= 0) {
       const int at = p.slots[u.whole], block = at >> p.pool.bs_shift;
-      uint4 w[2][4];
+      uint4 w[8];
+      uint32_t codes[8], sz[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const long long row = u.whole + i * 4 + sub;
-        w[0][i] = *reinterpret_cast<const uint4 *>(k + row * p.k_stride);
-        w[1][i] = *reinterpret_cast<const uint4 *>(v + row * p.v_stride);
+        w[i] = *reinterpret_cast<const uint4 *>(k + row * p.k_stride);
+        w[4 + i] = *reinterpret_cast<const uint4 *>(v + row * p.v_stride);
       }
+      quantise_rows<T>(w, lane, codes, sz);
       __syncwarp();
 #pragma unroll
-      for (int is_v = 0; is_v < 2; ++is_v)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t sz;
-          const uint32_t codes = quantise_row<T>(w[is_v][i], lane, sz);
-          put_codes(rec, i * 4 + sub, j, is_v, codes);
-          if (j == 0) *reinterpret_cast<uint32_t *>(rec + kv4_scale_offset(i * 4 + sub, is_v)) = sz;
-        }
+      for (int c = 0; c < 8; ++c) {
+        const int r = (c & 3) * 4 + sub;
+        put_codes(rec, r, j, c >> 2, codes[c]);
+        if (j == 0) *reinterpret_cast<uint32_t *>(rec + kv4_scale_offset(r, c >> 2)) = sz[c];
+      }
       __syncwarp();
       if (block < p.pool.n_blocks) {
         uint4 *dst = reinterpret_cast<uint4 *>(kv4_record(p.pool, block, 0, u.slab, (at & (p.pool.bs - 1)) >> 4));
@@ -308,7 +350,8 @@ __global__ void __launch_bounds__(kRowThreads) kv4_store_kernel(const StoreParam
       }
     }
     if (u.single) {
-      uint4 w[2][4];
+      uint4 w[8];
+      uint32_t codes[8], sz[8];
       int at[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -319,25 +362,22 @@ __global__ void __launch_bounds__(kRowThreads) kv4_store_kernel(const StoreParam
           if (j == 0) set_error(p.err, WF_DEV_ERR_PAGE);
           at[i] = -1;
         }
-        w[0][i] = w[1][i] = make_uint4(0, 0, 0, 0);
+        w[i] = w[4 + i] = make_uint4(0, 0, 0, 0);
         if (at[i] >= 0) {
           const long long row = static_cast<long long>(tile) * 16 + r;
-          w[0][i] = *reinterpret_cast<const uint4 *>(k + row * p.k_stride);
-          w[1][i] = *reinterpret_cast<const uint4 *>(v + row * p.v_stride);
+          w[i] = *reinterpret_cast<const uint4 *>(k + row * p.k_stride);
+          w[4 + i] = *reinterpret_cast<const uint4 *>(v + row * p.v_stride);
         }
       }
+      quantise_rows<T>(w, lane, codes, sz);
 #pragma unroll
-      for (int is_v = 0; is_v < 2; ++is_v)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t sz;
-          const uint32_t codes = quantise_row<T>(w[is_v][i], lane, sz);
-          if (at[i] < 0) continue;
-          const int pos = at[i] & (p.pool.bs - 1);
-          unsigned char *dst = kv4_record(p.pool, at[i] >> p.pool.bs_shift, 0, u.slab, pos >> 4);
-          put_codes(dst, pos & 15, j, is_v, codes);
-          if (j == 0) *reinterpret_cast<uint32_t *>(dst + kv4_scale_offset(pos & 15, is_v)) = sz;
-        }
+      for (int c = 0; c < 8; ++c) {
+        if (at[c & 3] < 0) continue;
+        const int pos = at[c & 3] & (p.pool.bs - 1);
+        unsigned char *dst = kv4_record(p.pool, at[c & 3] >> p.pool.bs_shift, 0, u.slab, pos >> 4);
+        put_codes(dst, pos & 15, j, c >> 2, codes[c]);
+        if (j == 0) *reinterpret_cast<uint32_t *>(dst + kv4_scale_offset(pos & 15, c >> 2)) = sz[c];
+      }
     }
   }
 }
