@@ -307,7 +307,7 @@ __device__ __forceinline__ uint32_t get_codes(const unsigned char *rec, int at, 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) kv4_store_kernel(const StoreParams p) {
+__global__ void __launch_bounds__(kRowThreads, 4) kv4_store_kernel(const StoreParams p) {
   __shared__ __align__(16) unsigned char records[kRowWarps][kKv4Rec];
   pdl_wait();
   pdl_launch_dependents();
