@@ -113,11 +113,21 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanParam
     const int32_t *ids = p.free_ids + (nf - 1 - own_block[k]);
     for (int c = c0 + threadIdx.x; c < c1; c += kPlanThreads) row[c] = ids[-(c - c0)];
     const int part = (a & (bs - 1)) ? row[a >> p.bs_shift] : 0;  // the block that old length ends in
-    for (int t = threadIdx.x; t < b - a; t += kPlanThreads) {
-      const int pos = a + t, c = pos >> p.bs_shift;
-      const int id = c < c0 ? part : ids[-(c - c0)];
-      p.slots[at + t] = id < 0 || id >= p.n_blocks ? -1 : (id << p.bs_shift) + (pos & (bs - 1));
-      if (id < 0 || id >= p.n_blocks) set_error(p.err, WF_DEV_ERR_PAGE);
+    for (int t0 = threadIdx.x; t0 < b - a; t0 += 8 * kPlanThreads) {
+      int id[8];  // eight reads in flight
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int c = (a + min(t0 + u * kPlanThreads, b - a - 1)) >> p.bs_shift;
+        id[u] = c < c0 ? part : ids[-(c - c0)];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int t = t0 + u * kPlanThreads;
+        if (t >= b - a) break;
+        const bool in = id[u] >= 0 && id[u] < p.n_blocks;
+        p.slots[at + t] = in ? (id[u] << p.bs_shift) + ((a + t) & (bs - 1)) : -1;
+        if (!in) set_error(p.err, WF_DEV_ERR_PAGE);
+      }
     }
   }
   for (int t = total + blockIdx.x * kPlanThreads + threadIdx.x; t < p.cap; t += gridDim.x * kPlanThreads) p.slots[t] = -1;
@@ -448,19 +458,22 @@ struct ReorderParams {
   const int32_t *table_in, *len, *parent, *n_free;
   int32_t *table_out, *free_ids, *n_free_out;
   int stride, n_req, W;
-  int32_t *gone, *gone_n, *moves, *n_free_copy;  // scratch
+  int32_t *moves, *gone, *gone_n, *n_free_copy;  // scratch
   uint32_t *err;
 };
 constexpr int kReorderThreads = 256;
 
 // One CTA per request: its table columns (each by one thread, which reads the
 // column before it writes it), the ids that no beam holds any more in order,
-// and the copies of last blocks that the second kernel makes.
+// and the copies of last blocks that the second kernel makes.  MAXW: 4, 8 or
+// 16, the least that holds the beams; a column's comparisons grow with its
+// square.
+template <int MAXW>
 __global__ void __launch_bounds__(kReorderThreads) beam_tables_kernel(const ReorderParams p) {
   pdl_wait();
   pdl_launch_dependents();
-  const int W = p.W, req = blockIdx.x, tid = threadIdx.x;
-  __shared__ int par[WF_MAX_BEAMS], from[WF_MAX_BEAMS], over_s;
+  const int W = p.W, req = blockIdx.x, tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
+  __shared__ int par_s[MAXW], from_s[MAXW], spare[MAXW];
   __shared__ int wsum[kReorderThreads / 32];
   const int32_t *in = p.table_in + static_cast<size_t>(req) * W * p.stride;
   int32_t *out = p.table_out + static_cast<size_t>(req) * W * p.stride;
@@ -472,83 +485,67 @@ __global__ void __launch_bounds__(kReorderThreads) beam_tables_kernel(const Reor
     err |= WF_DEV_ERR_PAGE;
     len = len < 0 ? 0 : p.stride * bs;
   }
-  const int full = len / bs, rem = len % bs;
-  if (tid < W) {
-    int v = p.parent[static_cast<size_t>(req) * W + tid];
-    if (v < -1 || v >= W) err |= WF_DEV_ERR_PAGE, v = -1;
-    par[tid] = v;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    uint32_t has_child = 0, keeps = 0;
-    int over = 1;
-    for (int w = 0; w < W; ++w) {
-      const int v = par[w];
-      if (v < 0) continue;
-      over = 0;
-      if (!(has_child >> v & 1)) keeps |= 1u << w;
-      has_child |= 1u << v;
+  const int full = len >> p.pool.bs_shift, rem = len & (bs - 1), cols = full + (rem ? 1 : 0);
+  if (wp == 0) {
+    int v = -1;
+    if (lane < W) {
+      v = p.parent[static_cast<size_t>(req) * W + lane];
+      if (v < -1 || v >= W) err |= WF_DEV_ERR_PAGE, v = -1;
     }
-    // the k-th beam that keeps nothing takes the last block of the k-th without children
-    uint32_t dead = ~has_child & ((1u << W) - 1);
-    for (int w = 0; w < W; ++w) {
-      if (keeps >> w & 1) {
-        from[w] = par[w];
-      } else {
-        from[w] = __ffs(dead) - 1;
-        dead &= dead - 1;
+    // a parent's first child keeps its last block; the k-th other beam takes that of the k-th without children
+    const unsigned same = __match_any_sync(0xffffffffu, v);
+    const bool keeps = v >= 0 && (same & ((1u << lane) - 1)) == 0;
+    const unsigned parents = __reduce_or_sync(0xffffffffu, v >= 0 ? 1u << v : 0u), all = (1u << W) - 1;
+    const unsigned dead = ~parents & all, takers = __ballot_sync(0xffffffffu, lane < W && !keeps);
+    if (dead >> lane & 1) spare[__popc(dead & ((1u << lane) - 1))] = lane;
+    __syncwarp();
+    if (lane < W) {
+      const int from = keeps ? v : spare[__popc(takers & ((1u << lane) - 1))];
+      par_s[lane] = v, from_s[lane] = from;
+      int src = -1, dst = -1;
+      if (rem && v >= 0 && from != v) {
+        src = in[v * p.stride + full];
+        dst = in[from * p.stride + full];
+        if (src < 0 || src >= p.pool.n_blocks || dst < 0 || dst >= p.pool.n_blocks) err |= WF_DEV_ERR_PAGE, src = dst = -1;
       }
+      *reinterpret_cast<int4 *>(p.moves + (static_cast<size_t>(req) * W + lane) * 4) = make_int4(src, dst, (rem + 15) / 16, 0);
     }
-    over_s = over;
-    if (req == 0) *p.n_free_copy = *p.n_free;
+    if (req == 0 && lane == 0) *p.n_free_copy = *p.n_free;
   }
-  __syncthreads();
-  const bool over = over_s;
-  // copies: (source, destination) of each child that takes another beam's block
-  if (tid < W) {
-    int src = -1, dst = -1;
-    if (rem && par[tid] >= 0 && from[tid] != par[tid]) {
-      src = in[par[tid] * p.stride + full];
-      dst = in[from[tid] * p.stride + full];
-      if (src < 0 || src >= p.pool.n_blocks || dst < 0 || dst >= p.pool.n_blocks) err |= WF_DEV_ERR_PAGE, src = dst = -1;
-    }
-    int32_t *m = p.moves + (static_cast<size_t>(req) * W + tid) * 4;
-    m[0] = src, m[1] = dst, m[2] = (rem + 15) / 16, m[3] = 0;
+  __syncthreads();  // (the copies' entries are read before any is written)
+  int par[MAXW], from[MAXW];
+  bool over = true;
+#pragma unroll
+  for (int w = 0; w < MAXW; ++w) {
+    par[w] = w < W ? par_s[w] : -1, from[w] = w < W ? from_s[w] : -1;
+    over = over && par[w] < 0;
   }
-  __syncthreads();
   int base = 0;
-  const int cols = full + (rem ? 1 : 0);
   for (int c0 = 0; c0 < cols; c0 += kReorderThreads) {
     const int c = c0 + tid;
-    int old[WF_MAX_BEAMS], now[WF_MAX_BEAMS];
+    int old[MAXW], now[MAXW];
     uint32_t dead = 0;
     if (c < cols) {
 #pragma unroll
-      for (int w = 0; w < WF_MAX_BEAMS; ++w)
-        if (w < W) old[w] = in[static_cast<size_t>(w) * p.stride + c];
-      for (int w = 0; w < W; ++w) {
-        int id = -1;
+      for (int w = 0; w < MAXW; ++w) old[w] = w < W ? in[static_cast<size_t>(w) * p.stride + c] : -1;
+#pragma unroll
+      for (int w = 0; w < MAXW; ++w) {
         const int f = c < full ? par[w] : (over ? -1 : from[w]);
+        now[w] = -1;
 #pragma unroll
-        for (int q = 0; q < WF_MAX_BEAMS; ++q)
-          if (q == f) id = old[q];
-#pragma unroll
-        for (int q = 0; q < WF_MAX_BEAMS; ++q)
-          if (q == w) now[q] = id;
-        out[static_cast<size_t>(w) * p.stride + c] = id;
+        for (int q = 0; q < MAXW; ++q) now[w] = q == f ? old[q] : now[w];
+        if (w < W) out[static_cast<size_t>(w) * p.stride + c] = now[w];
       }
 #pragma unroll
-      for (int w = 0; w < WF_MAX_BEAMS; ++w) {
-        if (w >= W || old[w] < 0) continue;
-        bool held = false;
+      for (int w = 0; w < MAXW; ++w) {
+        bool held = old[w] < 0;
 #pragma unroll
-        for (int q = 0; q < WF_MAX_BEAMS; ++q)
-          if (q < W) held |= now[q] == old[w] || (q < w && old[q] == old[w]);
+        for (int q = 0; q < MAXW; ++q) held |= now[q] == old[w] || (q < w && old[q] == old[w]);
         if (!held) dead |= 1u << w;
       }
     }
-    int cnt = __popc(dead), scan = cnt;
-    const int lane = tid & 31, wp = tid >> 5;
+    const int cnt = __popc(dead);
+    int scan = cnt;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, scan, off);
@@ -557,13 +554,14 @@ __global__ void __launch_bounds__(kReorderThreads) beam_tables_kernel(const Reor
     if (lane == 31) wsum[wp] = scan;
     __syncthreads();
     int total = 0, before = 0;
+#pragma unroll
     for (int i = 0; i < kReorderThreads / 32; ++i) {
       if (i < wp) before += wsum[i];
       total += wsum[i];
     }
     int at = base + before + scan - cnt;
 #pragma unroll
-    for (int w = 0; w < WF_MAX_BEAMS; ++w)
+    for (int w = 0; w < MAXW; ++w)
       if (dead >> w & 1) gone[at++] = old[w];
     base += total;
     __syncthreads();
@@ -578,16 +576,26 @@ __global__ void __launch_bounds__(kReorderThreads) beam_moves_kernel(const Reord
   pdl_wait();
   pdl_launch_dependents();
   const int req = blockIdx.x / p.W;
-  const int32_t *m = p.moves + static_cast<size_t>(blockIdx.x) * 4;
-  if (m[0] >= 0) {
-    const int chunk = m[2] * (kKv4Rec / 16);  // 16-byte pieces of a slab that are in use
+  const int4 m = *reinterpret_cast<const int4 *>(p.moves + static_cast<size_t>(blockIdx.x) * 4);
+  if (m.x >= 0) {
+    const int chunk = m.z * (kKv4Rec / 16);  // 16-byte pieces of a slab that are in use
     const int slabs = p.pool.heads * p.pool.groups, per = (p.pool.bs >> 4) * (kKv4Rec / 16);
     unsigned char *layer = p.pool.base + static_cast<long long>(blockIdx.y) * p.layer_stride;
-    const uint4 *src = reinterpret_cast<const uint4 *>(layer + m[0] * p.block_bytes);
-    uint4 *dst = reinterpret_cast<uint4 *>(layer + m[1] * p.block_bytes);
-    for (int i = threadIdx.x; i < slabs * chunk; i += kReorderThreads) {
-      const int at = i / chunk * per + i % chunk;
-      dst[at] = src[at];
+    const uint4 *src = reinterpret_cast<const uint4 *>(layer + m.x * p.block_bytes);
+    uint4 *dst = reinterpret_cast<uint4 *>(layer + m.y * p.block_bytes);
+    constexpr int kAhead = 6;  // reads in flight
+    for (int i0 = threadIdx.x; i0 < slabs * chunk; i0 += kAhead * kReorderThreads) {
+      uint4 v[kAhead];
+      int at[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = min(i0 + u * kReorderThreads, slabs * chunk - 1), slab = i / chunk;
+        at[u] = slab * per + i - slab * chunk;
+        v[u] = src[at[u]];
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i0 + u * kReorderThreads < slabs * chunk) dst[at[u]] = v[u];
     }
   }
   if (blockIdx.y != 0 || blockIdx.x % p.W != 0) return;
@@ -710,8 +718,8 @@ wf_status wf_kv4_load(const wf_kv4_pool *pool, int32_t layer, const int32_t *d_s
                      &p, stream);
 }
 
-// scratch: freed ids [n_req][beams * stride], their counts [n_req], copies
-// [n_req * beams][4], the free count
+// scratch: copies [n_req * beams][4], freed ids [n_req][beams * stride], their
+// counts [n_req], the free count
 size_t wf_beam_reorder_scratch_bytes(int32_t n_req, int32_t beams, int32_t table_stride) {
   if (n_req <= 0 || beams <= 0 || beams > WF_MAX_BEAMS || table_stride <= 0) return 0;
   const size_t rows = static_cast<size_t>(n_req) * beams;
@@ -727,7 +735,7 @@ wf_status wf_beam_reorder(const wf_kv4_pool *pool, const int32_t *d_table_in, in
   const wf_status st = kv4_pool_check(pool, 0, &p.pool, &stride);
   if (st != WF_OK) return st;
   if (!d_table_in || !d_table_out || !d_len || !d_parent || !d_free || !d_n_free || !d_n_free_out || !d_scratch || n_req <= 0 ||
-      beams <= 0 || table_stride <= 0 || (reinterpret_cast<uintptr_t>(d_scratch) & 3))
+      beams <= 0 || table_stride <= 0 || !aligned16(d_scratch))
     return WF_ERR_INVALID;
   if (beams > WF_MAX_BEAMS || pool->n_layers > 65535) return WF_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(table_stride) * pool->block_size > INT32_MAX || static_cast<int64_t>(n_req) * beams > INT32_MAX)
@@ -740,14 +748,17 @@ wf_status wf_beam_reorder(const wf_kv4_pool *pool, const int32_t *d_table_in, in
   p.table_in = d_table_in, p.table_out = d_table_out, p.stride = table_stride;
   p.len = d_len, p.parent = d_parent, p.n_req = n_req, p.W = beams;
   p.free_ids = d_free, p.n_free = d_n_free, p.n_free_out = d_n_free_out;
-  p.gone = static_cast<int32_t *>(d_scratch);
+  p.moves = static_cast<int32_t *>(d_scratch);
+  p.gone = p.moves + rows * 4;
   p.gone_n = p.gone + rows * table_stride;
-  p.moves = p.gone_n + n_req;
-  p.n_free_copy = p.moves + rows * 4;
+  p.n_free_copy = p.gone_n + n_req;
   p.err = d_err;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   void *args[] = {&p};
-  if (launch_pdl(reinterpret_cast<const void *>(beam_tables_kernel), n_req, kReorderThreads, 0, args, s) != cudaSuccess ||
+  const void *tables = beams <= 4   ? reinterpret_cast<const void *>(beam_tables_kernel<4>)
+                       : beams <= 8 ? reinterpret_cast<const void *>(beam_tables_kernel<8>)
+                                    : reinterpret_cast<const void *>(beam_tables_kernel<16>);
+  if (launch_pdl(tables, n_req, kReorderThreads, 0, args, s) != cudaSuccess ||
       launch_pdl(reinterpret_cast<const void *>(beam_moves_kernel), dim3(static_cast<unsigned>(rows), p.n_layers), kReorderThreads, 0,
                  args, s) != cudaSuccess)
     return WF_ERR_CUDA;
