@@ -59,11 +59,6 @@ __device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
                                           : __shfl_sync(0xffffffffu, static_cast<uint32_t>(k), __ffs(have) - 1);
   return static_cast<unsigned long long>(hi) << 32 | lo;
 }
-__device__ __forceinline__ float warp_max(float v) {
-  float m;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
-  return m;
-}
 // Sorts a warp's values, largest in lane 0: a bitonic network.
 __device__ __forceinline__ float warp_sort(float v, int lane) {
 #pragma unroll

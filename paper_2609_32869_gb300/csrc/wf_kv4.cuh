@@ -132,6 +132,13 @@ __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t m
   return d;
 }
 
+// The largest of a warp's values (no NaN, unless all are).
+__device__ __forceinline__ float warp_max(float v) {
+  float m;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+  return m;
+}
+
 template <typename T>
 struct Kv4Type;
 template <>

@@ -5,8 +5,20 @@
 // rank-one terms in fp32:
 //   q . k_j        = sum_g  s_jg (q_g . (c_jg - 8)) + z_jg sum(q_g)
 //   sum_j p_j v_jg = sum_j (p_j s_jg) (c_jg - 8)    + sum_j p_j z_jg
-// The codes enter mma.sync as exact 16-bit integers (a nibble ORed into the
-// mantissa of 128 or 1024, less that constant and 8); only p_j s_jg is rounded.
+// The codes enter mma.sync (m16n8k16, fp32 sums) as exact small integers in the
+// cache's 16-bit type.
+//   bf16: a nibble in the low mantissa bits of 128.  Keys keep the 128 + 8, which
+//   go into z (a few dozen units on a sum of 64 products in fp32); p_j s_jg is
+//   rounded to bf16, whose range holds any scale.
+//   fp16: a nibble where it lies, in bits 0 to 3 under 1024 or 4 to 7 under 64, so
+//   that a word of eight takes one shift.  Odd nibbles of keys keep their 64 + 8,
+//   which the sums start without.  p_j s_jg is rounded to fp16, its 11 bits
+//   relative to a power of two that follows the largest s of each 32 positions:
+//   below 2^-20 of that s bits are lost, below 2^-31 all of it.  Steps with
+//   positions that are not seen round to the sum of two bf16 instead.
+// (Keys and weights in fp16 for bf16 caches too, rows of queries scaled into its
+// range: 96 requests x 9 rows took 78 us instead of 71, the row scaling and its
+// registers costing more than the shifts.)
 //
 // The positions are the M side of both products (A operand: 16 positions of
 // keys, then 16 dims of values), the query rows the N side in tiles of 8, so
@@ -63,33 +75,35 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Nibbles i and i + 4 of w as a pair of 16-bit floats kBias + c.
-template <typename T>
-struct Codes;
-template <>
-struct Codes<__nv_bfloat16> {
-  static constexpr float kBias = 128.f;
-  template <int I>
-  static __device__ __forceinline__ uint32_t biased(uint32_t w) {
-    return and_or(w >> (4 * I), 0x000f000fu, 0x43004300u);
-  }
-  template <int I>
-  static __device__ __forceinline__ uint32_t exact(uint32_t w) {  // c - 8
-    const uint32_t u = biased<I>(w), eight = 0x43084308u;         // 136
-    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&eight));
-    return *reinterpret_cast<const uint32_t *>(&v);
-  }
-};
-template <>
-struct Codes<__half> {
-  static constexpr float kBias = 0.f;
-  template <int I>
-  static __device__ __forceinline__ uint32_t biased(uint32_t w) {  // 1024 + c, less 1024
-    const uint32_t u = and_or(w >> (4 * I), 0x000f000fu, 0x64006400u), bias = 0x64006400u;
-    const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&bias));
-    return *reinterpret_cast<const uint32_t *>(&v);
-  }
-};
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t u, uint32_t v) {
+  const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&v));
+  return *reinterpret_cast<const uint32_t *>(&d);
+}
+// Nibble I of each half of w as a pair of fp16 c - 8.
+template <int I>
+__device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
+  const uint32_t u = I < 2 ? w : w >> 8;
+  return I % 2 ? sub_f16x2(and_or(u, 0x00f000f0u, 0x54005400u), 0x54805480u)   // 64 + c, 72
+               : sub_f16x2(and_or(u, 0x000f000fu, 0x64006400u), 0x64086408u);  // 1024 + c, 1032
+}
+template <int I>
+__device__ __forceinline__ uint32_t key_codes(uint32_t w, __half) {
+  return I % 2 ? and_or(I < 2 ? w : w >> 8, 0x00f000f0u, 0x54005400u) : codes_f16<I>(w);
+}
+template <int I>
+__device__ __forceinline__ uint32_t key_codes(uint32_t w, __nv_bfloat16) {
+  return and_or(w >> (4 * I), 0x000f000fu, 0x43004300u);
+}
+template <int I>
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t w) {
+  const uint32_t u = and_or(w >> (4 * I), 0x000f000fu, 0x43004300u), eight = 0x43084308u;  // 128 + c, 136
+  const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&eight));
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t pack_f16(float2 v) {
+  const __half2 h = __floats2half2_rn(v.x, v.y);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
 
 __device__ __forceinline__ void bulk_load(void *smem_dst, const void *src, uint32_t bytes, uint64_t *bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(smem_dst)),
@@ -127,7 +141,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
   using X = Kv4Type<T>;
   using S = AtShape<G, NT>;
   constexpr int kRows = S::kRows, kStages = S::kStages, kSub = S::kSub;
-  constexpr bool kSplitP = std::is_same<T, __half>::value;  // see P below
+  constexpr bool kF16 = std::is_same<T, __half>::value;
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
   uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kBarOff) + warp * kStages;
@@ -181,9 +195,10 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
 #pragma unroll 1
   for (int i = 0; i < kStages && i < steps; ++i) issue();
 
-  // queries as B operands, and their sums
+  // Queries as B operands.  Of rows 2t and 2t + 1: sums over a group and what the
+  // odd codes' bias adds (fp16).
   uint32_t qb[NT][G][4][2];
-  float qs[NT][G][2];
+  float2 qs[NT][G], start[NT][G];
   int lim[NT][2], least = INT_MAX;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -198,14 +213,18 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
         const uint4 a = src[0], b = src[1];
         w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
       }
-      float sum = 0.f;
+      float even = 0.f, odd = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += X::lo(w[i]) + X::hi(w[i]);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      // this lane's scores are of rows 2t and 2t + 1
-      qs[n][g][0] = __shfl_sync(0xffffffffu, sum, t * 8);
-      qs[n][g][1] = __shfl_sync(0xffffffffu, sum, t * 8 + 4);
+      for (int i = 0; i < 8; ++i) even += X::lo(w[i]), odd += X::hi(w[i]);
+      even += odd, odd *= -72.f;
+#pragma unroll
+      for (int off = 1; off < 4; off <<= 1) {
+        even += __shfl_xor_sync(0xffffffffu, even, off);
+        if (kF16) odd += __shfl_xor_sync(0xffffffffu, odd, off);
+      }
+      qs[n][g] = make_float2(__shfl_sync(0xffffffffu, even, t * 8), __shfl_sync(0xffffffffu, even, t * 8 + 4));
+      start[n][g] = make_float2(0.f, 0.f);
+      if (kF16) start[n][g] = make_float2(__shfl_sync(0xffffffffu, odd, t * 8), __shfl_sync(0xffffffffu, odd, t * 8 + 4));
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -223,50 +242,60 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
   least = min(least, __shfl_xor_sync(0xffffffffu, least, 1));
   least = min(least, __shfl_xor_sync(0xffffffffu, least, 2));
 
-  float o[NT][G][4][4] = {}, zacc[NT][G][2] = {};
-  float2 l[NT], m[NT];  // of rows 2t and 2t + 1; m: what the weights are relative to
+  float o[NT][G][4][4] = {};  // in units of 1 / so
+  float so = kF16 ? 0.f : 1.f;  // fp16: a power of two near 1 / the largest value scale of the last steps; 0: none yet
+  const float c = p.scale * 1.4426950408889634f;  // base-2 softmax
+  float2 zacc[NT][G] = {}, l[NT], m[NT];  // of rows 2t and 2t + 1; m: the power of two that the weights are relative to
 #pragma unroll
   for (int n = 0; n < NT; ++n) l[n] = make_float2(0.f, 0.f), m[n] = make_float2(-INFINITY, -INFINITY);
-  const float c = p.scale * 1.4426950408889634f;  // base-2 softmax
 
   // kSub tiles of 16 positions from k0; `edge`: some are not seen by some row, or are not there
   auto step = [&](const unsigned char *buf, int k0, uint32_t there, auto edge_c) {
     constexpr bool edge = decltype(edge_c)::value;
     float2 x[kSub][NT][2];  // [16 positions][rows][position r, r + 8] (row 2t, row 2t + 1)
     uint2 szv[kSub][G];
-    float mx[NT][2];
+    float mx[NT][2], top_s = 0.f;
 #pragma unroll
     for (int n = 0; n < NT; ++n) mx[n][0] = mx[n][1] = -INFINITY;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       uint2 w0[kSub], w1[kSub];
-      float acc[kSub][NT][4] = {};
+      float acc[kSub][NT][4];
 #pragma unroll
       for (int i = 0; i < kSub; ++i) {
         const unsigned char *rg = buf + (g * 4 + i) * kKv4Rec;
         w0[i] = *reinterpret_cast<const uint2 *>(rg + r * 32 + t * 8);
         w1[i] = *reinterpret_cast<const uint2 *>(rg + (r + 8) * 32 + t * 8);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[i][n][0] = acc[i][n][2] = start[n][g].x, acc[i][n][1] = acc[i][n][3] = start[n][g].y;
       }
       // tile by tile within a step of 16 dims: the chains of sums interleave
-#define WF_KSTEP(K)                                                                                             \
-  _Pragma("unroll") for (int i = 0; i < kSub; ++i) {                                                            \
-    const uint32_t a[4] = {Codes<T>::template biased<K>(w0[i].x), Codes<T>::template biased<K>(w1[i].x),        \
-                           Codes<T>::template biased<K>(w0[i].y), Codes<T>::template biased<K>(w1[i].y)};       \
-    _Pragma("unroll") for (int n = 0; n < NT; ++n) mma16(acc[i][n], a, qb[n][g][K][0], qb[n][g][K][1], T()); \
+#define WF_KSTEP(K)                                                                                              \
+  _Pragma("unroll") for (int i = 0; i < kSub; ++i) {                                                             \
+    const uint32_t a[4] = {key_codes<K>(w0[i].x, T()), key_codes<K>(w1[i].x, T()), key_codes<K>(w0[i].y, T()),                    \
+                           key_codes<K>(w1[i].y, T())};                                                            \
+    _Pragma("unroll") for (int n = 0; n < NT; ++n) mma16(acc[i][n], a, qb[n][g][K][0], qb[n][g][K][1], T());  \
   }
       WF_KSTEP(0) WF_KSTEP(1) WF_KSTEP(2) WF_KSTEP(3)
 #undef WF_KSTEP
 #pragma unroll
       for (int i = 0; i < kSub; ++i) {
         const uint4 sz = *reinterpret_cast<const uint4 *>(buf + (g * 4 + i) * kKv4Rec + kKv4ScaleOff + r * 16);
-        // the codes' bias and 8 go into z: a few dozen units on a sum of 64 products in fp32
         const float s0 = X::lo(sz.x) * c, s1 = X::lo(sz.y) * c;
-        const float z0 = fmaf(X::hi(sz.x), c, -(Codes<T>::kBias + 8.f) * s0), z1 = fmaf(X::hi(sz.y), c, -(Codes<T>::kBias + 8.f) * s1);
+        float z0 = X::hi(sz.x) * c, z1 = X::hi(sz.y) * c;
+        if (!kF16) z0 = fmaf(-136.f, s0, z0), z1 = fmaf(-136.f, s1, z1);
         szv[i][g] = make_uint2(sz.z, sz.w);
+        if (kF16 && edge) {  // what lies past the sequence may hold anything
+          const bool here = there >> i & 1;
+          if (here && k0 + i * 16 + r < seen) top_s = fmaxf(top_s, X::lo(sz.z));
+          if (here && k0 + i * 16 + r + 8 < seen) top_s = fmaxf(top_s, X::lo(sz.w));
+        } else if (kF16) {
+          top_s = max3(top_s, X::lo(sz.z), X::lo(sz.w));
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const float2 a = make_float2(fmaf(s0, acc[i][n][0], z0 * qs[n][g][0]), fmaf(s0, acc[i][n][1], z0 * qs[n][g][1]));
-          const float2 b = make_float2(fmaf(s1, acc[i][n][2], z1 * qs[n][g][0]), fmaf(s1, acc[i][n][3], z1 * qs[n][g][1]));
+          const float2 a = make_float2(fmaf(s0, acc[i][n][0], z0 * qs[n][g].x), fmaf(s0, acc[i][n][1], z0 * qs[n][g].y));
+          const float2 b = make_float2(fmaf(s1, acc[i][n][2], z1 * qs[n][g].x), fmaf(s1, acc[i][n][3], z1 * qs[n][g].y));
           x[i][n][0] = g == 0 ? a : add2(x[i][n][0], a);
           x[i][n][1] = g == 0 ? b : add2(x[i][n][1], b);
         }
@@ -289,17 +318,29 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
       }
     }
     // The reference of the weights moves only when some row's maximum passes
-    // it by 2^8: the sums stay far inside fp32 and most steps rescale nothing.
+    // it by 2^8, that of the sums when the largest scale is 2^6 from it: the
+    // sums stay far inside fp32 and fp16 and most steps rescale nothing.
     bool moved = false;
+    if (kF16) {
+      top_s = warp_max(top_s);
+      moved = top_s > 0.f && !(top_s * so >= 0x1p-6f && top_s * so <= 0x1p6f);
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) moved |= mx[n][0] > m[n].x + 8.f || mx[n][1] > m[n].y + 8.f;
     if (__any_sync(0xffffffffu, moved)) {
+      float change = 1.f;
+      if (kF16) {
+        const int e = min(max(static_cast<int>(__float_as_uint(top_s) >> 23) - 127, -100), 100);
+        const float next_so = top_s > 0.f ? __uint_as_float(static_cast<uint32_t>(127 - e) << 23) : so;
+        change = so > 0.f ? next_so / so : 0.f;  // (of powers of two; no sums before the first)
+        so = next_so;
+      }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float next[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          next[e] = fmaxf(mx[n][e], e ? m[n].y : m[n].x);
+          next[e] = e ? fmaxf(mx[n][1], m[n].y) : fmaxf(mx[n][0], m[n].x);
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) next[e] = fmaxf(next[e], __shfl_xor_sync(0xffffffffu, next[e], off));
         }
@@ -308,23 +349,21 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
         l[n].x *= c0, l[n].y *= c1;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          zacc[n][g][0] *= c0, zacc[n][g][1] *= c1;
+          zacc[n][g].x *= c0, zacc[n][g].y *= c1;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) o[n][g][q][0] *= c0, o[n][g][q][1] *= c1, o[n][g][q][2] *= c0, o[n][g][q][3] *= c1;
+          for (int q = 0; q < 4; ++q)
+            o[n][g][q][0] *= c0 * change, o[n][g][q][1] *= c1 * change, o[n][g][q][2] *= c0 * change, o[n][g][q][3] *= c1 * change;
         }
         m[n] = make_float2(next[0], next[1]);
       }
     }
-    float2 minus[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) minus[n] = make_float2(-m[n].x, -m[n].y);
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const float2 y = add2(x[i][n][u], minus[n]);
+          const float2 y = add2(x[i][n][u], make_float2(-m[n].x, -m[n].y));
           float2 w = make_float2(ex2(y.x), ex2(y.y));
           if (edge) {
             if (x[i][n][u].x == -INFINITY) w.x = 0.f;
@@ -335,43 +374,60 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
         }
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        // P in bf16: its range holds any scale.  A cache in fp16 promises 11
-        // bits, so there P goes in as the sum of two.
-        uint32_t ph[NT][2], pl[NT][2];
+        const uint4 v = *reinterpret_cast<const uint4 *>(buf + (g * 4 + i) * kKv4Rec + kKv4ValOff + lane * 16);
+        if (kF16 && !edge) {
+          uint32_t ph[NT][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint32_t sz = u ? szv[i][g].y : szv[i][g].x;
-          const float sv = X::lo(sz), zv = X::hi(sz);
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t sz = u ? szv[i][g].y : szv[i][g].x;
+            const float sv = X::lo(sz) * so, zv = X::hi(sz);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const float2 w = x[i][n][u];
-            float a = w.x * sv, b = w.y * sv;
-            if (edge) {  // a weight of 0 stays 0 whatever the position holds
-              a = w.x == 0.f ? 0.f : a, b = w.y == 0.f ? 0.f : b;
-              zacc[n][g][0] += w.x == 0.f ? 0.f : w.x * zv;
-              zacc[n][g][1] += w.y == 0.f ? 0.f : w.y * zv;
-            } else {
-              zacc[n][g][0] = fmaf(w.x, zv, zacc[n][g][0]);
-              zacc[n][g][1] = fmaf(w.y, zv, zacc[n][g][1]);
+            for (int n = 0; n < NT; ++n) {
+              ph[n][u] = transpose8x8(pack_f16(mul2(x[i][n][u], make_float2(sv, sv))));
+              zacc[n][g] = fma2(x[i][n][u], make_float2(zv, zv), zacc[n][g]);
             }
-            const uint32_t h = pack_bf16(a, b);
-            ph[n][u] = transpose8x8(h);
-            if (kSplitP)
-              pl[n][u] = transpose8x8(pack_bf16(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u)));
           }
-        }
-        const uint4 w = *reinterpret_cast<const uint4 *>(buf + (g * 4 + i) * kKv4Rec + kKv4ValOff + lane * 16);
-#define WF_VSTEP(Q)                                                                                             \
-  {                                                                                                             \
-    using C = Codes<__nv_bfloat16>;                                                                             \
-    const uint32_t a[4] = {C::exact<Q>(w.x), C::exact<Q>(w.y), C::exact<Q>(w.z), C::exact<Q>(w.w)};             \
-    _Pragma("unroll") for (int n = 0; n < NT; ++n) {                                                            \
-      mma16(o[n][g][Q], a, ph[n][0], ph[n][1], __nv_bfloat16());                                                \
-      if (kSplitP) mma16(o[n][g][Q], a, pl[n][0], pl[n][1], __nv_bfloat16());                                   \
-    }                                                                                                           \
+#define WF_VSTEP(Q)                                                                                           \
+  {                                                                                                           \
+    const uint32_t a[4] = {codes_f16<Q>(v.x), codes_f16<Q>(v.y), codes_f16<Q>(v.z), codes_f16<Q>(v.w)};       \
+    _Pragma("unroll") for (int n = 0; n < NT; ++n) mma16(o[n][g][Q], a, ph[n][0], ph[n][1], __half());        \
   }
-        WF_VSTEP(0) WF_VSTEP(1) WF_VSTEP(2) WF_VSTEP(3)
+          WF_VSTEP(0) WF_VSTEP(1) WF_VSTEP(2) WF_VSTEP(3)
 #undef WF_VSTEP
+        } else {
+          uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t sz = u ? szv[i][g].y : szv[i][g].x;
+            const float sv = kF16 ? X::lo(sz) * so : X::lo(sz), zv = X::hi(sz);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const float2 w = x[i][n][u];
+              float a = w.x * sv, b = w.y * sv;
+              if (edge) {  // a weight of 0 stays 0 whatever the position holds
+                a = w.x == 0.f ? 0.f : a, b = w.y == 0.f ? 0.f : b;
+                zacc[n][g].x += w.x == 0.f ? 0.f : w.x * zv;
+                zacc[n][g].y += w.y == 0.f ? 0.f : w.y * zv;
+              } else {
+                zacc[n][g].x = fmaf(w.x, zv, zacc[n][g].x);
+                zacc[n][g].y = fmaf(w.y, zv, zacc[n][g].y);
+              }
+              const uint32_t h = pack_bf16(a, b);
+              ph[n][u] = transpose8x8(h);
+              if (kF16) pl[n][u] = transpose8x8(pack_bf16(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xffff0000u)));
+            }
+          }
+#define WF_VSTEP(Q)                                                                                           \
+  {                                                                                                           \
+    const uint32_t a[4] = {codes_bf16<Q>(v.x), codes_bf16<Q>(v.y), codes_bf16<Q>(v.z), codes_bf16<Q>(v.w)};   \
+    _Pragma("unroll") for (int n = 0; n < NT; ++n) {                                                          \
+      mma16(o[n][g][Q], a, ph[n][0], ph[n][1], __nv_bfloat16());                                              \
+      if (kF16) mma16(o[n][g][Q], a, pl[n][0], pl[n][1], __nv_bfloat16());                                    \
+    }                                                                                                         \
+  }
+          WF_VSTEP(0) WF_VSTEP(1) WF_VSTEP(2) WF_VSTEP(3)
+#undef WF_VSTEP
+        }
       }
     }
   };
@@ -401,6 +457,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
   }
 
   // the warp's results: sums over its 8 position lanes, rows 2t and 2t + 1
+  const float os = so > 0.f ? 1.f / so : 0.f;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -408,8 +465,8 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
       l[n].x += __shfl_xor_sync(0xffffffffu, l[n].x, off), l[n].y += __shfl_xor_sync(0xffffffffu, l[n].y, off);
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        zacc[n][g][0] += __shfl_xor_sync(0xffffffffu, zacc[n][g][0], off);
-        zacc[n][g][1] += __shfl_xor_sync(0xffffffffu, zacc[n][g][1], off);
+        zacc[n][g].x += __shfl_xor_sync(0xffffffffu, zacc[n][g].x, off);
+        zacc[n][g].y += __shfl_xor_sync(0xffffffffu, zacc[n][g].y, off);
       }
     }
   }
@@ -426,15 +483,16 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
       for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          sm_o[row * kLd + g * 64 + r * 8 + q] = o[n][g][q][e] + zacc[n][g][e];
-          sm_o[row * kLd + g * 64 + r * 8 + 4 + q] = o[n][g][q][e + 2] + zacc[n][g][e];
+          const float z = e ? zacc[n][g].y : zacc[n][g].x;
+          sm_o[row * kLd + g * 64 + r * 8 + q] = fmaf(o[n][g][q][e], os, z);
+          sm_o[row * kLd + g * 64 + r * 8 + 4 + q] = fmaf(o[n][g][q][e + 2], os, z);
         }
     }
   }
   __syncthreads();
   // the warps join in order; each thread takes pairs of dims
   const bool whole = seen <= p.chunk;  // no other chunk has positions
-  const size_t unit = static_cast<size_t>(blockIdx.x) * gridDim.z + blockIdx.z;
+  const size_t unit_at = static_cast<size_t>(blockIdx.x) * gridDim.z + blockIdx.z;
   float *cl_m = sm_o + kAtWarps * kRows * kLd, *cl_l = cl_m + kRows, *cl_o = cl_l + kRows;  // for the cluster
   for (int i = threadIdx.x; i < kRows * G * 32; i += kAtThreads) {
     const int row = i / (G * 32), d = i % (G * 32) * 2;
@@ -458,7 +516,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
       *reinterpret_cast<float2 *>(cl_o + row * (G * 64) + d) = make_float2(a, b);
       if (d == 0) cl_m[row] = mm, cl_l[row] = ll;
     } else {
-      const size_t at = (unit * p.chunks + blockIdx.y) * kRows + row;
+      const size_t at = (unit_at * p.chunks + blockIdx.y) * kRows + row;
       *reinterpret_cast<float2 *>(p.part_o + at * (G * 64) + d) = make_float2(a, b);
       if (d == 0) p.part_ml[at] = make_float2(mm, ll);
     }
