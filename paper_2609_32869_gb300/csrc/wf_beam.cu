@@ -460,15 +460,17 @@ __global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32) beam_join_kernel(const 
 
 using namespace wf;
 
-// The kernels of a call.  The segments keep the L1 that the suppressed ids are
-// read through: with the largest shared-memory carveout 96 requests x 5 beams
-// took 38 us instead of 31.
+// The kernels of a call, with one carveout: an SM drains before it changes it.
+// Half is L1, which the suppressed ids are read through (with the largest
+// shared-memory carveout 96 requests x 5 beams took 38 us).
 template <typename T>
 static bool select_ready(const void **segment, const void **join) {
   *segment = reinterpret_cast<const void *>(beam_segment_kernel<T>), *join = reinterpret_cast<const void *>(beam_join_kernel<T>);
-  static const bool ok = [](const void *b) {
-    return cudaFuncSetAttribute(b, cudaFuncAttributeMaxDynamicSharedMemorySize, WF_MAX_BEAMS * kJoinAhead * 512) == cudaSuccess;
-  }(*join);
+  static const bool ok = [](const void *a, const void *b) {
+    return cudaFuncSetAttribute(b, cudaFuncAttributeMaxDynamicSharedMemorySize, WF_MAX_BEAMS * kJoinAhead * 512) == cudaSuccess &&
+           cudaFuncSetAttribute(a, cudaFuncAttributePreferredSharedMemoryCarveout, 50) == cudaSuccess &&
+           cudaFuncSetAttribute(b, cudaFuncAttributePreferredSharedMemoryCarveout, 50) == cudaSuccess;
+  }(*segment, *join);
   return ok;
 }
 constexpr int kSelMaxVocab = 1 << 24;
