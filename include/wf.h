@@ -431,8 +431,8 @@ wf_status wf_kv4_load(const wf_kv4_pool *pool, int32_t layer, const int32_t *d_s
  *   max_len a bound on d_len; longer sequences are cut to it
  *           (WF_DEV_ERR_CAPACITY)
  *   d_out   dtype [n_seq * rps][n_heads * head_dim]
- * Strides are in elements, multiples of 8, pointers 16-byte aligned.  A row
- * that sees nothing is zeros; a block id outside the pool is not read and its
+ * Strides are in elements, multiples of 8, pointers 16-byte aligned; d_out is
+ * not d_q.  A row that sees nothing is zeros; a block id outside the pool is not read and its
  * positions are not seen (WF_DEV_ERR_PAGE).  Scores, softmax and sums are
  * fp32; results do not depend on timing.  d_scratch (16-byte aligned) holds
  * wf_kv4_attention_scratch_bytes() bytes and belongs to the call until it is
@@ -460,7 +460,7 @@ size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_head
  *       and -inf
  *   d_fin_parent int32, d_fin_score fp32 [n_req][beams]  hypotheses that end:
  *       eos among the first `beams` ranks; past the last one -1 and -inf
- * eos < 0: none ends.  2 beams <= vocab <= 2^24.  d_score may be d_scores. */
+ * eos < 0: none ends.  2 beams <= vocab <= 2^22.  d_score may be d_scores. */
 wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const float *d_scores,
                          const uint8_t *d_suppress, int32_t n_req, int32_t beams, int32_t vocab,
                          int32_t eos, int32_t *d_token, int32_t *d_parent, float *d_score,

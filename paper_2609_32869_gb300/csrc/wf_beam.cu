@@ -473,7 +473,7 @@ static bool select_ready(const void **segment, const void **join) {
   }(*segment, *join);
   return ok;
 }
-constexpr int kSelMaxVocab = 1 << 24;
+constexpr int kSelMaxVocab = 1 << 22;  // its terms in units of 2^-40 stay below 2^63
 // Segments of a row: as many as the GPU's warps take at once (32 an SM).
 struct SelectPlan {
   int tiles, segments, groups;

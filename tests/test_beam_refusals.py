@@ -85,7 +85,8 @@ def test_plan(kw, want):
 @pytest.mark.parametrize("kw,want", [
     (dict(logits=None), 1), (dict(scores=None), 1), (dict(token=None), 1), (dict(n=0), 1), (dict(beams=0), 1), (dict(ld=999), 1),
     (dict(scratch=None), 1), (dict(scratch=A + 4), 1), (dict(dtype=3), B.WF_ERR_UNSUPPORTED), (dict(dtype=-1), B.WF_ERR_UNSUPPORTED),
-    (dict(beams=17), B.WF_ERR_UNSUPPORTED), (dict(vocab=9), B.WF_ERR_UNSUPPORTED), (dict(scratch_bytes=100), B.WF_ERR_CAPACITY)])
+    (dict(beams=17), B.WF_ERR_UNSUPPORTED), (dict(vocab=9), B.WF_ERR_UNSUPPORTED),
+    (dict(vocab=(1 << 22) + 1, ld=1 << 23), B.WF_ERR_UNSUPPORTED), (dict(logits=A + 2), 1), (dict(scratch_bytes=100), B.WF_ERR_CAPACITY)])
 def test_select(kw, want):
     assert _status(_select, **kw) == want
 
