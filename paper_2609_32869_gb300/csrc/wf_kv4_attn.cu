@@ -547,45 +547,72 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
   cluster_sync();  // no CTA leaves while another reads it
 }
 
-// Joins the chunks of a row group in order: one warp per row, whose lanes
-// hold 2 G dims each.
+// Joins a row's chunks in order: a CTA per row, each of whose warps takes a
+// quarter of the chunks, eight at a time, and whose lanes hold 2 G dims each.
+// A chunk that the row sees nothing of holds zeros.
 template <typename T, int G, int NT>
 __global__ void __launch_bounds__(kAtThreads) kv4_join_kernel(const Kv4AttnParams p) {
   using X = Kv4Type<T>;
-  constexpr int kRows = NT * 8;
+  constexpr int kRows = NT * 8, kAhead = 8;
+  __shared__ float2 part[kAtWarps][G][32];
+  __shared__ float2 part_ml[kAtWarps];
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int head = blockIdx.x % p.pool.heads, seq = blockIdx.x / p.pool.heads;
-  const int row0 = blockIdx.y * kRows, rows = p.rps * p.group;
+  const int group = blockIdx.y, row = blockIdx.z, row0 = group * kRows, rows = p.rps * p.group;
+  if (row0 + row >= rows) return;
   const int seen = row_limit(p, min(row0 + kRows, rows) - 1, clamp_len(p, p.len[seq]));
   if (seen <= p.chunk) return;
-  const int chunks = (seen + p.chunk - 1) / p.chunk;
-  const size_t task = (static_cast<size_t>(blockIdx.x) * gridDim.y + blockIdx.y) * p.chunks;
-  for (int row = threadIdx.x >> 5; row < kRows && row0 + row < rows; row += kAtWarps) {
-    float mm = -INFINITY;
-    for (int k = lane; k < chunks; k += 32) mm = fmaxf(mm, p.part_ml[(task + k) * kRows + row].x);
+  const int chunks = (seen + p.chunk - 1) / p.chunk, per = (chunks + kAtWarps - 1) / kAtWarps;
+  const size_t task = (static_cast<size_t>(blockIdx.x) * p.row_groups + group) * p.chunks;
+  const int last = min(chunks, (warp + 1) * per);
+  float m = -INFINITY, l = 0.f;
+  float2 o[G] = {};
+  for (int k = warp * per; k < last; k += kAhead) {
+    float2 ml[kAhead], v[kAhead][G];
 #pragma unroll
-    for (int off = 16; off; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
-    float ll = 0.f, a[G] = {}, b[G] = {};
-    for (int k = 0; k < chunks; ++k) {
-      const size_t at = (task + k) * kRows + row;
-      const float2 ml = p.part_ml[at];
-      const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm);
-      ll += f * ml.y;
+    for (int i = 0; i < kAhead; ++i) {
+      const size_t at = (task + k + i) * kRows + row;
+      const bool has = k + i < last;
+      ml[i] = has ? p.part_ml[at] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const float2 v = *reinterpret_cast<const float2 *>(p.part_o + at * (G * 64) + g * 64 + lane * 2);
-        // a chunk that the row sees nothing of holds zeros
-        a[g] += f * v.x, b[g] += f * v.y;
-      }
+      for (int g = 0; g < G; ++g) v[i][g] = !has ? make_float2(0.f, 0.f) : *reinterpret_cast<const float2 *>(p.part_o + at * (G * 64) + g * 64 + lane * 2);
     }
-    const float inv = ll == 0.f ? 0.f : 1.f / ll;
-    const int j = p.row_of(row0 + row), h = head * p.group + row0 + row - j * p.group;
-    T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + lane * 2;
+    float top = m;
 #pragma unroll
-    for (int g = 0; g < G; ++g) *reinterpret_cast<uint32_t *>(dst + g * 64) = X::pack(a[g] * inv, b[g] * inv);
+    for (int i = 0; i < kAhead; ++i) top = fmaxf(top, ml[i].x);
+    const float keep = m == -INFINITY ? 0.f : ex2(m - top);
+    m = top, l *= keep;
+#pragma unroll
+    for (int g = 0; g < G; ++g) o[g].x *= keep, o[g].y *= keep;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float f = ml[i].x == -INFINITY ? 0.f : ex2(ml[i].x - m);
+      l += f * ml[i].y;
+#pragma unroll
+      for (int g = 0; g < G; ++g) o[g].x += f * v[i][g].x, o[g].y += f * v[i][g].y;
+    }
   }
+  if (lane == 0) part_ml[warp] = make_float2(m, l);
+#pragma unroll
+  for (int g = 0; g < G; ++g) part[warp][g][lane] = o[g];
+  __syncthreads();
+  if (warp >= G) return;
+  float mm = part_ml[0].x, ll = 0.f;
+#pragma unroll
+  for (int w = 1; w < kAtWarps; ++w) mm = fmaxf(mm, part_ml[w].x);
+  float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int w = 0; w < kAtWarps; ++w) {
+    const float f = part_ml[w].x == -INFINITY ? 0.f : ex2(part_ml[w].x - mm);
+    ll += f * part_ml[w].y;
+    sum.x += f * part[w][warp][lane].x, sum.y += f * part[w][warp][lane].y;
+  }
+  const float inv = ll == 0.f ? 0.f : 1.f / ll;
+  const int j = p.row_of(row0 + row), h = head * p.group + row0 + row - j * p.group;
+  T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + warp * 64 + lane * 2;
+  *reinterpret_cast<uint32_t *>(dst) = X::pack(sum.x * inv, sum.y * inv);
 }
 
 }  // namespace wf
@@ -627,7 +654,7 @@ static cudaError_t launch(const Kv4AttnParams &p, cudaStream_t s) {
   cudaError_t e = launch_pdl(reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>), grid, kAtThreads, S::kSmem, args, s,
                              p.cluster ? p.chunks : 1);
   if (e == cudaSuccess && p.chunks > 1 && !p.cluster)
-    e = launch_pdl(reinterpret_cast<const void *>(kv4_join_kernel<T, G, NT>), dim3(grid.x, p.row_groups), kAtThreads, 0, args, s);
+    e = launch_pdl(reinterpret_cast<const void *>(kv4_join_kernel<T, G, NT>), dim3(grid.x, p.row_groups, NT * 8), kAtThreads, 0, args, s);
   return e;
 }
 
