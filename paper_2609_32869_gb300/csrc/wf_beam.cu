@@ -33,8 +33,10 @@ struct SelectParams {
 };
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kSelBlocks = 3;  // CTAs of an SM
 constexpr int kSelPer = 32;             // logits of a lane and tile
 constexpr int kSelTile = 32 * kSelPer;  // of a warp's step
+constexpr int kSelTiles = 8;            // of a segment, at most
 constexpr int kSelKeep = 128;           // candidates of a row that the join holds
 
 // (value descending, index ascending) as one descending unsigned key; 0 is
@@ -135,63 +137,84 @@ struct RowOf {
   }
 };
 
-// A warp walks `tiles` tiles of 1024 logits of a row; no warp waits for
-// another.  The sum adds a tile's 32 terms a lane in fp32 and the tiles with
+__device__ __forceinline__ void copy16_async(void *smem_dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem_dst)), "l"(src) : "memory");
+}
+
+// A CTA has a segment of up to 8 tiles of 1024 logits of eight rows, a warp
+// each; its suppressed ids are read once for the eight.  A tile's logits go to
+// shared memory and from there to registers, which frees their place for the
+// next tile's while this one is worked on: bound by HBM, and by the ends of the
+// one wave of CTAs.  With the joining kernel after it 96 requests x 5 beams x
+// 51866 fp32 take 28.8 us, 3.5 TB/s (tiles straight to registers and a mask per
+// warp 30.8; four CTAs an SM, which spill, 31.3).  The sum adds a tile's 32 terms a lane in fp32 and the tiles with
 // the rounding carried along; lanes and segments add in fixed point (2^-40),
 // without order.  A NaN is never the larger of a comparison, which keeps it out
 // of the maxima and the candidates; only the sum has to look for it.
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads, 4) beam_segment_kernel(const SelectParams p) {
+__global__ void __launch_bounds__(kSelThreads, kSelBlocks) beam_segment_kernel(const SelectParams p) {
   using L = Logits<T>;
   constexpr int kVec = L::kVec, kVecs = kSelPer / kVec;
-  __shared__ __align__(16) unsigned char masks[kSelWarps][kSelTile + 32];
+  constexpr int kMask = kSelTiles * kSelTile + 48;         // 16 bytes before a segment, for skew, and to the next multiple of 16
+  __shared__ uint4 ahead[kSelWarps][kVecs][32];            // the next tile: a lane's own vectors, which no other lane reads
+  __shared__ __align__(16) unsigned char mask[kMask + 16]; // the segment's suppressed ids, for all the CTA's rows
+  __shared__ uint32_t flags[kMask / 512 + 4];              // bit i of word k: some id of mask's 16 from 512 k + 16 i on
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long unit = static_cast<long long>(blockIdx.x) * kSelWarps + warp, row = unit / p.segments;
-  const int segment = static_cast<int>(unit - row * p.segments);
-  if (row >= static_cast<long long>(p.n_req) * p.W) return;
-  unsigned char *mask = masks[warp];
+  const int segment = blockIdx.x % p.segments;
+  const long long row = static_cast<long long>(blockIdx.x / p.segments) * kSelWarps + warp, unit = row * p.segments + segment;
+  const bool live = row < static_cast<long long>(p.n_req) * p.W;
   pdl_wait();
-  const RowOf<T> in(p, row);
-  const int start = segment * p.tiles * kSelTile - in.skew, end = min(start + p.tiles * kSelTile, p.V);
+  const RowOf<T> in(p, live ? row : 0);
+  const int base = segment * p.tiles * kSelTile, start = base - in.skew, end = live ? min(start + p.tiles * kSelTile, p.V) : start;
   float *group = p.group_max + row * p.groups + segment * p.tiles * kVecs;
   float m = -INFINITY, sum = 0.f, carry = 0.f;
+  uint4 *next = &ahead[warp][0][lane];
+  const auto request = [&](int first) {
+    if (first >= 0 && first + kSelTile <= p.V) {
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) copy16_async(next + v * 32, in.src + first + (v * 32 + lane) * kVec);
+    } else {
+#pragma unroll 1
+      for (int v = 0; v < kVecs; ++v) {
+        const int id = first + (v * 32 + lane) * kVec;
+        if (id >= 0 && id + kVec <= p.V)
+          copy16_async(next + v * 32, in.src + id);
+        else
+          next[v * 32] = edge_vector<T>(in.src, id, p.V);
+      }
+    }
+  };
+  if (start < end) request(start);
+  int mask_from = 0;  // id of mask's first byte; the id's address is a multiple of 16
+  if (p.suppress) {
+    mask_from = base - 16 - static_cast<int>((reinterpret_cast<uintptr_t>(p.suppress) + base) & 15);
+    for (int i = threadIdx.x; i < (kMask / 512 + 1) * 32; i += kSelThreads) {  // whole warps: their ballots are the flags
+      const int id = mask_from + i * 16;
+      uint4 w = {};
+      if (i * 16 < p.tiles * kSelTile + 48) {
+        if (id >= 0 && id + 16 <= p.V)
+          w = *reinterpret_cast<const uint4 *>(p.suppress + id);
+        else if (id + 16 > 0 && id < p.V)
+          w = edge_bytes(p.suppress, id, p.V);
+        *reinterpret_cast<uint4 *>(mask + i * 16) = w;
+      }
+      const uint32_t some = __ballot_sync(0xffffffffu, (w.x | w.y | w.z | w.w) != 0);
+      if (lane == 0) flags[i >> 5] = some;
+    }
+    __syncthreads();
+  }
   for (int first = start; first < end; first += kSelTile, group += kVecs) {
     float x[kSelPer];
-    {
-      uint4 raw[kVecs];
-      if (first >= 0 && first + kSelTile <= p.V) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) raw[v] = *reinterpret_cast<const uint4 *>(in.src + first + (v * 32 + lane) * kVec);
-      } else {
-#pragma unroll
-        for (int v = 0; v < kVecs; ++v) raw[v] = in.vector(first + (v * 32 + lane) * kVec);
-      }
-#pragma unroll
-      for (int v = 0; v < kVecs; ++v) L::unpack(raw[v], x + v * kVec);
-    }
-    if (p.suppress) {  // the tile's bytes by 16, from the multiple of 16 before it; read back at the skew between the two
-      const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(p.suppress) + first) & 15), from = first - lead;
-      uint4 w[3] = {};
-#pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        const int id = from + (i * 32 + lane) * 16;
-        if (i == 2 && lane > 0) continue;
-        if (id >= 0 && id + 16 <= p.V) {
-          w[i] = *reinterpret_cast<const uint4 *>(p.suppress + id);
-        } else if (id + 16 > 0 && id < p.V) {
-          w[i] = edge_bytes(p.suppress, id, p.V);
-        }
-      }
-      const uint32_t some = w[0].x | w[0].y | w[0].z | w[0].w | w[1].x | w[1].y | w[1].z | w[1].w | w[2].x | w[2].y | w[2].z | w[2].w;
-      if (__any_sync(0xffffffffu, some != 0)) {
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-          if (i < 2 || lane == 0) *reinterpret_cast<uint4 *>(mask + (i * 32 + lane) * 16) = w[i];
-        __syncwarp();
+    for (int v = 0; v < kVecs; ++v) L::unpack(next[v * 32], x + v * kVec);
+    if (first + kSelTile < end) request(first + kSelTile);
+    if (p.suppress) {
+      const int from = first - mask_from;
+      if (flags[from >> 9] | flags[(from >> 9) + 1] | flags[(from >> 9) + 2]) {
 #pragma unroll
         for (int q = 0; q < kSelPer / 4; ++q) {
-          const int at = lead + ((q * 4 / kVec) * 32 + lane) * kVec + q * 4 % kVec;
+          const int at = from + ((q * 4 / kVec) * 32 + lane) * kVec + q * 4 % kVec;
           const uint32_t *word = reinterpret_cast<const uint32_t *>(mask) + (at >> 2);
           const uint32_t b = __funnelshift_r(word[0], word[1], (at & 3) * 8);
           if (!b) continue;
@@ -239,6 +262,7 @@ __global__ void __launch_bounds__(kSelThreads, 4) beam_segment_kernel(const Sele
     sum = t;
   }
   pdl_launch_dependents();  // not before: the join's CTAs would take the room of this kernel's
+  if (!live) return;
   // tiles of the last segment that lie past the row
   for (int i = static_cast<int>(group - p.group_max - row * p.groups) + lane; i < min((segment + 1) * p.tiles * kVecs, p.groups); i += 32)
     p.group_max[row * p.groups + i] = -INFINITY;
@@ -255,10 +279,6 @@ __device__ __forceinline__ void load_groups(const float *tops, int base, int gro
     const int i = base + u * 32 + lane;
     t[u] = i < groups ? tops[i] : -INFINITY;
   }
-}
-
-__device__ __forceinline__ void copy16_async(void *smem_dst, const void *src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem_dst)), "l"(src) : "memory");
 }
 
 // One CTA per request, two warps per beam: one picks the row's best logits,
@@ -461,28 +481,27 @@ __global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32) beam_join_kernel(const 
 using namespace wf;
 
 // The kernels of a call, with one carveout: an SM drains before it changes it.
-// Half is L1, which the suppressed ids are read through (with the largest
-// shared-memory carveout 96 requests x 5 beams took 38 us).
+constexpr int kSelCarve = 60;  // percent: three of the first kernel's CTAs
 template <typename T>
 static bool select_ready(const void **segment, const void **join) {
   *segment = reinterpret_cast<const void *>(beam_segment_kernel<T>), *join = reinterpret_cast<const void *>(beam_join_kernel<T>);
   static const bool ok = [](const void *a, const void *b) {
     return cudaFuncSetAttribute(b, cudaFuncAttributeMaxDynamicSharedMemorySize, WF_MAX_BEAMS * kJoinAhead * 512) == cudaSuccess &&
-           cudaFuncSetAttribute(a, cudaFuncAttributePreferredSharedMemoryCarveout, 50) == cudaSuccess &&
-           cudaFuncSetAttribute(b, cudaFuncAttributePreferredSharedMemoryCarveout, 50) == cudaSuccess;
+           cudaFuncSetAttribute(a, cudaFuncAttributePreferredSharedMemoryCarveout, kSelCarve) == cudaSuccess &&
+           cudaFuncSetAttribute(b, cudaFuncAttributePreferredSharedMemoryCarveout, kSelCarve) == cudaSuccess;
   }(*segment, *join);
   return ok;
 }
 constexpr int kSelMaxVocab = 1 << 22;  // its terms in units of 2^-40 stay below 2^63
-// Segments of a row: as many as the GPU's warps take at once (32 an SM).
+// Segments of a row: as many as make one wave of CTAs, or more of at most 8 tiles.
 struct SelectPlan {
   int tiles, segments, groups;
 };
 static SelectPlan select_plan(long long rows, int V, bool wide) {
   const int all = (V + 7 + kSelTile - 1) / kSelTile;  // 15 bytes of skew may push a row's end into another tile
   SelectPlan a;
-  const long long most = std::min<long long>(all, std::max<long long>(1, 152 * 32 / rows));
-  a.tiles = static_cast<int>((all + most - 1) / most);
+  const long long most = std::min<long long>(all, std::max<long long>(1, 152 * kSelBlocks / ((rows + kSelWarps - 1) / kSelWarps)));
+  a.tiles = static_cast<int>(std::min<long long>(kSelTiles, (all + most - 1) / most));
   a.segments = (all + a.tiles - 1) / a.tiles;
   a.groups = all * (wide ? 8 : 4);
   return a;
@@ -523,7 +542,7 @@ wf_status wf_beam_select(const void *d_logits, int32_t dtype, int64_t ld, const 
     return WF_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   void *args[] = {&p};
-  const long long grid = (rows * p.segments + kSelWarps - 1) / kSelWarps;
+  const long long grid = (rows + kSelWarps - 1) / kSelWarps * p.segments;
   if (grid > INT32_MAX) return WF_ERR_UNSUPPORTED;
   if (launch_pdl(fn, static_cast<unsigned>(grid), kSelThreads, 0, args, s) != cudaSuccess ||
       launch_pdl(join, n_req, beams * 64, static_cast<size_t>(beams) * kJoinAhead * 512, args, s) != cudaSuccess)
