@@ -384,8 +384,8 @@ typedef struct wf_kv4_pool {
 /* Bytes of one block in one layer; 0 for a shape that is not supported. */
 size_t wf_kv4_block_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_dim);
 
-/* Block tables and slot maps from request lengths.  Request i (0 <= i < n)
- * grows from d_old_len[i] to d_new_len[i] positions.  Its table row,
+/* Block tables and slot maps from request lengths.  Request i (0 <= i < n,
+ * n <= 65536) grows from d_old_len[i] to d_new_len[i] positions.  Its table row,
  * d_table + i * table_stride, names the blocks of its first
  * ceil(old / block_size) columns; the columns up to ceil(new / block_size) are
  * filled from the free list, a stack of *d_n_free ids in d_free (capacity

@@ -104,3 +104,7 @@ def test_sizes():
     assert B.wf_kv4_block_bytes(48, 20, 64) == 0 and B.wf_kv4_block_bytes(16, 0, 64) == 0 and B.wf_kv4_block_bytes(16, 1, 80) == 0
     assert B.wf_beam_select_scratch_bytes(0, 5, 1000) == 0 and B.wf_beam_select_scratch_bytes(2, 5, 1000) > 0
     assert B.wf_beam_reorder_scratch_bytes(1, 17, 4) == 0
+
+
+def test_plan_takes_65536_requests():
+    assert _status(_plan, n=(1 << 16) + 1) == B.WF_ERR_UNSUPPORTED

@@ -120,6 +120,28 @@ def test_page_plan_many(n, bs, most):
     assert left.item() == want[4] and err.item() == B.WF_DEV_ERR_CAPACITY * want[5][0]
 
 
+@pytest.mark.parametrize("n,share", [(300, 0.5), (1300, 0.9), (1300, 0.0), (5000, 0.3)])
+def test_page_plan_many_run_out(n, share):
+    """Bad requests among good ones, and a stack that holds a share of what all of them need."""
+    import torch
+    from paper_2609_32869_gb300 import binding as B
+    rng = np.random.default_rng(n)
+    new = rng.integers(0, 40, n)
+    old = np.where(rng.random(n) < 0.02, new + 1, 0)
+    bs, cols, cap = 16, 2, 40 * n
+    n_free = int(share * sum(-(-int(b) // bs) for a, b in zip(old, new) if b >= a and -(-int(b) // bs) <= cols))
+    blocks = n_free + 5
+    ids, table = rng.permutation(blocks), np.full((n, cols), -1)
+    want = ob.page_plan(list(old), list(new), bs, ids, n_free, table, cap, blocks)
+    t, slots = _i32(torch, table), torch.full((cap,), 77, dtype=torch.int32, device="cuda")
+    off, ln, left, err = _i32(torch, np.zeros(n + 1)), _i32(torch, np.zeros(n)), _err(torch), _err(torch)
+    B.wf_page_plan(_i32(torch, old), _i32(torch, new), n, bs, _i32(torch, ids), blocks, _i32(torch, [n_free]), t, cols, off,
+                   slots, cap, ln, left, err)
+    for got, w in zip((t, off, slots, ln), want):
+        np.testing.assert_array_equal(got.cpu().numpy(), np.asarray(w))
+    assert left.item() == want[4] and err.item() == B.WF_DEV_ERR_CAPACITY | B.WF_DEV_ERR_PAGE
+
+
 # -------------------------------------------------------------- store, load --
 @pytest.mark.parametrize("n,bs,heads,dim,dtype,pad", [
     (1, 16, 1, 64, "bf16", 0), (5, 16, 3, 64, "bf16", 64), (33, 32, 2, 128, "f16", 8), (64, 64, 6, 64, "f16", 0),
