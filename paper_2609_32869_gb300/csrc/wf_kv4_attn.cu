@@ -119,7 +119,7 @@ struct AtShape {
   static constexpr int kBlocks = G == 1 ? 6 - NT : 4 - NT;  // CTAs of an SM that the registers allow
   static constexpr int kStageBytes = 4 * G * kKv4Rec;  // 64 positions of a head
   static constexpr int kRingBytes = kAtWarps * kStages * kStageBytes;
-  static constexpr int kMergeBytes = kAtWarps * kRows * (G * 64 + 1 + 2) * 4 + kRows * (G * 64 + 2) * 4;
+  static constexpr int kMergeBytes = kAtWarps * kRows * (G * 64 + 4 + 2) * 4 + kRows * (G * 64 + 2) * 4;
   static constexpr int kBarOff = ((kRingBytes > kMergeBytes ? kRingBytes : kMergeBytes) + 15) / 16 * 16;
   static constexpr int kSmem = kBarOff + kAtWarps * kStages * 8;
 };
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
     }
   }
   __syncthreads();  // the ring is done with
-  constexpr int kLd = G * 64 + 1;
+  constexpr int kLd = G * 64 + 4;
   float *sm_m = reinterpret_cast<float *>(smem), *sm_l = sm_m + kAtWarps * kRows, *sm_o = sm_l + kAtWarps * kRows;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -482,43 +482,56 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int u = 0; u < 2; ++u) {
           const float z = e ? zacc[n][g].y : zacc[n][g].x;
-          sm_o[row * kLd + g * 64 + r * 8 + q] = fmaf(o[n][g][q][e], os, z);
-          sm_o[row * kLd + g * 64 + r * 8 + 4 + q] = fmaf(o[n][g][q][e + 2], os, z);
+          *reinterpret_cast<float4 *>(sm_o + row * kLd + g * 64 + r * 8 + u * 4) =
+              make_float4(fmaf(o[n][g][0][e + 2 * u], os, z), fmaf(o[n][g][1][e + 2 * u], os, z), fmaf(o[n][g][2][e + 2 * u], os, z),
+                          fmaf(o[n][g][3][e + 2 * u], os, z));
         }
     }
   }
   __syncthreads();
-  // the warps join in order; each thread takes pairs of dims
+  // the warps join in order; kAtThreads / kRows threads a row, by four dims
   const bool whole = seen <= p.chunk;  // no other chunk has positions
   const size_t unit_at = static_cast<size_t>(blockIdx.x) * gridDim.z + blockIdx.z;
   float *cl_m = sm_o + kAtWarps * kRows * kLd, *cl_l = cl_m + kRows, *cl_o = cl_l + kRows;  // for the cluster
-  for (int i = threadIdx.x; i < kRows * G * 32; i += kAtThreads) {
-    const int row = i / (G * 32), d = i % (G * 32) * 2;
-    if (row0 + row >= rows) break;
-    float mm = -INFINITY, ll = 0.f, a = 0.f, b = 0.f;
+  constexpr int kTeam = kAtThreads / kRows;
+  const int row = threadIdx.x / kTeam;
+  if (row0 + row < rows) {
+    float f[kAtWarps], mm = -INFINITY, ll = 0.f;
 #pragma unroll
     for (int w = 0; w < kAtWarps; ++w) mm = fmaxf(mm, sm_m[w * kRows + row]);
 #pragma unroll
     for (int w = 0; w < kAtWarps; ++w) {
-      const int at = w * kRows + row;
-      if (sm_m[at] == -INFINITY) continue;
-      const float f = ex2(sm_m[at] - mm);
-      ll += f * sm_l[at], a += f * sm_o[at * kLd + d], b += f * sm_o[at * kLd + d + 1];
+      const float at = sm_m[w * kRows + row];
+      f[w] = at == -INFINITY ? 0.f : ex2(at - mm);  // (a warp that saw nothing has zeros)
+      ll += f[w] * sm_l[w * kRows + row];
     }
-    if (whole && !p.cluster) {
-      const float inv = ll == 0.f ? 0.f : 1.f / ll;
-      const int j = p.row_of(row0 + row), h = head * p.group + row0 + row - j * p.group;
-      T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64) + d;
-      *reinterpret_cast<uint32_t *>(dst) = X::pack(a * inv, b * inv);
-    } else if (p.cluster) {
-      *reinterpret_cast<float2 *>(cl_o + row * (G * 64) + d) = make_float2(a, b);
-      if (d == 0) cl_m[row] = mm, cl_l[row] = ll;
-    } else {
-      const size_t at = (unit_at * p.chunks + blockIdx.y) * kRows + row;
-      *reinterpret_cast<float2 *>(p.part_o + at * (G * 64) + d) = make_float2(a, b);
-      if (d == 0) p.part_ml[at] = make_float2(mm, ll);
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+    const int j = p.row_of(row0 + row), h = head * p.group + row0 + row - j * p.group;
+    T *dst = static_cast<T *>(p.out) + (static_cast<long long>(seq) * p.rps + j) * p.out_stride + h * (G * 64);
+    const size_t part = (unit_at * p.chunks + blockIdx.y) * kRows + row;
+    if (p.cluster) {
+      if (threadIdx.x % kTeam == 0) cl_m[row] = mm, cl_l[row] = ll;
+    } else if (!whole) {
+      if (threadIdx.x % kTeam == 0) p.part_ml[part] = make_float2(mm, ll);
+    }
+#pragma unroll
+    for (int d = threadIdx.x % kTeam * 4; d < G * 64; d += kTeam * 4) {
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kAtWarps; ++w) {
+        const float4 u = *reinterpret_cast<const float4 *>(sm_o + (w * kRows + row) * kLd + d);
+        v.x = fmaf(f[w], u.x, v.x), v.y = fmaf(f[w], u.y, v.y), v.z = fmaf(f[w], u.z, v.z), v.w = fmaf(f[w], u.w, v.w);
+      }
+      if (p.cluster) {
+        *reinterpret_cast<float4 *>(cl_o + row * (G * 64) + d) = v;
+      } else if (whole) {
+        *reinterpret_cast<uint2 *>(dst + d) = make_uint2(X::pack(v.x * inv, v.y * inv), X::pack(v.z * inv, v.w * inv));
+      } else {
+        float2 *to = reinterpret_cast<float2 *>(p.part_o + part * (G * 64) + d);
+        to[0] = make_float2(v.x, v.y), to[1] = make_float2(v.z, v.w);
+      }
     }
   }
   if (!p.cluster) return;
