@@ -284,7 +284,8 @@ __device__ __forceinline__ void load_groups(const float *tops, int base, int gro
 // One CTA per request, two warps per beam: one picks the row's best logits,
 // one takes its maximum, sum and (in 64 bits) logarithm meanwhile.  Most of
 // its time is the latency of a few dependent reads, so each is issued at once:
-// the maxima into registers, the groups into shared memory.
+// the maxima into registers, the groups into shared memory.  About 5 us of one
+// request's 10 and 7 of 96 requests' 29.
 constexpr int kJoinGroups = 64;  // groups of a row that are looked through
 constexpr int kJoinAhead = 8;    // of them in shared memory at a time
 template <typename T>
