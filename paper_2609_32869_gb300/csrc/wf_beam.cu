@@ -61,6 +61,14 @@ __device__ __forceinline__ unsigned long long warp_max(unsigned long long k) {
                                           : __shfl_sync(0xffffffffu, static_cast<uint32_t>(k), __ffs(have) - 1);
   return static_cast<unsigned long long>(hi) << 32 | lo;
 }
+// floor(x 2^k) of x in [0, 2^(63 - k)), by shifts: the FP64 pipe takes a warp's
+// instruction in tens of clocks, and its conversions with it.
+__device__ __forceinline__ unsigned long long fixed_point(float x, int k) {
+  const uint32_t b = __float_as_uint(x), e = b >> 23;
+  const unsigned long long mant = (b & 0x7fffffu) | (e ? 0x800000u : 0u);
+  const int up = static_cast<int>(e ? e : 1u) - 150 + k;
+  return up >= 0 ? mant << up : up > -24 ? mant >> -up : 0;
+}
 // Sorts a warp's values, largest in lane 0: a bitonic network.
 __device__ __forceinline__ float warp_sort(float v, int lane) {
 #pragma unroll
@@ -79,6 +87,7 @@ template <>
 struct Logits<float> {
   using Half = __half;  // unused
   static constexpr int kVec = 4;
+  static __device__ __forceinline__ float one(const uint4 *v, int i) { return reinterpret_cast<const float *>(v)[i]; }
   static __device__ __forceinline__ void unpack(uint4 v, float *x) {
     x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
   }
@@ -87,6 +96,7 @@ template <typename T>
 struct Logits16 {
   using Half = T;
   static constexpr int kVec = 8;
+  static __device__ __forceinline__ float one(const uint4 *v, int i) { return Kv4Type<T>::lo(reinterpret_cast<const uint16_t *>(v)[i]); }
   static __device__ __forceinline__ void unpack(uint4 v, float *x) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -266,7 +276,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelBlocks) beam_segment_kernel(c
   // tiles of the last segment that lie past the row
   for (int i = static_cast<int>(group - p.group_max - row * p.groups) + lane; i < min((segment + 1) * p.tiles * kVecs, p.groups); i += 32)
     p.group_max[row * p.groups + i] = -INFINITY;
-  unsigned long long fixed = static_cast<unsigned long long>(static_cast<double>(sum) * 0x1p40);
+  unsigned long long fixed = fixed_point(sum, 40);
 #pragma unroll
   for (int off = 16; off; off >>= 1) fixed += __shfl_xor_sync(0xffffffffu, fixed, off);
   if (lane == 0) p.sum[unit] = fixed, p.max[unit] = m;
@@ -282,19 +292,20 @@ __device__ __forceinline__ void load_groups(const float *tops, int base, int gro
 }
 
 // One CTA per request, two warps per beam: one picks the row's best logits,
-// one takes its maximum, sum and (in 64 bits) logarithm meanwhile.  Most of
+// one takes its maximum and sum meanwhile; the logarithms (in 64 bits) are one
+// warp's for all rows.  Most of
 // its time is the latency of a few dependent reads, so each is issued at once:
 // the maxima into registers, the groups into shared memory.  About 5 us of one
 // request's 10 and 7 of 96 requests' 29.
 constexpr int kJoinGroups = 64;  // groups of a row that are looked through
 constexpr int kJoinAhead = 8;    // of them in shared memory at a time
 template <typename T>
-__global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32) beam_join_kernel(const SelectParams p) {
+__global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32, 1) beam_join_kernel(const SelectParams p) {
   using L = Logits<T>;
   constexpr int kVec = L::kVec;
   const int W = p.W, K = 2 * W, req = blockIdx.x, lane = threadIdx.x & 31, beam = threadIdx.x >> 5;
   __shared__ unsigned long long keeps[WF_MAX_BEAMS][kSelKeep], best_key[WF_MAX_BEAMS * 2 * WF_MAX_BEAMS], cand[WF_MAX_BEAMS * 2 * WF_MAX_BEAMS];
-  __shared__ unsigned long long ranked[2 * WF_MAX_BEAMS];
+  __shared__ unsigned long long ranked[2 * WF_MAX_BEAMS], row_sum[WF_MAX_BEAMS];
   __shared__ float row_max[WF_MAX_BEAMS], row_log[WF_MAX_BEAMS], row_score[WF_MAX_BEAMS];
   __shared__ int counts[WF_MAX_BEAMS], chosen[WF_MAX_BEAMS][kJoinGroups];
   extern __shared__ uint4 vectors[];  // [W][kJoinAhead][32]
@@ -313,48 +324,50 @@ __global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32) beam_join_kernel(const 
     for (int c = lane + 32; c < p.segments; c += 32) m = fmaxf(m, sm[c]);
     m = warp_max(m);
     const auto scaled = [&](unsigned long long v, float at) -> unsigned long long {
+      if (at == m) return v;
       const float f = expf(at - m);
-      return f == f ? static_cast<unsigned long long>(static_cast<double>(v) * static_cast<double>(f)) : 0;
+      return f < 1.f ? __umul64hi(v, fixed_point(f, 64)) : f == 1.f ? v : 0;
     };
     unsigned long long s = scaled(s0, m0);
     for (int c = lane + 32; c < p.segments; c += 32) s += scaled(ss[c], sm[c]);
 #pragma unroll
     for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    if (lane == 0) row_max[w] = m, row_log[w] = static_cast<float>(log(static_cast<double>(s) * 0x1p-40));
+    if (lane == 0) row_max[w] = m, row_sum[w] = s;
+    asm volatile("bar.sync 1, %0;" ::"r"(W * 32) : "memory");  // these warps; one takes the logarithms of all rows
+    if (w == 0 && lane < W) row_log[lane] = static_cast<float>(log(static_cast<double>(row_sum[lane]) * 0x1p-40));
   } else {
     const long long row = row0 + beam;
     float *tops = p.group_max + row * p.groups;
-    float lane_top = -INFINITY;
+    float lane_top = -INFINITY, lane_next = -INFINITY;  // the largest and the next of this lane's groups
     if (lane == 0) counts[beam] = 0;
     for (int i = lane; i < K; i += 32) best_key[beam * K + i] = 0;
     for (int base = 0; base < p.groups; base += 512) {
       float t[16];
       load_groups(tops, base, p.groups, lane, t);
 #pragma unroll
-      for (int u = 0; u < 16; ++u) lane_top = fmaxf(lane_top, t[u]);
+      for (int u = 0; u < 16; ++u) lane_next = fmaxf(lane_next, fminf(lane_top, t[u])), lane_top = fmaxf(lane_top, t[u]);
     }
     __syncwarp();
     // Of 32 maxima over the lanes' groups the K-th is reached by K groups and
-    // few more (all, below K finite ones).  For K up to 16; more beams, or
-    // more groups than can be held, pick the K groups one by one.
-    float floor_v = __shfl_sync(0xffffffffu, warp_sort(lane_top, lane), min(K, 32) - 1);
+    // few more (all, below K finite ones); for K above 16, of the lanes' two
+    // largest.  More groups than can be held: K groups one by one.
+    float order = warp_sort(lane_top, lane);
+    if (K > 16) order = warp_sort(fmaxf(order, __shfl_sync(0xffffffffu, warp_sort(lane_next, lane), 31 - lane)), lane);
+    float floor_v = __shfl_sync(0xffffffffu, order, K - 1);
     if (floor_v == -INFINITY) floor_v = -FLT_MAX;
-    int n_groups = kJoinGroups + 1;
-    if (K <= 16) {
-      for (int base = 0; base < p.groups; base += 512) {
-        float t[16];
-        load_groups(tops, base, p.groups, lane, t);
-        uint32_t hits = 0;
+    for (int base = 0; base < p.groups; base += 512) {
+      float t[16];
+      load_groups(tops, base, p.groups, lane, t);
+      uint32_t hits = 0;
 #pragma unroll
-        for (int u = 0; u < 16; ++u) hits |= t[u] >= floor_v ? 1u << u : 0u;
-        for (; hits; hits &= hits - 1) {
-          const int at = atomicAdd(&counts[beam], 1);
-          if (at < kJoinGroups) chosen[beam][at] = base + (__ffs(hits) - 1) * 32 + lane;
-        }
+      for (int u = 0; u < 16; ++u) hits |= t[u] >= floor_v ? 1u << u : 0u;
+      for (; hits; hits &= hits - 1) {
+        const int at = atomicAdd(&counts[beam], 1);
+        if (at < kJoinGroups) chosen[beam][at] = base + (__ffs(hits) - 1) * 32 + lane;
       }
-      __syncwarp();
-      n_groups = counts[beam];
     }
+    __syncwarp();
+    int n_groups = counts[beam];
     if (n_groups > kJoinGroups) {
       unsigned long long last = 0, mine = 0;
       const auto look = [&]() {
@@ -396,16 +409,30 @@ __global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32) beam_join_kernel(const 
           mine[u * 32] = edge_vector<T>(in.src, id, p.V);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
-      for (int u = 0; u < here; ++u) {
-        float y[kVec];
-        L::unpack(mine[u * 32], y);
+      // a bit for each of a lane's values, 32 at a time; the lanes' hits one after another
+      constexpr int kBatch = 32 / kVec;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const unsigned have = __ballot_sync(0xffffffffu, y[e] >= floor_v);
-          if (!have) continue;
-          const int at = n + __popc(have & ((1u << lane) - 1));
-          if (y[e] >= floor_v && at < kSelKeep) keep[at] = order_key(y[e], id_of(k0 + u) + e);
-          n += __popc(have);
+      for (int u0 = 0; u0 < kJoinAhead; u0 += kBatch) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          if (u0 + u >= here) continue;
+          float y[kVec];
+          L::unpack(mine[(u0 + u) * 32], y);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) hits |= y[e] >= floor_v ? 1u << (u * kVec + e) : 0u;
+        }
+        int upto = __popc(hits);
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, upto, off);
+          if (lane >= off) upto += v;
+        }
+        int at = n + upto - __popc(hits);
+        n += __shfl_sync(0xffffffffu, upto, 31);
+        for (; hits && at < kSelKeep; hits &= hits - 1, ++at) {
+          const int bit = __ffs(hits) - 1, u = u0 + bit / kVec, e = bit % kVec;
+          keep[at] = order_key(L::one(mine + u * 32, e), id_of(k0 + u) + e);
         }
       }
     }
@@ -454,10 +481,17 @@ __global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32) beam_join_kernel(const 
   __syncthreads();
   for (int i = threadIdx.x; i < W * K; i += blockDim.x) {
     const unsigned long long k = cand[i];
-    int rank = 0;
-#pragma unroll 5
-    for (int j = 0; j < W * K; ++j) rank += cand[j] > k;
-    if (k && rank < K) ranked[rank] = k;
+    if (!k) continue;
+    int rank = 0;  // of every row, whose candidates descend, those above
+#pragma unroll 4
+    for (int w = 0; w < W; ++w) {
+      const unsigned long long *of = cand + w * K;
+      int above = 0;
+      for (int step = 1 << (31 - __clz(K)); step; step >>= 1)
+        if (above + step <= K && of[above + step - 1] > k) above += step;
+      rank += above;
+    }
+    if (rank < K) ranked[rank] = k;
   }
   __syncthreads();
   if (beam != 0) return;
