@@ -498,6 +498,36 @@ def test_select_random(n, W, V, dtype):
     _check_select(got, x, scores, sup, eos)
 
 
+@pytest.mark.parametrize("n,W,V,dtype,kind", [(3, 16, 30011, "f32", "ties"), (2, 9, 51866, "f32", "normal"), (2, 12, 20003, "bf16", "ties"),
+                                              (3, 13, 12001, "f16", "few"), (1, 16, 9000, "f32", "few"), (4, 16, 51866, "f32", "normal")])
+@pytest.mark.parametrize("shift", [0, 3, 13])
+def test_select_many_beams(n, W, V, dtype, kind, shift):
+    """More than 8 beams: equal logits in many groups, fewer finite ones than places, suppressed ids from any address."""
+    import torch
+    from paper_2609_32869_gb300 import binding as B
+    rng = np.random.default_rng(V + shift)
+    if kind == "ties":
+        logits = rng.integers(-20, 5, (n, W, V)) / 4.0
+    elif kind == "few":
+        logits = np.where(rng.random((n, W, V)) < 20 / V, rng.integers(-40, 40, (n, W, V)) / 4.0, -np.inf)
+    else:
+        logits = rng.normal(0, 3, (n, W, V))
+    sup = rng.random(V) < 0.01
+    held = torch.zeros(V + 32, dtype=torch.uint8, device="cuda")
+    held[:] = 1                                    # what lies around the suppressed ids is not read as one
+    held[shift:shift + V] = _dev(torch, sup.astype(np.uint8))
+    x, scores = _dev(torch, logits.reshape(n * W, V), dtype), -rng.uniform(0, 10, (n, W)).astype(np.float32)
+    code = {"f32": B.WF_F32, "bf16": B.WF_BF16, "f16": B.WF_F16}[dtype]
+    nb = B.wf_beam_select_scratch_bytes(n, W, V)
+    sc = torch.full((nb + 64,), GUARD, dtype=torch.uint8, device="cuda")
+    out = {k: _i32(torch, np.full((n, W), 55)) for k in ("token", "parent", "fin_parent")}
+    out.update({k: torch.full((n, W), 5.0, device="cuda") for k in ("score", "fin_score")})
+    B.wf_beam_select(x, code, V, _dev(torch, scores), held[shift:shift + V], n, W, V, 7, out["token"], out["parent"], out["score"],
+                     out["fin_parent"], out["fin_score"], sc, nb)
+    assert (sc[nb:] == GUARD).all()
+    _check_select({k: v.cpu().numpy() for k, v in out.items()}, x.float().cpu().numpy().reshape(n, W, V), scores.astype(np.float64), sup, 7)
+
+
 def test_select_ties_go_to_the_lowest_beam_and_id():
     """Beams with equal rows and equal scores; equal logits all over the row, in one CTA's chunk and across."""
     import torch
