@@ -157,10 +157,11 @@ __device__ __forceinline__ void copy16_async(void *smem_dst, const void *src) {
 // next tile's while this one is worked on: bound by HBM, and by the ends of the
 // one wave of CTAs.  With the joining kernel after it 96 requests x 5 beams x
 // 51866 fp32 take 28.8 us, 3.5 TB/s (tiles straight to registers and a mask per
-// warp 30.8; four CTAs an SM, which spill, 31.3).  The sum adds a tile's 32 terms a lane in fp32 and the tiles with
-// the rounding carried along; lanes and segments add in fixed point (2^-40),
-// without order.  A NaN is never the larger of a comparison, which keeps it out
-// of the maxima and the candidates; only the sum has to look for it.
+// warp 30.8; four CTAs an SM, which spill, 31.3).  The sum adds a tile's 32
+// terms a lane in fp32 and the tiles with the rounding carried along; lanes and
+// segments add in fixed point (2^-40), without order.  A NaN is never the
+// larger of a comparison, which keeps it out of the maxima and the candidates;
+// only the sum has to look for it.
 template <typename T>
 __global__ void __launch_bounds__(kSelThreads, kSelBlocks) beam_segment_kernel(const SelectParams p) {
   using L = Logits<T>;
@@ -296,7 +297,8 @@ __device__ __forceinline__ void load_groups(const float *tops, int base, int gro
 // warp's for all rows.  Most of
 // its time is the latency of a few dependent reads, so each is issued at once:
 // the maxima into registers, the groups into shared memory.  About 5 us of one
-// request's 10 and 7 of 96 requests' 29.
+// request's 9.5 and 7 of 96 requests' 28.5 with 5 beams each; one request's 16
+// beams take 20 in all, by issue on one SM.
 constexpr int kJoinGroups = 64;  // groups of a row that are looked through
 constexpr int kJoinAhead = 8;    // of them in shared memory at a time
 template <typename T>
