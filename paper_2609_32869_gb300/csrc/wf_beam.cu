@@ -401,42 +401,66 @@ __global__ void __launch_bounds__(2 * WF_MAX_BEAMS * 32, 1) beam_join_kernel(con
     unsigned long long *keep = keeps[beam];
     uint4 *mine = vectors + beam * (kJoinAhead * 32) + lane;
     int n = 0;
-    for (int k0 = 0; k0 < n_groups; k0 += kJoinAhead) {
-      const int here = min(kJoinAhead, n_groups - k0);
-      for (int u = 0; u < here; ++u) {
-        const int id = id_of(k0 + u);
-        if (id >= 0 && id + kVec <= p.V)
-          copy16_async(mine + u * 32, in.src + id);
-        else
-          mine[u * 32] = edge_vector<T>(in.src, id, p.V);
-      }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      // a bit for each of a lane's values, 32 at a time; the lanes' hits one after another
-      constexpr int kBatch = 32 / kVec;
-#pragma unroll
-      for (int u0 = 0; u0 < kJoinAhead; u0 += kBatch) {
-        uint32_t hits = 0;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          if (u0 + u >= here) continue;
+    for (bool again = floor_v == -FLT_MAX;; again = true) {
+      // fewer groups than places, or a bound that too many reach: that of the lanes'
+      // two largest logits (20 x 8 beams x 1000: 14 us, by rounds as below 56)
+      if (again) {
+        float top = -INFINITY, next = -INFINITY;
+#pragma unroll 2
+        for (int g = 0; g < n_groups; ++g) {
+          const int id = id_of(g);
           float y[kVec];
-          L::unpack(mine[(u0 + u) * 32], y);
+          L::unpack(in.vector(id), y);
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) hits |= y[e] >= floor_v ? 1u << (u * kVec + e) : 0u;
+          for (int e = 0; e < kVec; ++e) {
+            if (!(y[e] > next) || (p.suppress && p.suppress[id + e])) continue;  // (outside the row -inf)
+            next = fmaxf(next, fminf(top, y[e])), top = fmaxf(top, y[e]);
+          }
         }
-        int upto = __popc(hits);
+        order = warp_sort(top, lane);
+        order = warp_sort(fmaxf(order, __shfl_sync(0xffffffffu, warp_sort(next, lane), 31 - lane)), lane);
+        floor_v = fmaxf(floor_v, __shfl_sync(0xffffffffu, order, K - 1));
+        n = 0;
+        __syncwarp();
+      }
+      for (int k0 = 0; k0 < n_groups; k0 += kJoinAhead) {
+        const int here = min(kJoinAhead, n_groups - k0);
+        for (int u = 0; u < here; ++u) {
+          const int id = id_of(k0 + u);
+          if (id >= 0 && id + kVec <= p.V)
+            copy16_async(mine + u * 32, in.src + id);
+          else
+            mine[u * 32] = edge_vector<T>(in.src, id, p.V);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        // a bit for each of a lane's values, 32 at a time; the lanes' hits one after another
+        constexpr int kBatch = 32 / kVec;
 #pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const int v = __shfl_up_sync(0xffffffffu, upto, off);
-          if (lane >= off) upto += v;
-        }
-        int at = n + upto - __popc(hits);
-        n += __shfl_sync(0xffffffffu, upto, 31);
-        for (; hits && at < kSelKeep; hits &= hits - 1, ++at) {
-          const int bit = __ffs(hits) - 1, u = u0 + bit / kVec, e = bit % kVec;
-          keep[at] = order_key(L::one(mine + u * 32, e), id_of(k0 + u) + e);
+        for (int u0 = 0; u0 < kJoinAhead; u0 += kBatch) {
+          uint32_t hits = 0;
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            if (u0 + u >= here) continue;
+            float y[kVec];
+            L::unpack(mine[(u0 + u) * 32], y);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) hits |= y[e] >= floor_v ? 1u << (u * kVec + e) : 0u;
+          }
+          int upto = __popc(hits);
+#pragma unroll
+          for (int off = 1; off < 32; off <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += v;
+          }
+          int at = n + upto - __popc(hits);
+          n += __shfl_sync(0xffffffffu, upto, 31);
+          for (; hits && at < kSelKeep; hits &= hits - 1, ++at) {
+            const int bit = __ffs(hits) - 1, u = u0 + bit / kVec, e = bit % kVec;
+            keep[at] = order_key(L::one(mine + u * 32, e), id_of(k0 + u) + e);
+          }
         }
       }
+      if (n <= kSelKeep || again) break;
     }
     __syncwarp();
     if (n <= kSelKeep) {  // each one's rank is the number of larger ones

@@ -528,6 +528,24 @@ def test_select_many_beams(n, W, V, dtype, kind, shift):
     _check_select({k: v.cpu().numpy() for k, v in out.items()}, x.float().cpu().numpy().reshape(n, W, V), scores.astype(np.float64), sup, 7)
 
 
+@pytest.mark.parametrize("n,W,V,dtype", [(20, 8, 1000, "f32"), (9, 8, 3045, "bf16"), (3, 16, 4096, "f32"), (3, 16, 8192, "f16"), (2, 16, 33, "bf16"),
+                                         (2, 16, 300, "f32"), (5, 3, 200, "f16")])
+@pytest.mark.parametrize("suppressed", [0.0, 0.05, 0.97])
+def test_select_few_groups(n, W, V, dtype, suppressed):
+    """Vocabularies of about as many groups as places: the bound comes from the logits themselves."""
+    import torch
+    from paper_2609_32869_gb300 import binding as B
+    rng = np.random.default_rng(V + W)
+    logits = rng.normal(0, 3, (n, W, V))
+    logits[0, 0, ::3] = np.nan
+    logits[-1, -1] = -np.inf
+    scores, sup = -rng.uniform(0, 10, (n, W)), rng.random(V) < suppressed
+    sup[V // 2] = False
+    got, x = _select(torch, B, logits, scores, sup, V // 2, dtype, pad=5)
+    x = np.where(np.isnan(x), -np.inf, x)          # a NaN is no candidate and no part of the sum
+    _check_select(got, x, scores, sup, V // 2)
+
+
 def test_select_ties_go_to_the_lowest_beam_and_id():
     """Beams with equal rows and equal scores; equal logits all over the row, in one CTA's chunk and across."""
     import torch
