@@ -58,6 +58,7 @@ constexpr int kAtWarps = 4;
 constexpr int kAtThreads = kAtWarps * 32;
 constexpr int kAtTile = 64;    // positions of a warp's step
 constexpr int kAtCluster = 8;  // chunks that a cluster joins
+constexpr int kAtShort = 2048; // positions of a chunk that two CTAs an SM may have
 
 // None of these is volatile: the compiler may interleave independent chains.
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
@@ -141,8 +142,8 @@ __device__ __forceinline__ int clamp_len(const Kv4AttnParams &p, int len) { retu
 //     instructions unpack nibbles)
 //   80 sequences of 4 to 448 positions, 20 heads, bf16: 13.7 us, by the
 //     instructions before and after the loop
-//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 40 us,
-//     3.1 TB/s, by issue at 12 warps an SM
+//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 37 us,
+//     3.4 TB/s, by issue at 12 warps an SM
 //   5 rows of one sequence, 1500 positions, 20 heads, bf16: 6 us, by the launch
 //     and one chain of reads
 // One wave of CTAs that go on to their next unit, its first records on their way
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
   if (raw_len != len && threadIdx.x == 0) set_error(p.err, raw_len < 0 ? WF_DEV_ERR_PAGE : WF_DEV_ERR_CAPACITY);
   // positions that any row of this unit sees, and this CTA's share of them
   const int seen = row_limit(p, min(row0 + kRows, rows) - 1, len);
-  const int begin = blockIdx.y * p.chunk, end = min(seen, begin + p.chunk);
+  const int begin = blockIdx.y * p.chunk, end = begin + min(seen - begin, p.chunk);
   if (begin >= end && blockIdx.y > 0 && !p.cluster) return;
 
   // The ring: step i of this warp is positions begin + (warp + i kAtWarps) 64.
@@ -655,13 +656,23 @@ static AtPlan at_plan(int64_t n_seq, int64_t heads, int64_t rows, int max_len) {
   a.tiles = rows > 8 ? 2 : 1;
   a.row_groups = (rows + a.tiles * 8 - 1) / (a.tiles * 8);
   a.units = n_seq * heads * a.row_groups;
-  // A CTA's four warps take at least 64 positions each; sequences are cut
-  // until there are about eight CTAs an SM at the longest, so that SMs whose
-  // sequences are short find other work.
-  const int64_t least = kAtWarps * kAtTile, want = 152 * 8;
-  const int64_t per = (a.units * max_len + want - 1) / want;
-  a.chunk = static_cast<int>(std::min<int64_t>(std::max(least, (per + least - 1) / least * least), 1 << 30));
-  a.chunks = (max_len + a.chunk - 1) / a.chunk;
+  // A CTA's four warps take at least 64 positions each.  Short sequences: cut
+  // into even chunks, a cluster each, until there are two CTAs an SM, for a
+  // cluster stays until its last is done (1500 positions, 20 heads: 50 sequences
+  // x 9 rows 41 us, 8 x 5 rows 10.1; cut until there are eight CTAs an SM 54 and
+  // 14.1).  Long ones: eight CTAs an SM, so that SMs whose sequences are short
+  // find other work (12 sequences of 3000 to 9000 positions, 32 heads on 8: 32 us
+  // against 34; 6 of 5000 to 65001: 37 against 105).
+  const auto cut = [&](int64_t want) {
+    const int64_t least = kAtWarps * kAtTile, longest = max_len;
+    const int64_t per = std::max(least, (a.units * longest + want - 1) / want);
+    const int64_t chunks = (longest + per - 1) / per;
+    const int64_t chunk = (longest + chunks * least - 1) / (chunks * least) * least;
+    a.chunk = static_cast<int>(std::min<int64_t>(chunk, 1 << 30));
+    a.chunks = static_cast<int>((longest + a.chunk - 1) / a.chunk);
+  };
+  cut(152 * 2);
+  if (a.chunks > kAtCluster || a.chunk > kAtShort) cut(152 * 8);
   return a;
 }
 
