@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
 #pragma unroll
     for (int w = 0; w < kAtWarps; ++w) {
       const float at = sm_m[w * kRows + row];
-      f[w] = at == -INFINITY ? 0.f : ex2(at - mm);  // (a warp that saw nothing has zeros)
+      f[w] = at == -INFINITY ? 0.f : ex2(at - mm);  // (a warp that saw nothing has zeros, one of NaN scores NaN)
       ll += f[w] * sm_l[w * kRows + row];
     }
     const float inv = ll == 0.f ? 0.f : 1.f / ll;
@@ -559,8 +559,9 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
       if (k < chunks) cm[k] = dsmem_ld_f32(dsmem_map(smem_u32(cl_m + row), k)), mm = fmaxf(mm, cm[k]);
 #pragma unroll
     for (int k = 0; k < kAtCluster; ++k) {
-      if (k >= chunks || cm[k] == -INFINITY) continue;
-      const float f = ex2(cm[k] - mm);
+      if (k >= chunks) continue;
+      // no maximum: a chunk that the row sees nothing of, whose sums are zeros, or one of NaN scores, which stay NaN
+      const float f = cm[k] == -INFINITY ? 0.f : ex2(cm[k] - mm);
       const uint32_t at = dsmem_map(smem_u32(cl_o + row * (G * 64) + d), k);
       ll += f * dsmem_ld_f32(dsmem_map(smem_u32(cl_l + row), k));
       a += f * dsmem_ld_f32(at), b += f * dsmem_ld_f32(at + 4);
