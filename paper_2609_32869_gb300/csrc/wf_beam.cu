@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kSelThreads, kSelBlocks) beam_segment_kernel(c
     float tops = 0.f, tile_top = -INFINITY;
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
-      float t = fmaxf(x[v * kVec], x[v * kVec + 1]);
+      float t = max3(-INFINITY, x[v * kVec], x[v * kVec + 1]);  // -inf where all are NaN: the join orders these
 #pragma unroll
       for (int e = 2; e < kVec; e += 2) t = max3(t, x[v * kVec + e], x[v * kVec + e + 1]);
       const float g = warp_max(t);
