@@ -479,7 +479,8 @@ size_t wf_beam_select_scratch_bytes(int32_t n_req, int32_t beams, int32_t vocab)
  * own; if all of a request's parents are -1 the request is released.  Blocks
  * that no beam of the request holds any more are pushed on the free list
  * (d_free, capacity pool->n_blocks, *d_n_free ids before, *d_n_free_out
- * after; they may be one), by request, column and beam.  Columns past the length are not written.
+ * after; they may be one), by request, column and beam; an id outside the pool
+ * is not pushed (WF_DEV_ERR_PAGE).  Columns past the length are not written.
  * d_table_out may be d_table_in. */
 wf_status wf_beam_reorder(const wf_kv4_pool *pool, const int32_t *d_table_in, int32_t *d_table_out,
                           int32_t table_stride, const int32_t *d_len, const int32_t *d_parent,

@@ -548,7 +548,8 @@ __global__ void __launch_bounds__(kReorderThreads) beam_tables_kernel(const Reor
       }
 #pragma unroll
       for (int w = 0; w < MAXW; ++w) {
-        bool held = old[w] < 0;
+        if (old[w] >= p.pool.n_blocks) err |= WF_DEV_ERR_PAGE;  // no block of the pool: not one to push
+        bool held = old[w] < 0 || old[w] >= p.pool.n_blocks;
 #pragma unroll
         for (int q = 0; q < MAXW; ++q) held |= now[q] == old[w] || (q < w && old[q] == old[w]);
         if (!held) dead |= 1u << w;
