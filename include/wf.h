@@ -410,8 +410,10 @@ wf_status wf_page_plan(const int32_t *d_old_len, const int32_t *d_new_len, int32
 /* Quantise n rows of keys and values into one layer of the cache.
  *   d_k, d_v  dtype [n][n_kv_heads * head_dim], row strides in elements
  *             (multiples of 8; pointers 16-byte aligned)
- *   d_slots   int32 [n]: a negative slot skips its row; a slot named twice
- *             holds either row
+ *   d_slots   int32 [n]: a negative slot skips its row.  The others are
+ *             distinct: rows are written by many threads without order, so a
+ *             slot named twice may hold one row's codes under another's scale
+ *             (no other slot is touched)
  * wf_kv4_load reads the slots back into rows (zeros for a negative slot). */
 wf_status wf_kv4_store(const wf_kv4_pool *pool, int32_t layer, const void *d_k, int64_t k_stride,
                        const void *d_v, int64_t v_stride, const int32_t *d_slots, int32_t n,
