@@ -436,7 +436,10 @@ wf_status wf_kv4_load(const wf_kv4_pool *pool, int32_t layer, const int32_t *d_s
  * Strides are in elements, multiples of 8, pointers 16-byte aligned; d_out is
  * not d_q.  A row that sees nothing is zeros; a block id outside the pool is not read and its
  * positions are not seen (WF_DEV_ERR_PAGE).  Scores, softmax and sums are
- * fp32; results do not depend on timing.  d_scratch (16-byte aligned) holds
+ * fp32; a weight times its value's s is rounded for the second product, to bf16
+ * for a bf16 cache and to at least 11 bits for an fp16 one (of weights down to
+ * 2^-14 of a row's largest; of smaller ones at most 2^-25 of the s is lost).
+ * Results do not depend on timing.  d_scratch (16-byte aligned) holds
  * wf_kv4_attention_scratch_bytes() bytes and belongs to the call until it is
  * done. */
 wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d_q,

@@ -12,10 +12,12 @@
 //   rounded to bf16, whose range holds any scale.
 //   fp16: a nibble where it lies, in bits 0 to 3 under 1024 or 4 to 7 under 64, so
 //   that a word of eight takes one shift.  Odd nibbles of keys keep their 64 + 8,
-//   which the sums start without.  p_j s_jg is rounded to fp16, its 11 bits
-//   relative to a power of two that follows the largest s of each 32 positions:
-//   below 2^-20 of that s bits are lost, below 2^-31 all of it.  Steps with
-//   positions that are not seen round to the sum of two bf16 instead.
+//   which the sums start without.  p_j s_jg is rounded to fp16 after a scaling by
+//   a power of two (kept per group, moved with the scales) that holds every s of
+//   32 positions between 1 and 2^7: 11 bits of weights down to 2^-14 of the
+//   running reference, and at most 2^-25 of its s off below.  Steps whose scales
+//   span more than that, and steps with positions that are not seen, round to
+//   the sum of two bf16, 16 bits of any size.
 // (Keys and weights in fp16 for bf16 caches too, rows of queries scaled into its
 // range: 96 requests x 9 rows took 78 us instead of 71, the row scaling and its
 // registers costing more than the shifts.)
@@ -142,8 +144,8 @@ __device__ __forceinline__ int clamp_len(const Kv4AttnParams &p, int len) { retu
 //     instructions unpack nibbles)
 //   80 sequences of 4 to 448 positions, 20 heads, bf16: 13.7 us, by the
 //     instructions before and after the loop
-//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 37 us,
-//     3.4 TB/s, by issue at 12 warps an SM
+//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 38 us,
+//     3.3 TB/s, by issue at 12 warps an SM
 //   5 rows of one sequence, 1500 positions, 20 heads, bf16: 6 us, by the launch
 //     and one chain of reads
 // One wave of CTAs that go on to their next unit, its first records on their way
@@ -255,19 +257,23 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
   least = min(least, __shfl_xor_sync(0xffffffffu, least, 1));
   least = min(least, __shfl_xor_sync(0xffffffffu, least, 2));
 
-  float o[NT][G][4][4] = {};  // in units of 1 / so
-  float so = kF16 ? 0.f : 1.f;  // fp16: a power of two near 1 / the largest value scale of the last steps; 0: none yet
+  float o[NT][G][4][4] = {};  // of group g in units of 1 / so[g]
+  float so[G];                // 1; fp16: a power of two that holds s so of the values in [1, 2^7]
+#pragma unroll
+  for (int g = 0; g < G; ++g) so[g] = 1.f;
   const float c = p.scale * 1.4426950408889634f;  // base-2 softmax
   float2 zacc[NT][G] = {}, l[NT], m[NT];  // of rows 2t and 2t + 1; m: the power of two that the weights are relative to
 #pragma unroll
   for (int n = 0; n < NT; ++n) l[n] = make_float2(0.f, 0.f), m[n] = make_float2(-INFINITY, -INFINITY);
 
-  // kSub tiles of 16 positions from k0; `edge`: some are not seen by some row, or are not there
+  // kSub tiles of 16 positions from k0; `edge`: some are not seen by some row, or are not there.
+  // False, with nothing added: their scales need the two terms that an edge's weights have.
   auto step = [&](const unsigned char *buf, int k0, uint32_t there, auto edge_c) {
     constexpr bool edge = decltype(edge_c)::value;
     float2 x[kSub][NT][2];  // [16 positions][rows][position r, r + 8] (row 2t, row 2t + 1)
     uint2 szv[kSub][G];
-    float mx[NT][2], top_s = 0.f;
+    float mx[NT][2];
+    bool wide = false;  // fp16: some scales are too far apart for one power of two (0 is none of them)
 #pragma unroll
     for (int n = 0; n < NT; ++n) mx[n][0] = mx[n][1] = -INFINITY;
 #pragma unroll
@@ -298,13 +304,6 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
         float z0 = X::hi(sz.x) * c, z1 = X::hi(sz.y) * c;
         if (!kF16) z0 = fmaf(-136.f, s0, z0), z1 = fmaf(-136.f, s1, z1);
         szv[i][g] = make_uint2(sz.z, sz.w);
-        if (kF16 && edge) {  // what lies past the sequence may hold anything
-          const bool here = there >> i & 1;
-          if (here && k0 + i * 16 + r < seen) top_s = fmaxf(top_s, X::lo(sz.z));
-          if (here && k0 + i * 16 + r + 8 < seen) top_s = fmaxf(top_s, X::lo(sz.w));
-        } else if (kF16) {
-          top_s = max3(top_s, X::lo(sz.z), X::lo(sz.w));
-        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const float2 a = make_float2(fmaf(s0, acc[i][n][0], z0 * qs[n][g].x), fmaf(s0, acc[i][n][1], z0 * qs[n][g].y));
@@ -331,22 +330,42 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
       }
     }
     // The reference of the weights moves only when some row's maximum passes
-    // it by 2^8, that of the sums when the largest scale is 2^6 from it: the
-    // sums stay far inside fp32 and fp16 and most steps rescale nothing.
+    // it by 2^8, that of the sums when a scale leaves its range (or is 0, which
+    // changes nothing): the products stay below 2^15, which fp16 holds, and most
+    // steps rescale nothing.
+    constexpr float kLowS = 1.f, kHighS = 0x1p7f;
     bool moved = false;
-    if (kF16) {
-      top_s = warp_max(top_s);
-      moved = top_s > 0.f && !(top_s * so >= 0x1p-6f && top_s * so <= 0x1p6f);
+    if (kF16 && !edge) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const float a = X::lo(szv[0][g].x), b = X::lo(szv[0][g].y), e = X::lo(szv[1][g].x), f = X::lo(szv[1][g].y);
+        moved |= fminf(fminf(a, b), fminf(e, f)) * so[g] < kLowS || fmaxf(max3(a, b, e), f) * so[g] > kHighS;
+      }
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) moved |= mx[n][0] > m[n].x + 8.f || mx[n][1] > m[n].y + 8.f;
     if (__any_sync(0xffffffffu, moved)) {
-      float change = 1.f;
-      if (kF16) {
-        const int e = min(max(static_cast<int>(__float_as_uint(top_s) >> 23) - 127, -100), 100);
-        const float next_so = top_s > 0.f ? __uint_as_float(static_cast<uint32_t>(127 - e) << 23) : so;
-        change = so > 0.f ? next_so / so : 0.f;  // (of powers of two; no sums before the first)
-        so = next_so;
+      float change[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        change[g] = 1.f;
+        if (!kF16 || edge) continue;
+        float top = 0.f, low = INFINITY;  // the largest scale and the smallest above 0
+#pragma unroll
+        for (int i = 0; i < kSub; ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float v = X::lo(u ? szv[i][g].y : szv[i][g].x);
+            top = fmaxf(top, v);
+            if (v > 0.f) low = fminf(low, v);
+          }
+        top = warp_max(top), low = -warp_max(-low);
+        if (top > 0.f && (low * so[g] < kLowS || top * so[g] > kHighS)) {
+          const float next_so = __uint_as_float((259u << 23) - (__float_as_uint(top) & 0x7f800000u));  // top in [2^5, 2^6)
+          change[g] = next_so / so[g];                                                                 // (of powers of two)
+          so[g] = next_so;
+          wide |= low * next_so < kLowS;
+        }
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -365,10 +384,11 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
           zacc[n][g].x *= c0, zacc[n][g].y *= c1;
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            o[n][g][q][0] *= c0 * change, o[n][g][q][1] *= c1 * change, o[n][g][q][2] *= c0 * change, o[n][g][q][3] *= c1 * change;
+            o[n][g][q][0] *= c0 * change[g], o[n][g][q][1] *= c1 * change[g], o[n][g][q][2] *= c0 * change[g], o[n][g][q][3] *= c1 * change[g];
         }
         m[n] = make_float2(next[0], next[1]);
       }
+      if (kF16 && wide) return false;
     }
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {
@@ -393,7 +413,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const uint32_t sz = u ? szv[i][g].y : szv[i][g].x;
-            const float sv = X::lo(sz) * so, zv = X::hi(sz);
+            const float sv = X::lo(sz) * so[g], zv = X::hi(sz);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               ph[n][u] = transpose8x8(pack_f16(mul2(x[i][n][u], make_float2(sv, sv))));
@@ -412,7 +432,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const uint32_t sz = u ? szv[i][g].y : szv[i][g].x;
-            const float sv = kF16 ? X::lo(sz) * so : X::lo(sz), zv = X::hi(sz);
+            const float sv = kF16 ? X::lo(sz) * so[g] : X::lo(sz), zv = X::hi(sz);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               const float2 w = x[i][n][u];
@@ -443,6 +463,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
         }
       }
     }
+    return true;
   };
 
   int stage = 0, k0 = first;
@@ -458,9 +479,8 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
     const unsigned char *buf = ring + stage * S::kStageBytes;
 #pragma unroll 1
     for (int h = 0; h < 4; h += kSub) {
-      if (k0 + (h + kSub) * 16 <= least && there == 15u)
-        step(buf + h * kKv4Rec, k0 + h * 16, there >> h, std::false_type());
-      else
+      const bool all = k0 + (h + kSub) * 16 <= least && there == 15u;
+      if (!all || !step(buf + h * kKv4Rec, k0 + h * 16, there >> h, std::false_type()))
         step(buf + h * kKv4Rec, k0 + h * 16, there >> h, std::true_type());
     }
     __syncwarp();
@@ -470,7 +490,6 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
   }
 
   // the warp's results: sums over its 8 position lanes, rows 2t and 2t + 1
-  const float os = so > 0.f ? 1.f / so : 0.f;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -496,7 +515,7 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
       for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const float z = e ? zacc[n][g].y : zacc[n][g].x;
+          const float z = e ? zacc[n][g].y : zacc[n][g].x, os = 1.f / so[g];
           *reinterpret_cast<float4 *>(sm_o + row * kLd + g * 64 + r * 8 + u * 4) =
               make_float4(fmaf(o[n][g][0][e + 2 * u], os, z), fmaf(o[n][g][1][e + 2 * u], os, z), fmaf(o[n][g][2][e + 2 * u], os, z),
                           fmaf(o[n][g][3][e + 2 * u], os, z));
