@@ -34,6 +34,10 @@ class BeamDecoder:
 
     def __init__(self, cfg, weights, n_req: int, beams: int, max_ctx: int | None = None, block_size: int = 16, device="cuda"):
         import torch
+        if n_req < 1 or not 1 <= beams <= B.WF_MAX_BEAMS or 2 * beams > cfg.vocab:
+            raise ValueError(f"requests must be positive and beams from 1 to {B.WF_MAX_BEAMS}, at most half the vocabulary")
+        if not B.wf_kv4_block_bytes(block_size, cfg.n_heads, cfg.head_dim):
+            raise ValueError("the 4-bit cache takes blocks of 16, 32 or 64 positions and heads of 64 or 128")
         self.torch, self.cfg, self.n, self.W = torch, cfg, n_req, beams
         self.w = weights if isinstance(weights, dict) else upload_weights(weights, device)
         self.max_ctx, self.bs, self.device = max_ctx or cfg.max_pos, block_size, device
@@ -129,19 +133,42 @@ class BeamDecoder:
         self.tables, self.n_free = self.tables[::-1], self.n_free[::-1]
 
     # -------------------------------------------------------------- search --
-    def decode(self, enc, prompt, max_new: int, suppress=None, length_penalty: float = 1.0):
-        """enc [n, frames, d] (bf16 tensor, or its bits in numpy), prompt int [n, P].  Up to max_new tokens a
-        beam; per request its hypotheses, best score / length ** length_penalty first."""
-        torch, cfg, n, W = self.torch, self.cfg, self.n, self.W
-        prompt = np.asarray(prompt, np.int32)
-        if prompt.shape[1] + max_new > min(self.max_ctx, cfg.max_pos):
+    def _inputs(self, enc, prompt, max_new, suppress):
+        """The arguments of decode, checked on the host: the kernels read them by address and index with them."""
+        torch, cfg, n = self.torch, self.cfg, self.n
+        device = self.err.device
+        prompt = np.asarray(prompt)
+        if prompt.ndim != 2 or prompt.shape[0] != n or prompt.shape[1] < 1 or prompt.dtype.kind not in "iu":
+            raise ValueError(f"prompt must hold {n} rows of at least one token id")
+        if prompt.min() < 0 or prompt.max() >= cfg.vocab:
+            raise ValueError("a prompt's token id is outside the vocabulary")
+        if max_new < 0 or prompt.shape[1] + max_new > min(self.max_ctx, cfg.max_pos):
             raise ValueError("prompt and new tokens exceed the positions of the cache")
+        shape = (n, cfg.enc_frames, cfg.d_model)
+        if isinstance(enc, np.ndarray):
+            if enc.shape != shape or enc.dtype.itemsize != 2:
+                raise ValueError(f"enc must be the bits of bf16 values of shape {shape}")
+            enc = _bf16_tensor(enc, self.device)
+        elif tuple(enc.shape) != shape or enc.dtype != torch.bfloat16 or enc.device != device:
+            raise ValueError(f"enc must be a bf16 tensor of shape {shape} on {device}")
+        if suppress is not None:
+            if tuple(suppress.shape) != (cfg.vocab,) or suppress.dtype not in (torch.uint8, torch.bool) or suppress.device != device:
+                raise ValueError(f"suppress must be a uint8 or bool tensor of {cfg.vocab} entries on {device}")
+            suppress = suppress.contiguous()
+        return enc, prompt.astype(np.int32), suppress
+
+    def decode(self, enc, prompt, max_new: int, suppress=None, length_penalty: float = 1.0):
+        """enc [n, frames, d] (bf16 tensor, or its bits in numpy), prompt int [n, P], suppress (optional)
+        uint8 or bool [vocab], nonzero for ids that are never proposed.  Up to max_new tokens a beam; per
+        request its hypotheses, best score / length ** length_penalty first."""
+        torch, cfg, n, W = self.torch, self.cfg, self.n, self.W
+        enc, prompt, suppress = self._inputs(enc, prompt, max_new, suppress)
         self.err.zero_()
         self.free.copy_(torch.arange(self.n_blocks, device=self.device))
         self.n_free[0].fill_(self.n_blocks)
         self.tables[0].fill_(-1)
         self.lens[0].zero_()
-        self._encode(_bf16_tensor(enc, self.device) if isinstance(enc, np.ndarray) else enc)
+        self._encode(enc)
         # every beam runs the prompt; the first selection has one live beam, and its children share the blocks
         tokens = torch.as_tensor(prompt, device=self.device).repeat_interleave(W, 0).contiguous()
         score = torch.full((n, W), -float("inf"), device=self.device)
