@@ -163,6 +163,8 @@ class BeamDecoder:
         request its hypotheses, best score / length ** length_penalty first."""
         torch, cfg, n, W = self.torch, self.cfg, self.n, self.W
         enc, prompt, suppress = self._inputs(enc, prompt, max_new, suppress)
+        if max_new == 0:
+            return [[Hypothesis([], 0.0, False)] for _ in range(n)]
         self.err.zero_()
         self.free.copy_(torch.arange(self.n_blocks, device=self.device))
         self.n_free[0].fill_(self.n_blocks)

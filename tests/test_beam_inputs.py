@@ -58,3 +58,8 @@ def test_construction_refuses(kw):
     args = {"n_req": 1, "beams": 2, "max_ctx": 16, **kw}
     with pytest.raises(ValueError):
         BeamDecoder(cfg, {}, device="cpu", **args)
+
+
+def test_no_new_tokens_is_an_empty_transcript(decoder):
+    found = decoder.decode(**{**_good(), "max_new": 0})
+    assert [[(h.tokens, h.score, h.ended) for h in r] for r in found] == [[([], 0.0, False)]] * 2
