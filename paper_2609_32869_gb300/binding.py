@@ -147,10 +147,12 @@ def _check(name, status):
 
 def _ptr(t):
     """Device pointer of a torch tensor (or an int / None)."""
+    if t is None or t.__class__ is int:
+        return t
     try:
         return t.data_ptr()
     except AttributeError:
-        if t is None or isinstance(t, int):
+        if isinstance(t, int):  # of a derived class
             return t
         raise
 

@@ -1,0 +1,34 @@
+"""How the binding takes a device pointer: a tensor's, an address or none (CPU)."""
+import enum
+import sys
+
+import pytest
+
+from paper_2609_32869_gb300 import binding as B
+
+torch = pytest.importorskip("torch")
+
+
+def test_kinds():
+    t = torch.zeros(4)
+    address = enum.IntEnum("Address", {"a": 4096})
+    assert B._ptr(t) == t.data_ptr() and B._ptr(t[2:]) == t.data_ptr() + 8
+    assert B._ptr(None) is None and B._ptr(4096) == 4096 and B._ptr(address.a) == 4096
+    with pytest.raises(AttributeError):
+        B._ptr("4096")
+
+
+@pytest.mark.skipif(not hasattr(sys, "monitoring"), reason="needs sys.monitoring")
+@pytest.mark.parametrize("value", [None, 4096])
+def test_no_exception_on_the_way(value):
+    """A step passes several optional pointers as None; an exception caught inside costs each of them 0.35 us."""
+    mon, tool, raised = sys.monitoring, 4, []
+    mon.use_tool_id(tool, "pointers")
+    try:
+        mon.register_callback(tool, mon.events.RAISE, lambda *a: raised.append(a))
+        mon.set_events(tool, mon.events.RAISE)
+        B._ptr(value)
+        mon.set_events(tool, 0)
+    finally:
+        mon.free_tool_id(tool)
+    assert not raised
