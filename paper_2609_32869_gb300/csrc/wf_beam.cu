@@ -546,12 +546,12 @@ constexpr int kSelCarve = 60;  // percent: three of the first kernel's CTAs
 template <typename T>
 static bool select_ready(const void **segment, const void **join) {
   *segment = reinterpret_cast<const void *>(beam_segment_kernel<T>), *join = reinterpret_cast<const void *>(beam_join_kernel<T>);
-  static const bool ok = [](const void *a, const void *b) {
-    return cudaFuncSetAttribute(b, cudaFuncAttributeMaxDynamicSharedMemorySize, WF_MAX_BEAMS * kJoinAhead * 512) == cudaSuccess &&
-           cudaFuncSetAttribute(a, cudaFuncAttributePreferredSharedMemoryCarveout, kSelCarve) == cudaSuccess &&
-           cudaFuncSetAttribute(b, cudaFuncAttributePreferredSharedMemoryCarveout, kSelCarve) == cudaSuccess;
-  }(*segment, *join);
-  return ok;
+  static PerDevice ready;
+  return ready.get(current_device(), [&]() -> int {
+    return cudaFuncSetAttribute(*join, cudaFuncAttributeMaxDynamicSharedMemorySize, WF_MAX_BEAMS * kJoinAhead * 512) == cudaSuccess &&
+           cudaFuncSetAttribute(*segment, cudaFuncAttributePreferredSharedMemoryCarveout, kSelCarve) == cudaSuccess &&
+           cudaFuncSetAttribute(*join, cudaFuncAttributePreferredSharedMemoryCarveout, kSelCarve) == cudaSuccess;
+  });
 }
 constexpr int kSelMaxVocab = 1 << 22;  // its terms in units of 2^-40 stay below 2^63
 // Segments of a row: as many as make one wave of CTAs, or more of at most 8 tiles.

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/wf.h"
+#include "wf_per_device.h"
 
 namespace wf {
 
@@ -84,6 +85,11 @@ inline cudaError_t launch_pdl(const void *fn, dim3 grid, dim3 block, size_t smem
   return cudaLaunchKernelExC(&cfg, fn, args);
 }
 
+// The device that a call runs on; -1 where there is none.
+inline int current_device() {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess ? dev : -1;
+}
 inline cudaError_t prefer_shared(const void *fn) {
   return cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }

@@ -699,16 +699,18 @@ static AtPlan at_plan(int64_t n_seq, int64_t heads, int64_t rows, int max_len) {
 template <typename T, int G, int NT>
 static cudaError_t launch(const Kv4AttnParams &p, cudaStream_t s) {
   using S = AtShape<G, NT>;
-  static const cudaError_t ready = [] {
-    const void *fn = reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>);
-    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-    return e != cudaSuccess ? e : prefer_shared(fn);
-  }();
-  if (ready != cudaSuccess) return ready;
+  static PerDevice ready;
+  const void *fn = reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>);
+  cudaError_t e = cudaSuccess;
+  if (!ready.get(current_device(), [&]() -> int {
+        e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+        if (e == cudaSuccess) e = prefer_shared(fn);
+        return e == cudaSuccess;
+      }))
+    return e;
   const dim3 grid(p.n_seq * p.pool.heads, p.chunks, p.row_groups);
   void *args[] = {const_cast<Kv4AttnParams *>(&p)};
-  cudaError_t e = launch_pdl(reinterpret_cast<const void *>(kv4_attention_kernel<T, G, NT>), grid, kAtThreads, S::kSmem, args, s,
-                             p.cluster ? p.chunks : 1);
+  e = launch_pdl(fn, grid, kAtThreads, S::kSmem, args, s, p.cluster ? p.chunks : 1);
   if (e == cudaSuccess && p.chunks > 1 && !p.cluster)
     e = launch_pdl(reinterpret_cast<const void *>(kv4_join_kernel<T, G, NT>), dim3(grid.x, p.row_groups, NT * 8), kAtThreads, 0, args, s);
   return e;

@@ -640,13 +640,12 @@ __global__ void __launch_bounds__(kReorderThreads) beam_moves_kernel(const Reord
 }
 
 static int sm_count() {
-  static const int n = [] {
-    int dev = 0, v = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-      return 0;
-    return v;
-  }();
-  return n;
+  static PerDevice count;
+  const int dev = current_device();
+  return count.get(dev, [&] {
+    int v = 0;
+    return cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess ? v : 0;
+  });
 }
 
 }  // namespace wf
