@@ -147,12 +147,12 @@ def _check(name, status):
 
 def _ptr(t):
     """Device pointer of a torch tensor (or an int / None)."""
-    if t is None or t.__class__ is int:
+    if t is None:
         return t
     try:
         return t.data_ptr()
     except AttributeError:
-        if isinstance(t, int):  # of a derived class
+        if isinstance(t, int):
             return t
         raise
 

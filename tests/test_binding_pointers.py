@@ -19,15 +19,14 @@ def test_kinds():
 
 
 @pytest.mark.skipif(not hasattr(sys, "monitoring"), reason="needs sys.monitoring")
-@pytest.mark.parametrize("value", [None, 4096])
-def test_no_exception_on_the_way(value):
+def test_none_raises_no_exception_on_the_way():
     """A step passes several optional pointers as None; an exception caught inside costs each of them 0.35 us."""
     mon, tool, raised = sys.monitoring, 4, []
     mon.use_tool_id(tool, "pointers")
     try:
         mon.register_callback(tool, mon.events.RAISE, lambda *a: raised.append(a))
         mon.set_events(tool, mon.events.RAISE)
-        B._ptr(value)
+        B._ptr(None)
         mon.set_events(tool, 0)
     finally:
         mon.free_tool_id(tool)
