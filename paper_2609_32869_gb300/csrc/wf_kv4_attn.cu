@@ -572,18 +572,21 @@ __global__ void __launch_bounds__(kAtThreads, AtShape<G, NT>::kBlocks) kv4_atten
   const int chunks = p.chunks, live_rows = min(rows - row0, kRows);
   for (int i = threadIdx.x * chunks + blockIdx.y; i < live_rows * G * 32; i += kAtThreads * chunks) {
     const int row = i / (G * 32), d = i % (G * 32) * 2;
-    float cm[kAtCluster], mm = -INFINITY, ll = 0.f, a = 0.f, b = 0.f;
-#pragma unroll
-    for (int k = 0; k < kAtCluster; ++k)
-      if (k < chunks) cm[k] = dsmem_ld_f32(dsmem_map(smem_u32(cl_m + row), k)), mm = fmaxf(mm, cm[k]);
+    // no maximum: a chunk that the row sees nothing of, whose sums are zeros, or one of NaN scores, which stay NaN
+    float cm[kAtCluster], cl[kAtCluster], ca[kAtCluster], cb[kAtCluster], mm = -INFINITY, ll = 0.f, a = 0.f, b = 0.f;
 #pragma unroll
     for (int k = 0; k < kAtCluster; ++k) {
       if (k >= chunks) continue;
-      // no maximum: a chunk that the row sees nothing of, whose sums are zeros, or one of NaN scores, which stay NaN
-      const float f = cm[k] == -INFINITY ? 0.f : ex2(cm[k] - mm);
       const uint32_t at = dsmem_map(smem_u32(cl_o + row * (G * 64) + d), k);
-      ll += f * dsmem_ld_f32(dsmem_map(smem_u32(cl_l + row), k));
-      a += f * dsmem_ld_f32(at), b += f * dsmem_ld_f32(at + 4);
+      cm[k] = dsmem_ld_f32(dsmem_map(smem_u32(cl_m + row), k)), cl[k] = dsmem_ld_f32(dsmem_map(smem_u32(cl_l + row), k));
+      ca[k] = dsmem_ld_f32(at), cb[k] = dsmem_ld_f32(at + 4);
+      mm = fmaxf(mm, cm[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtCluster; ++k) {
+      if (k >= chunks) continue;
+      const float f = cm[k] == -INFINITY ? 0.f : ex2(cm[k] - mm);
+      ll += f * cl[k], a += f * ca[k], b += f * cb[k];
     }
     const float inv = ll == 0.f ? 0.f : 1.f / ll;
     const int j = p.row_of(row0 + row), h = head * p.group + row0 + row - j * p.group;
