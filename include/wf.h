@@ -394,6 +394,7 @@ size_t wf_kv4_block_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_d
  *                                 [d_offsets[i], d_offsets[i + 1])
  *   d_slots    int32 [slots_cap]  out: of each new token, block * block_size +
  *                                 position % block_size; -1 after the last
+ *                                 (slots_cap < 2^31 - 2^20)
  *   d_len      int32 [n]          out: new length if granted, else the old one
  *   d_n_free_out int32 [1]        out: ids left
  * Requests are granted in order; the first whose blocks or slots do not fit,
@@ -430,8 +431,8 @@ wf_status wf_kv4_load(const wf_kv4_pool *pool, int32_t layer, const int32_t *d_s
  *           sequences may share blocks, and stride 0 shares one row)
  *   d_len   int32 [n_seq]  positions held; the rps rows are the last of them
  *           when causal: row j sees len - (rps - 1 - j) positions, else len
- *   max_len a bound on d_len; longer sequences are cut to it
- *           (WF_DEV_ERR_CAPACITY)
+ *   max_len a bound on d_len, at most 2^31 - 1024; longer sequences are cut
+ *           to it (WF_DEV_ERR_CAPACITY)
  *   d_out   dtype [n_seq * rps][n_heads * head_dim]
  * Strides are in elements, multiples of 8, pointers 16-byte aligned; d_out is
  * not d_q.  A row that sees nothing is zeros; a block id outside the pool is not read and its

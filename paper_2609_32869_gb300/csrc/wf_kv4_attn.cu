@@ -61,6 +61,7 @@ constexpr int kAtThreads = kAtWarps * 32;
 constexpr int kAtTile = 64;    // positions of a warp's step
 constexpr int kAtCluster = 8;  // chunks that a cluster joins
 constexpr int kAtShort = 2048; // positions of a chunk that two CTAs an SM may have
+constexpr int kAtLongest = INT_MAX - 1023;  // a step past the last position is still an int
 
 // None of these is volatile: the compiler may interleave independent chains.
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
@@ -723,7 +724,8 @@ extern "C" {
 
 size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                       int32_t max_len) {
-  if (n_seq <= 0 || rps <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || (head_dim != 64 && head_dim != 128))
+  if (n_seq <= 0 || rps <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || max_len > kAtLongest ||
+      (head_dim != 64 && head_dim != 128))
     return 0;
   const AtPlan a = at_plan(n_seq, n_kv_heads, static_cast<int64_t>(rps) * (n_heads / n_kv_heads), max_len);
   return a.chunks > kAtCluster ? static_cast<size_t>(a.units * a.chunks * a.tiles * 8) * (head_dim + 2) * sizeof(float) : 0;
@@ -744,7 +746,8 @@ wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d
   // every position up to max_len needs a table column (stride 0: one row that the caller made long enough)
   if (table_stride && static_cast<int64_t>(table_stride) * pool->block_size < max_len) return WF_ERR_INVALID;
   const int64_t rows = static_cast<int64_t>(rps) * (n_heads / pool->n_kv_heads);
-  if (static_cast<int64_t>(n_seq) * pool->n_kv_heads > INT32_MAX || rows > 65535 * 8LL || n_heads / pool->n_kv_heads > 4096)
+  if (static_cast<int64_t>(n_seq) * pool->n_kv_heads > INT32_MAX || rows > 65535 * 8LL || n_heads / pool->n_kv_heads > 4096 ||
+      max_len > kAtLongest)
     return WF_ERR_UNSUPPORTED;
   p.block_bytes = static_cast<uint32_t>(kv4_block_bytes(pool->block_size, pool->n_kv_heads, pool->head_dim));
   p.q = d_q, p.out = d_out, p.q_stride = q_stride, p.out_stride = out_stride;

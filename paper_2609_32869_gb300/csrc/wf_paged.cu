@@ -19,6 +19,7 @@ struct PlanParams {
 constexpr int kPlanThreads = 256;
 constexpr int kPlanOwned = 64;  // requests of one CTA
 constexpr int kPlanRequests = 1 << 16;  // every CTA reads all lengths: n^2 / 64 reads
+constexpr int kPlanSlots = INT32_MAX - (1 << 20);  // a grid's step past the last slot is still an int
 
 // Inclusive scan over the CTA of two counts at a time, and their totals.
 __device__ __forceinline__ void block_scan2(long long &a, long long &b, long long (*sm)[2], long long &ta, long long &tb) {
@@ -669,7 +670,7 @@ wf_status wf_page_plan(const int32_t *d_old_len, const int32_t *d_new_len, int32
   if (block_size != 16 && block_size != 32 && block_size != 64) return WF_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(n_blocks) * block_size > INT32_MAX || static_cast<int64_t>(table_stride) * block_size > INT32_MAX)
     return WF_ERR_INVALID;
-  if (n > kPlanRequests) return WF_ERR_UNSUPPORTED;
+  if (n > kPlanRequests || slots_cap > kPlanSlots) return WF_ERR_UNSUPPORTED;
   const int sms = sm_count();
   if (!sms) return WF_ERR_CUDA;
   PlanParams p = {d_old_len, d_new_len, d_free,     d_n_free,     d_table,   d_offsets, d_slots, d_len,
