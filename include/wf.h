@@ -458,7 +458,8 @@ size_t wf_kv4_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_head
  * the score d_scores[i * beams + w], the sum of its log-probabilities (-inf:
  * not in use).  A token's score is score + ((logit - max) - log(sum)) in fp32,
  * max the row's largest logit and sum that of exp(logit - max); ids with a nonzero d_suppress entry (nullable uint8
- * [vocab]) and NaN logits count as -inf.  Each beam proposes its 2 beams best
+ * [vocab]) and NaN logits count as -inf; a row whose largest logit is +inf has
+ * no scores and proposes nothing.  Each beam proposes its 2 beams best
  * tokens (ties: the lower id); of all proposals the 2 beams best are ranked
  * (ties: the lower beam, then its better token).  Then
  *   d_token, d_parent int32, d_score fp32 [n_req][beams]  the first `beams`

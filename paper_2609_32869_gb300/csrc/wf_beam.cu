@@ -85,7 +85,6 @@ template <typename T>
 struct Logits;
 template <>
 struct Logits<float> {
-  using Half = __half;  // unused
   static constexpr int kVec = 4;
   static __device__ __forceinline__ float one(const uint4 *v, int i) { return reinterpret_cast<const float *>(v)[i]; }
   static __device__ __forceinline__ void unpack(uint4 v, float *x) {
@@ -94,7 +93,6 @@ struct Logits<float> {
 };
 template <typename T>
 struct Logits16 {
-  using Half = T;
   static constexpr int kVec = 8;
   static __device__ __forceinline__ float one(const uint4 *v, int i) { return Kv4Type<T>::lo(reinterpret_cast<const uint16_t *>(v)[i]); }
   static __device__ __forceinline__ void unpack(uint4 v, float *x) {
@@ -113,8 +111,8 @@ template <typename T>
 __device__ __noinline__ uint4 edge_vector(const T *src, int id, int V) {
   constexpr int kVec = Logits<T>::kVec, kBits = 128 / kVec;
   uint32_t w[4];
-  const float low = -INFINITY;
-  const uint32_t none = kBits == 32 ? 0xff800000u : Kv4Type<typename Logits<T>::Half>::pack(low, low) & 0xffffu;
+  uint32_t none = 0xff800000u;  // -inf in fp32
+  if constexpr (kBits == 16) none = Kv4Type<T>::pack(-INFINITY, -INFINITY) & 0xffffu;
   for (int i = 0; i < 4; ++i) {
     w[i] = 0;
     for (int e = 0; e < kVec / 4; ++e) {
@@ -561,7 +559,7 @@ struct SelectPlan {
 static SelectPlan select_plan(long long rows, int V, bool wide) {
   const int all = (V + 7 + kSelTile - 1) / kSelTile;  // 15 bytes of skew may push a row's end into another tile
   SelectPlan a;
-  const long long most = std::min<long long>(all, std::max<long long>(1, 152 * kSelBlocks / ((rows + kSelWarps - 1) / kSelWarps)));
+  const long long most = std::min<long long>(all, std::max<long long>(1, kSms * kSelBlocks / ((rows + kSelWarps - 1) / kSelWarps)));
   a.tiles = static_cast<int>(std::min<long long>(kSelTiles, (all + most - 1) / most));
   a.segments = (all + a.tiles - 1) / a.tiles;
   a.groups = all * (wide ? 8 : 4);

@@ -6,9 +6,14 @@
 #include <stdint.h>
 
 #include "../../include/wf.h"
+#include "wf_internal.h"
 #include "wf_per_device.h"
 
 namespace wf {
+
+// SMs that a call's work is cut for.  A constant: the scratch sizes depend on
+// the cut and are asked for without a device.
+constexpr int kSms = 152;
 
 // A record: 16 positions of one group of 64 values, keys and values.
 //   key codes    [position][32 bytes], dims 2b and 2b + 1 in byte b (low nibble first)
@@ -89,9 +94,6 @@ inline cudaError_t launch_pdl(const void *fn, dim3 grid, dim3 block, size_t smem
 inline int current_device() {
   int dev = -1;
   return cudaGetDevice(&dev) == cudaSuccess ? dev : -1;
-}
-inline cudaError_t prefer_shared(const void *fn) {
-  return cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 

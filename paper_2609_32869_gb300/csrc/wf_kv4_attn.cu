@@ -43,7 +43,7 @@ struct Kv4AttnParams {
   void *out;
   long long q_stride, out_stride;
   const int32_t *table, *len;
-  int table_stride, n_seq, rps, n_heads, group, causal, max_len;
+  int table_stride, n_seq, rps, group, causal, max_len;
   uint32_t group_inv;  // 2^32 / group, rounded up (group > 1)
   float scale;
   // A unit is (sequence, key/value head, group of query rows); it is cut into
@@ -695,8 +695,8 @@ static AtPlan at_plan(int64_t n_seq, int64_t heads, int64_t rows, int max_len) {
     a.chunk = static_cast<int>(std::min<int64_t>(chunk, 1 << 30));
     a.chunks = static_cast<int>((longest + a.chunk - 1) / a.chunk);
   };
-  cut(152 * 2);
-  if (a.chunks > kAtCluster || a.chunk > kAtShort) cut(152 * 8);
+  cut(kSms * 2);
+  if (a.chunks > kAtCluster || a.chunk > kAtShort) cut(kSms * 8);
   return a;
 }
 
@@ -708,7 +708,7 @@ static cudaError_t launch(const Kv4AttnParams &p, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   if (!ready.get(current_device(), [&]() -> int {
         e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-        if (e == cudaSuccess) e = prefer_shared(fn);
+        if (e == cudaSuccess) e = prefer_max_shared(fn);
         return e == cudaSuccess;
       }))
     return e;
@@ -752,7 +752,7 @@ wf_status wf_kv4_attention(const wf_kv4_pool *pool, int32_t layer, const void *d
   p.block_bytes = static_cast<uint32_t>(kv4_block_bytes(pool->block_size, pool->n_kv_heads, pool->head_dim));
   p.q = d_q, p.out = d_out, p.q_stride = q_stride, p.out_stride = out_stride;
   p.table = d_table, p.len = d_len, p.table_stride = table_stride;
-  p.n_seq = n_seq, p.rps = rps, p.n_heads = n_heads, p.group = n_heads / pool->n_kv_heads;
+  p.n_seq = n_seq, p.rps = rps, p.group = n_heads / pool->n_kv_heads;
   p.group_inv = static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
   p.causal = causal != 0, p.max_len = max_len, p.scale = scale, p.err = d_err;
   const AtPlan a = at_plan(n_seq, pool->n_kv_heads, rows, max_len);

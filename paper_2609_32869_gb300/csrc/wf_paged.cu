@@ -283,8 +283,9 @@ __device__ __forceinline__ void quantise_rows(const uint4 (&w)[8], int lane, uin
   }
 }
 
-// 8 codes against (s, z), rounded once: s (c - 8) has at most 15 bits, and the
-// sum that the fused operation rounds is what fp32 would hold first.
+// 8 codes against (s, z), rounded once: s (c - 8) has at most 15 bits, and fp32
+// holds the sum that the fused operation rounds unless the two span more than
+// its 24.
 __device__ __forceinline__ uint4 dequantise8(uint32_t w, uint32_t sz, __nv_bfloat16) {
   uint32_t r[4];
 #pragma unroll
