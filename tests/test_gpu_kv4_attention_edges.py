@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import beam as ob
-from test_gpu_beam_ops import _check_rows, _dev, _err, _filled, _i32, _pool
+from test_gpu_beam_ops import ATT, _attend_case, _check_rows, _dev, _err, _filled, _i32, _pool, _rows_of
 
 pytestmark = pytest.mark.gpu
 
@@ -167,7 +167,6 @@ def test_every_position_counts_once(rps, heads, dim, bs, causal, lens, dtype):
     cache.raw[..., 1024:] = pairs.view(np.uint8).reshape(*cache.raw.shape[:3], 128)
     q = np.zeros((len(lens) * rps, heads * dim), np.float32)
     got, _ = _run(cache, lens, q, rps, heads, causal, 1.0, dtype, table, max(lens))
-    from test_gpu_beam_ops import _rows_of
     u = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -11
     for s, n in enumerate(lens):
         for h in range(heads):
@@ -179,3 +178,58 @@ def test_every_position_counts_once(rps, heads, dim, bs, causal, lens, dtype):
                 tol = np.abs(want) * (u + 2.0 ** -22) + (2.0 ** -25 if dtype == "f16" else 0)
                 off = np.abs(got[s * rps + j, h * dim:(h + 1) * dim] - want)
                 assert (off <= tol).all(), (s, h, j, off.max())
+
+
+# --------------------------------------------------- every rounding, and no more --
+def _pairs(cache, table, length, head):
+    """(s, z) of keys and of values [length, groups] each."""
+    pos = np.arange(length)
+    rec = cache.raw[table[pos // cache.bs], head * cache.groups:(head + 1) * cache.groups, pos % cache.bs // 16]
+    out = []
+    for is_v in (0, 1):
+        at = np.array([ob.scale_place(p, is_v) for p in range(16)])[pos % 16]
+        raw = np.stack([rec[np.arange(length), :, at + b] for b in range(4)], -1)
+        sz = ob.from_bits16(np.ascontiguousarray(raw).view(np.uint16), cache.dtype).astype(np.float64)
+        out += [sz[..., 0], sz[..., 1]]
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("i", range(len(ATT)))
+def test_attention_is_off_by_its_roundings_alone(i, dtype):
+    """out = sum w_j (sc_j + z_j) with sc = s (c - 8).  A score's error d_j moves the output by sum w_j d_j (v_j - out).
+    d_j: products of queries with codes of up to 8 around a bias that is taken off again (136 for bf16, 72 for half of
+    them in fp16), eight additions each to 2^-24 of at most s B sum|q|, the same for z; and 2^-22 of the score and of its
+    exponential.  Weights times s are rounded once (2^-8 for bf16, 2^-11 for fp16 or 2^-25 of s), the output once; the
+    tensor products of a warp and the joins add n / 64 times to 2^-23."""
+    rps, hq, hkv, dim, bs, causal, lens = ATT[i]
+    cache, table, q = _attend_case(i, dtype)
+    scale, g = dim ** -0.5, hq // hkv
+    got, _ = _run(cache, lens, q, rps, hq, causal, scale, dtype, table, max(1, max(lens)))
+    u, bias = (2.0 ** -8, 144) if dtype == "bf16" else (2.0 ** -11, 80)
+    worst = 0
+    for s, n in enumerate(lens):
+        for head in range(hkv):
+            k, v = _rows_of(cache, table[s], n, head)
+            ks, kz, vs, vz = _pairs(cache, table[s], n, head)
+            z = vz.repeat(64, 1)
+            sc = v - z
+            for j in range(rps):
+                m = max(n - (rps - 1 - j) if causal else n, 0)
+                for e in range(g):
+                    cols = slice((head * g + e) * dim, (head * g + e + 1) * dim)
+                    out, row = got[s * rps + j, cols], q[s * rps + j, cols].astype(np.float64)
+                    if not m:
+                        assert (out == 0).all()
+                        continue
+                    x = k[:m] @ row * scale
+                    p = np.exp(x - x.max())
+                    w, size = p / p.sum(), np.abs(row).reshape(-1, 64).sum(1)
+                    d = 8 * 2.0 ** -24 * scale * ((2 * bias * ks[:m] + np.abs(kz[:m])) @ size) + 2.0 ** -22 * (1 + np.abs(x))
+                    want = w @ v[:m]
+                    tol = 1.01 * u * np.abs(want) + u * (w @ np.abs(sc[:m])) + (w * d) @ np.abs(v[:m] - want) \
+                        + m / 64 * 2.0 ** -23 * (w @ (np.abs(sc[:m]) + np.abs(z[:m])))
+                    if dtype == "f16":
+                        tol = tol + 2.0 ** -25 * (1 + np.abs(sc[:m]).sum(0) / p.sum())
+                    worst = max(worst, (np.abs(out - want) / tol).max())
+    assert worst <= 1, worst
