@@ -140,13 +140,14 @@ __device__ __forceinline__ int clamp_len(const Kv4AttnParams &p, int len) { retu
 // for) and keeps a running maximum, sum and weighted values.  A CTA's warps
 // take a unit, or a chunk of one, in turns and join in order; up to 8 chunks
 // join over a cluster, more by a second kernel.
-//   96 sequences x 9 rows x 20 heads, 1500 positions, bf16: 71 us, 3.0 TB/s,
-//     bound by issue (59% of the slots at 16 warps an SM; half of the loop's
-//     instructions unpack nibbles)
+//   96 sequences x 9 rows x 20 heads, 1500 positions, bf16: 70 us, 3.0 TB/s,
+//     by instructions and their latencies (58% of the slots at 15 warps an SM;
+//     half of the loop's instructions unpack nibbles) and a last, sixth-full
+//     round of CTAs
 //   80 sequences of 4 to 448 positions, 20 heads, bf16: 13.7 us, by the
 //     instructions before and after the loop
 //   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 38 us,
-//     3.3 TB/s, by issue at 12 warps an SM
+//     3.3 TB/s, likewise (52% of the slots at 9 warps an SM)
 //   5 rows of one sequence, 1500 positions, 20 heads, bf16: 6 us, by the launch
 //     and one chain of reads
 // One wave of CTAs that go on to their next unit, its first records on their way
@@ -683,10 +684,10 @@ static AtPlan at_plan(int64_t n_seq, int64_t heads, int64_t rows, int max_len) {
   // A CTA's four warps take at least 64 positions each.  Short sequences: cut
   // into even chunks, a cluster each, until there are two CTAs an SM, for a
   // cluster stays until its last is done (1500 positions, 20 heads: 50 sequences
-  // x 9 rows 41 us, 8 x 5 rows 10.1; cut until there are eight CTAs an SM 54 and
-  // 14.1).  Long ones: eight CTAs an SM, so that SMs whose sequences are short
+  // x 9 rows 41 us, 8 x 5 rows 10.3; cut until there are eight CTAs an SM 54 and
+  // 13.8).  Long ones: eight CTAs an SM, so that SMs whose sequences are short
   // find other work (12 sequences of 3000 to 9000 positions, 32 heads on 8: 32 us
-  // against 34; 6 of 5000 to 65001: 37 against 105).
+  // against 34; 6 of 5000 to 65001: 38 against 108).
   const auto cut = [&](int64_t want) {
     const int64_t least = kAtWarps * kAtTile, longest = max_len;
     const int64_t per = std::max(least, (a.units * longest + want - 1) / want);

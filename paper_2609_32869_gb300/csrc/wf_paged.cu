@@ -43,8 +43,8 @@ __device__ __forceinline__ void block_scan2(long long &a, long long &b, long lon
 // prefixes of the requests it owns, i = blockIdx mod gridDim; then it fills
 // those requests' table columns and slots.  Counts only grow along the
 // requests, so the granted ones are a prefix.  Bound by its chain of reads
-// (lengths, ids, slots) and the launch: 4.7 us for one token each of 80
-// requests, 7.3 us for 512 prompts of up to 4096 tokens (by passes of 256
+// (lengths, ids, slots) and the launch: 4.8 us for one token each of 80
+// requests, 7.2 us for 512 prompts of up to 4096 tokens (by passes of 256
 // requests 9.9).
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanParams p) {
   pdl_wait();
@@ -479,7 +479,7 @@ constexpr int kReorderThreads = 256;
 // and the copies of last blocks that the second kernel makes.  MAXW: 4, 8 or
 // 16, the least that holds the beams; a column's comparisons grow with its
 // square.  Bound by its chain of reads (parents, lengths, columns) and, with
-// the second kernel, by two launches: 11.4 us for one request's 5 beams.
+// the second kernel, by two launches: 11.7 to 12.6 us for one request's 5 beams.
 template <int MAXW>
 __global__ void __launch_bounds__(kReorderThreads) beam_tables_kernel(const ReorderParams p) {
   pdl_wait();
@@ -585,8 +585,8 @@ __global__ void __launch_bounds__(kReorderThreads) beam_tables_kernel(const Reor
 
 // grid (n_req * W, layers): the copies of last blocks, 16 positions at a time;
 // in layer 0 the first CTA of a request also pushes its freed ids.  16 requests
-// x 5 beams move 41 MB in 32 layers; with the first kernel 12.6 us (with one
-// read in flight a thread instead of six 14.3).
+// x 5 beams move 41 MB in 32 layers; with the first kernel 12.7 to 14.1 us
+// (with one read in flight a thread instead of six 1.7 more).
 __global__ void __launch_bounds__(kReorderThreads) beam_moves_kernel(const ReorderParams p) {
   pdl_wait();
   pdl_launch_dependents();
