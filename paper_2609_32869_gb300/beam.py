@@ -146,7 +146,7 @@ class BeamDecoder:
             raise ValueError("prompt and new tokens exceed the positions of the cache")
         shape = (n, cfg.enc_frames, cfg.d_model)
         if isinstance(enc, np.ndarray):
-            if enc.shape != shape or enc.dtype.itemsize != 2:
+            if enc.shape != shape or enc.dtype.kind not in "iu" or enc.dtype.itemsize != 2:
                 raise ValueError(f"enc must be the bits of bf16 values of shape {shape}")
             enc = _bf16_tensor(enc, self.device)
         elif tuple(enc.shape) != shape or enc.dtype != torch.bfloat16 or enc.device != device:

@@ -38,6 +38,7 @@ BAD = {
     "more positions than there are": dict(max_new=13),
     "frames for one request": dict(enc=np.zeros((1, CFG.enc_frames, CFG.d_model), np.uint16)),
     "frames of four bytes": dict(enc=np.zeros((2, CFG.enc_frames, CFG.d_model), np.float32)),
+    "frames as numpy's fp16, which is not the bits of bf16": dict(enc=np.zeros((2, CFG.enc_frames, CFG.d_model), np.float16)),
     "too many frames": dict(enc=np.zeros((2, CFG.enc_frames + 1, CFG.d_model), np.uint16)),
     "a tensor of fp32 frames": dict(enc=_tensor(dtype=torch.float32)),
     "a tensor of fp16 frames": dict(enc=_tensor(dtype=torch.float16)),
