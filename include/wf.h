@@ -496,6 +496,165 @@ wf_status wf_beam_reorder(const wf_kv4_pool *pool, const int32_t *d_table_in, in
                           uint32_t *d_err, void *stream);
 size_t wf_beam_reorder_scratch_bytes(int32_t n_req, int32_t beams, int32_t table_stride);
 
+/* ------------------------------------------------------------------------
+ * From a prompt to its first tokens: rotary positions, attention over whole
+ * prompts, and a paged cache in 8 bits beside the one in 4.  These calls take
+ * no handle either; a request's way through them is
+ *   wf_rope              the new queries and keys of a layer,
+ *   wf_prompt_attention  the prompt's rows among themselves,
+ *   wf_kv8_store         its keys and values (slots from wf_page_plan),
+ * and then, token by token, wf_rope, wf_kv8_store and wf_kv8_attention.
+ * ---------------------------------------------------------------------- */
+
+#define WF_ROPE_HALF 0        /* pairs are dims i and i + rot_dim / 2 */
+#define WF_ROPE_INTERLEAVED 1 /* pairs are dims 2 i and 2 i + 1 */
+#define WF_ROPE_MAX_PAIRS 128
+#define WF_ROPE_PLAIN 0  /* f_i = base^(-2 i / rot_dim), pair i of 0 .. rot_dim / 2 - 1 */
+#define WF_ROPE_LINEAR 1 /* f_i / factor */
+#define WF_ROPE_BASE 2   /* the plain ones of base * factor^(rot_dim / (rot_dim - 2)) (rot_dim 2: plain) */
+#define WF_ROPE_WAVES 3  /* by the turns n_i = f_i trained_len / 2 pi of the trained context:
+                            w f_i + (1 - w) f_i / factor, w = clamp((n_i - low) / (high - low), 0, 1) */
+#define WF_ROPE_PARTS 4  /* by a ramp over the pairs: w f_i / factor + (1 - w) f_i,
+                            w = clamp((i - a) / max(b - a, 0.001), 0, 1), a = max(floor(c(high)), 0),
+                            b = min(ceil(c(low)), rot_dim - 1),
+                            c(n) = rot_dim log(trained_len / (2 pi n)) / (2 log(base)) */
+
+typedef struct wf_rope_spec {
+  int32_t head_dim; /* 2 .. 4096 */
+  int32_t rot_dim;  /* the first rot_dim dims of a head turn; even, 2 .. min(head_dim, 256) */
+  int32_t layout;   /* WF_ROPE_HALF or WF_ROPE_INTERLEAVED */
+  int32_t scaling;  /* WF_ROPE_PLAIN .. WF_ROPE_PARTS */
+  double base;      /* above 1 */
+  double factor;    /* at least 1 (any scaling but WF_ROPE_PLAIN) */
+  double trained_len, low, high; /* WF_ROPE_WAVES and WF_ROPE_PARTS: 0 < low < high, trained_len > 0 */
+  double gain;      /* cos and sin are multiplied by it; above 0 */
+} wf_rope_spec;
+
+/* What a spec comes to, a plain value that the caller keeps and passes by
+ * address.  turns[i] is pair i's turn per position, a fraction of 2^64: an
+ * angle is pos * turns[i] in 64-bit integers, so that far positions lose
+ * nothing (2^-32 of a turn, whatever the position). */
+typedef struct wf_rope_table {
+  int32_t head_dim, rot_dim, layout;
+  float gain;
+  uint64_t turns[WF_ROPE_MAX_PAIRS];
+} wf_rope_table;
+
+wf_status wf_rope_init(const wf_rope_spec *spec, wf_rope_table *out);
+
+/* Rotary positions of n rows of queries and keys.  Pair (a, b) of a head in
+ * row i becomes gain (a cos - b sin, a sin + b cos) of the angle d_pos[i] f;
+ * the dims from rot_dim on are copied.  adjoint nonzero: the transposed
+ * turn, which takes the outputs' gradients to the inputs'.
+ *   d_q      dtype [n][n_heads * head_dim] (WF_BF16, WF_F16 or WF_F32)
+ *   d_k      dtype [n][n_kv_heads * head_dim]; null with n_kv_heads 0: queries alone
+ *   d_pos    int32 [n], any value
+ *   d_q_out, d_k_out  as d_q and d_k; an output may be its own input (with the
+ *            same stride), else it overlaps none
+ * Row strides are in elements, at any alignment of the type.  The arithmetic
+ * is fp32, rounded once.  Slices of one fused projection can be given. */
+wf_status wf_rope(const wf_rope_table *table, const void *d_q, int64_t q_stride, int32_t n_heads,
+                  const void *d_k, int64_t k_stride, int32_t n_kv_heads, const int32_t *d_pos,
+                  int32_t n, int32_t dtype, int32_t adjoint, void *d_q_out, int64_t q_out_stride,
+                  void *d_k_out, int64_t k_out_stride, void *stream);
+
+/* Attention of whole prompts, packed one after another: softmax(scale q K^T) V
+ * within each of n_seq sequences, n_heads query heads on n_kv_heads (query
+ * head h reads key/value head h / (n_heads / n_kv_heads)).
+ *   d_q      dtype [n_q][n_heads * head_dim] (WF_BF16 or WF_F16; head_dim 64 or 128)
+ *   d_k, d_v dtype [n_k][n_kv_heads * head_dim]
+ *   d_q_start, d_k_start  int32 [n_seq + 1]  sequence i has the query rows
+ *            d_q_start[i] .. d_q_start[i + 1] - 1 and the keys d_k_start[i] ..
+ *            d_k_start[i + 1] - 1, both ascending; each may be empty
+ *   max_k    a bound on a sequence's keys; what is past it is not seen
+ *            (WF_DEV_ERR_CAPACITY)
+ *   causal   nonzero: of r query rows and t keys, row j sees the first
+ *            t - (r - 1 - j): the queries are the last rows (t > r: keys that
+ *            the request holds already); else every row sees all t
+ *   d_out    dtype [n_q][n_heads * head_dim]
+ *   d_lse    fp32 [n_q][n_heads], nullable: log of the sum of exp(scale q k)
+ * A row that sees nothing is zeros (lse -inf).  Rows before the first
+ * sequence and behind the last are left as they were.  Keys and values that a
+ * row does not see, in its sequence or outside it, do not reach it whatever
+ * they hold.  Starts that descend or leave the buffers are clamped
+ * (WF_DEV_ERR_PAGE).  Strides are in elements, multiples of 8, pointers
+ * 16-byte aligned; d_out overlaps no input.  scale is above 0 and finite.
+ * Scores, softmax and sums are fp32; a weight is rounded to dtype for the
+ * second product.  Results do not depend on timing.  d_scratch (16-byte
+ * aligned) holds wf_prompt_attention_scratch_bytes() bytes and belongs to the
+ * call until it is done. */
+wf_status wf_prompt_attention(const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride,
+                              const void *d_v, int64_t v_stride, const int32_t *d_q_start,
+                              const int32_t *d_k_start, int32_t n_seq, int32_t n_q, int32_t n_k,
+                              int32_t max_k, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                              int32_t dtype, int32_t causal, float scale, void *d_out,
+                              int64_t out_stride, float *d_lse, void *d_scratch,
+                              size_t scratch_bytes, uint32_t *d_err, void *stream);
+size_t wf_prompt_attention_scratch_bytes(int32_t n_seq, int32_t n_q, int32_t max_k, int32_t n_heads,
+                                         int32_t n_kv_heads, int32_t head_dim);
+
+/* A paged cache in 8 bits, laid out in blocks like wf_kv4_pool.  16 positions
+ * of a head are a record: their keys are e4m3 codes (4 bits of exponent, 3 of
+ * fraction; no infinities) times a power of two 2^e, their values likewise
+ * under one of their own.  e is the least integer of -60 .. 36 with
+ * max |x| <= 448 * 2^e over the record; codes are rounded to nearest even, and
+ * what lies beyond 448 * 2^36 is held as that.  Values that are not finite do
+ * not count toward e and read back as NaN, each for itself.
+ * Layout: [block][head][block_size / 16][32 * head_dim + 16 bytes].  A record
+ * holds, for every 64 dims, 1024 bytes of key codes [position][dim] and 1024 of
+ * value codes: of dim d and position p the byte
+ *   512 (d/2 % 2) + 64 (d/8) + 16 (p/2 % 4) + 8 (d % 2) + 4 (p/8) + 2 (d/4 % 2) + p % 2;
+ * then 2^e of the keys and 2^e of the values in fp32 and 8 bytes of zeros. */
+typedef struct wf_kv8_pool {
+  void *d_base;         /* 16-byte aligned */
+  int64_t layer_stride; /* bytes, a multiple of 16; 0: n_blocks * wf_kv8_block_bytes() */
+  int32_t n_layers;
+  int32_t n_blocks;     /* block ids are 0 .. n_blocks - 1; n_blocks * block_size < 2^31 */
+  int32_t block_size;   /* 16, 32 or 64 positions */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t dtype;        /* of rows and queries: WF_BF16 or WF_F16 */
+} wf_kv8_pool;
+
+/* Bytes of one block in one layer; 0 for a shape that is not supported. */
+size_t wf_kv8_block_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_dim);
+
+/* Quantise n rows of keys and values into one layer of the cache.
+ *   d_k, d_v  dtype [n][n_kv_heads * head_dim], row strides in elements
+ *             (multiples of 8; pointers 16-byte aligned)
+ *   d_slots   int32 [n]: block * block_size + position % block_size; a negative
+ *             slot skips its row.  Rows of the same 16 positions follow one
+ *             another in the call, as wf_page_plan gives them (the same
+ *             position twice: the later row holds)
+ * Positions are appended: of a record that a call writes to, those before the
+ * first one written are kept, those after that are not written become zeros.
+ * A kept record's e never falls; where it grows, codes are rounded again.
+ * wf_kv8_load reads slots back into rows, in any order (zeros for a negative
+ * slot, or one outside the pool: WF_DEV_ERR_PAGE). */
+wf_status wf_kv8_store(const wf_kv8_pool *pool, int32_t layer, const void *d_k, int64_t k_stride,
+                       const void *d_v, int64_t v_stride, const int32_t *d_slots, int32_t n,
+                       uint32_t *d_err, void *stream);
+wf_status wf_kv8_load(const wf_kv8_pool *pool, int32_t layer, const int32_t *d_slots, int32_t n,
+                      void *d_k, int64_t k_stride, void *d_v, int64_t v_stride, uint32_t *d_err,
+                      void *stream);
+
+/* Attention of rps query rows per sequence over one layer of the cache: the
+ * arguments and the rows that see nothing are wf_kv4_attention's.  Positions
+ * that a row does not see do not reach it whatever they hold; a position that
+ * reads back as NaN makes NaN of the dims it has them in.  Scores, softmax and
+ * sums are fp32.  Queries enter the first product in fp16 under a power of two
+ * of their own (bf16: exact but for dims 2^-28 of a row's largest); a weight
+ * times its record's 2^e is rounded to 11 bits (of those down to 2^-21 of the
+ * row's largest; of smaller ones at most 2^-32 of that is lost). */
+wf_status wf_kv8_attention(const wf_kv8_pool *pool, int32_t layer, const void *d_q,
+                           int64_t q_stride, const int32_t *d_table, int32_t table_stride,
+                           const int32_t *d_len, int32_t n_seq, int32_t rps, int32_t n_heads,
+                           int32_t causal, float scale, int32_t max_len, void *d_out,
+                           int64_t out_stride, void *d_scratch, size_t scratch_bytes,
+                           uint32_t *d_err, void *stream);
+size_t wf_kv8_attention_scratch_bytes(int32_t n_seq, int32_t rps, int32_t n_heads,
+                                      int32_t n_kv_heads, int32_t head_dim, int32_t max_len);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,6 +20,9 @@ WF_DEV_ERR_TIMEOUT, WF_DEV_ERR_CAPACITY, WF_DEV_ERR_TOKEN, WF_DEV_ERR_LAUNCH = 1
 WF_DEV_ERR_PAGE = 16
 WF_BF16, WF_F16, WF_F32 = 0, 1, 2
 WF_KV4_GROUP, WF_KV4_RECORD, WF_MAX_BEAMS = 64, 1152, 16
+WF_ROPE_HALF, WF_ROPE_INTERLEAVED = 0, 1
+WF_ROPE_PLAIN, WF_ROPE_LINEAR, WF_ROPE_BASE, WF_ROPE_WAVES, WF_ROPE_PARTS = range(5)
+WF_ROPE_MAX_PAIRS = 128
 WF_MAX_TAPS = 8
 WF_OPT_KEEP_LOGITS = 1
 WF_OPT_PROFILE = 2
@@ -77,11 +80,28 @@ class WfKv4Pool(C.Structure):
                 ("head_dim", C.c_int32), ("dtype", C.c_int32)]
 
 
+class WfKv8Pool(C.Structure):
+    _fields_ = WfKv4Pool._fields_
+
+
+class WfRopeSpec(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("trained_len", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("gain", C.c_double)]
+
+
+class WfRopeTable(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("gain", C.c_float),
+                ("turns", C.c_uint64 * WF_ROPE_MAX_PAIRS)]
+
+
 _P = C.c_void_p
 _I = C.c_int32
 _L = C.c_int64
 _SZ = C.c_size_t
 _PL = C.POINTER(WfKv4Pool)
+_PL8 = C.POINTER(WfKv8Pool)
+_RT = C.POINTER(WfRopeTable)
 _SIGS = {
     "wf_workspace_bytes": (_I, [C.POINTER(WfConfig), _I, _I, C.POINTER(_SZ)]),
     "wf_create": (_I, [C.POINTER(WfConfig), C.POINTER(WfTargetWeights), C.POINTER(WfDrafterWeights),
@@ -117,6 +137,17 @@ _SIGS = {
     "wf_beam_select_scratch_bytes": (_SZ, [_I, _I, _I]),
     "wf_beam_reorder": (_I, [_PL, _P, _P, _I, _P, _P, _I, _I, _P, _P, _P, _P, _SZ, _P, _P]),
     "wf_beam_reorder_scratch_bytes": (_SZ, [_I, _I, _I]),
+    "wf_rope_init": (_I, [C.POINTER(WfRopeSpec), _RT]),
+    "wf_rope": (_I, [_RT, _P, _L, _I, _P, _L, _I, _P, _I, _I, _I, _P, _L, _P, _L, _P]),
+    "wf_prompt_attention": (_I, [_P, _L, _P, _L, _P, _L, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _I, C.c_float,
+                                 _P, _L, _P, _P, _SZ, _P, _P]),
+    "wf_prompt_attention_scratch_bytes": (_SZ, [_I, _I, _I, _I, _I, _I]),
+    "wf_kv8_block_bytes": (_SZ, [_I, _I, _I]),
+    "wf_kv8_store": (_I, [_PL8, _I, _P, _L, _P, _L, _P, _I, _P, _P]),
+    "wf_kv8_load": (_I, [_PL8, _I, _P, _I, _P, _L, _P, _L, _P, _P]),
+    "wf_kv8_attention": (_I, [_PL8, _I, _P, _L, _P, _I, _P, _I, _I, _I, _I, C.c_float, _I, _P, _L,
+                              _P, _SZ, _P, _P]),
+    "wf_kv8_attention_scratch_bytes": (_SZ, [_I, _I, _I, _I, _I, _I]),
 }
 EXPORTED = tuple(_SIGS)
 
@@ -420,3 +451,73 @@ def wf_beam_reorder(pool, table_in, table_out, table_stride, length, parent, n_r
         C.byref(pool), _ptr(table_in), _ptr(table_out), table_stride, _ptr(length), _ptr(parent),
         n_req, beams, _ptr(free), _ptr(n_free), _ptr(n_free_out), _ptr(scratch), scratch_bytes,
         _ptr(err), _stream(stream)))
+
+
+# ------------------------ rotary positions, prompts, paged 8-bit cache --
+def wf_rope_init(head_dim, rot_dim=None, layout=WF_ROPE_HALF, base=10000.0, scaling=WF_ROPE_PLAIN,
+                 factor=1.0, trained_len=0.0, low=0.0, high=0.0, gain=1.0) -> WfRopeTable:
+    """The table of a rotary embedding, for wf_rope (the whole head turns if rot_dim is None)."""
+    spec = WfRopeSpec(head_dim, head_dim if rot_dim is None else rot_dim, layout, scaling, base,
+                      factor, trained_len, low, high, gain)
+    table = WfRopeTable()
+    _check("wf_rope_init", lib().wf_rope_init(C.byref(spec), C.byref(table)))
+    return table
+
+
+def wf_rope(table, q, q_stride, n_heads, k, k_stride, n_kv_heads, pos, n, dtype, adjoint, q_out,
+            q_out_stride, k_out, k_out_stride, stream=None):
+    _check("wf_rope", lib().wf_rope(
+        C.byref(table), _ptr(q), q_stride, n_heads, _ptr(k), k_stride, n_kv_heads, _ptr(pos), n,
+        dtype, int(adjoint), _ptr(q_out), q_out_stride, _ptr(k_out), k_out_stride, _stream(stream)))
+
+
+def wf_prompt_attention_scratch_bytes(n_seq, n_q, max_k, n_heads, n_kv_heads, head_dim) -> int:
+    return lib().wf_prompt_attention_scratch_bytes(n_seq, n_q, max_k, n_heads, n_kv_heads, head_dim)
+
+
+def wf_prompt_attention(q, q_stride, k, k_stride, v, v_stride, q_start, k_start, n_seq, n_q, n_k,
+                        max_k, n_heads, n_kv_heads, head_dim, dtype, causal, scale, out, out_stride,
+                        lse, scratch, scratch_bytes, err=None, stream=None):
+    _check("wf_prompt_attention", lib().wf_prompt_attention(
+        _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(q_start), _ptr(k_start),
+        n_seq, n_q, n_k, max_k, n_heads, n_kv_heads, head_dim, dtype, int(causal), scale, _ptr(out),
+        out_stride, _ptr(lse), _ptr(scratch), scratch_bytes, _ptr(err), _stream(stream)))
+
+
+def kv8_pool(base, n_layers, n_blocks, block_size, n_kv_heads, head_dim, dtype=WF_BF16,
+             layer_stride=0) -> WfKv8Pool:
+    """Descriptor of a paged 8-bit cache over a device buffer of n_layers *
+    n_blocks * wf_kv8_block_bytes(...) bytes, which it keeps alive."""
+    pool = WfKv8Pool(_ptr(base), layer_stride, n_layers, n_blocks, block_size, n_kv_heads,
+                     head_dim, dtype)
+    pool.buffer = base
+    return pool
+
+
+def wf_kv8_block_bytes(block_size, n_kv_heads, head_dim) -> int:
+    return lib().wf_kv8_block_bytes(block_size, n_kv_heads, head_dim)
+
+
+def wf_kv8_store(pool, layer, k, k_stride, v, v_stride, slots, n, err=None, stream=None):
+    _check("wf_kv8_store", lib().wf_kv8_store(
+        C.byref(pool), layer, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(slots), n, _ptr(err),
+        _stream(stream)))
+
+
+def wf_kv8_load(pool, layer, slots, n, k, k_stride, v, v_stride, err=None, stream=None):
+    _check("wf_kv8_load", lib().wf_kv8_load(
+        C.byref(pool), layer, _ptr(slots), n, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(err),
+        _stream(stream)))
+
+
+def wf_kv8_attention_scratch_bytes(n_seq, rps, n_heads, n_kv_heads, head_dim, max_len) -> int:
+    return lib().wf_kv8_attention_scratch_bytes(n_seq, rps, n_heads, n_kv_heads, head_dim, max_len)
+
+
+def wf_kv8_attention(pool, layer, q, q_stride, table, table_stride, length, n_seq, rps, n_heads,
+                     causal, scale, max_len, out, out_stride, scratch, scratch_bytes, err=None,
+                     stream=None):
+    _check("wf_kv8_attention", lib().wf_kv8_attention(
+        C.byref(pool), layer, _ptr(q), q_stride, _ptr(table), table_stride, _ptr(length), n_seq,
+        rps, n_heads, int(causal), scale, max_len, _ptr(out), out_stride, _ptr(scratch),
+        scratch_bytes, _ptr(err), _stream(stream)))

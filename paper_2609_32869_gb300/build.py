@@ -21,7 +21,8 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include")]
 SOURCES = ["wf_gemm.cu", "wf_skinny.cu", "wf_skinny_mt.cu", "wf_attn.cu", "wf_step_kernels.cu", "wf_persist.cu",
-           "wf_api.cu", "wf_paged.cu", "wf_kv4_attn.cu", "wf_beam.cu"]
+           "wf_api.cu", "wf_paged.cu", "wf_kv4_attn.cu", "wf_beam.cu",
+           "wf_rope.cu", "wf_prompt.cu", "wf_kv8.cu", "wf_kv8_attn.cu"]
 
 
 def _nvcc() -> str:
