@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(128) kv8_attention_kernel(const Kv8AttnParams 
       v[g] = codes_to_f32(va[0] | va[8] << 8);
     }
     x = warp_sum(x) * (sc.x * p.scale);
-    const float next = fmaxf(m, x), keep = m == -INFINITY ? 0.f : __expf(m - next), w = next == -INFINITY ? 0.f : __expf(x - next);
+    const float next = fmaxf(m, x), keep = m == -INFINITY ? 0.f : __expf(m - next), w = x == -INFINITY ? 0.f : __expf(x - next);
     l = l * keep + w;
     m = next;
 #pragma unroll
