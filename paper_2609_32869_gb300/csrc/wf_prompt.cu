@@ -42,13 +42,46 @@ template <int D>
 struct PtShape {
   static constexpr int kHalf = 16384;            // 128 rows of 64 dims
   static constexpr int kTile = kHalf * D / 64;   // queries, keys or values
-  static constexpr int kStages = D == 64 ? 6 : 4;
-  static constexpr int kMarkOff = 2 * kTile + kStages * kTile;  // [3][D] first position of a value that is not finite
+  static constexpr int kStages = D == 64 ? 4 : 2;  // of keys, and of values
+  // Buffers of scores in TMEM beside the tiles' sums: with a third one the scores
+  // of a tile's next block are there before its last ones are done with.
+  static constexpr int kScores = D == 64 ? 3 : 2;
+  static constexpr int kSumCol = kScores * 128;
+  static constexpr int kMarkOff = 2 * kTile + 2 * kStages * kTile;  // [3][D] first position of a value that is not finite
   static constexpr int kBarOff = kMarkOff + 3 * D * 4;
-  static constexpr int kBars = 2 + 4 * kStages + 2 + 2 + 2 + 1;
+  static constexpr int kBars = 2 + 6 * kStages + 3 * kScores + 2 + 1;
   static constexpr int kSmem = 1024 + kBarOff + kBars * 8 + 64;
   static constexpr uint32_t kCols = 512;
 };
+
+// A warp's waits on barriers, all lanes together.  After one that gave up the
+// others ask once: the kernel comes to its end, with the error recorded.
+struct PtWaits {
+  uint32_t *err;
+  long long limit;
+};
+__device__ __forceinline__ bool pt_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return __all_sync(0xffffffffu, ok) != 0;
+}
+__device__ __forceinline__ void pt_wait(PtWaits &w, uint32_t bar, uint32_t parity) {
+  if (pt_try(bar, parity)) return;
+  const long long t0 = clock64();
+  while (!pt_try(bar, parity)) {
+    if (__any_sync(0xffffffffu, clock64() - t0 > w.limit)) {
+      set_error(w.err, WF_DEV_ERR_TIMEOUT);
+      w.limit = 0;
+      return;
+    }
+  }
+}
 
 // What a CTA works on.
 struct PtWork {
@@ -87,13 +120,41 @@ __host__ __device__ constexpr uint32_t pt_idesc(int N, bool b_rows_contiguous) {
   return (1u << 4) | (type << 7) | (type << 10) | (static_cast<uint32_t>(b_rows_contiguous) << 16) | (static_cast<uint32_t>(N >> 3) << 17) |
          (8u << 24);
 }
-// D (+)= A B with A in TMEM.
-__device__ __forceinline__ void umma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// One lane of a converged warp.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e;
+}
+// The products are issued by a whole warp under a predicate that one lane has:
+// behind a branch on the lane each instruction's operands took the slow way to
+// the uniform registers, 76 clocks an instruction instead of the product's own 32 to 64.
+// D (+)= A B^T, both in shared memory.
+__device__ __forceinline__ void pt_mma_ss(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
+      : "memory");
+}
+// D (+)= A B with A in TMEM.
+__device__ __forceinline__ void pt_mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void pt_commit(uint32_t lead, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(lead)
       : "memory");
 }
 // 32 columns of the warp's lanes, without the wait.
@@ -110,6 +171,12 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, float (&v)[32]) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Behind tmem_ld_wait: what is computed from v stays behind it too.
+__device__ __forceinline__ void tmem_loaded(float (&v)[32]) {
+  asm volatile(""
+               : "+f"(v[0]),"+f"(v[1]),"+f"(v[2]),"+f"(v[3]),"+f"(v[4]),"+f"(v[5]),"+f"(v[6]),"+f"(v[7]),"+f"(v[8]),"+f"(v[9]),"+f"(v[10]),"+f"(v[11]),"+f"(v[12]),"+f"(v[13]),"+f"(v[14]),"+f"(v[15]),
+                 "+f"(v[16]),"+f"(v[17]),"+f"(v[18]),"+f"(v[19]),"+f"(v[20]),"+f"(v[21]),"+f"(v[22]),"+f"(v[23]),"+f"(v[24]),"+f"(v[25]),"+f"(v[26]),"+f"(v[27]),"+f"(v[28]),"+f"(v[29]),"+f"(v[30]),"+f"(v[31]));
+}
 template <int N>
 __device__ __forceinline__ void tmem_st(uint32_t at, const uint32_t (&r)[N]) {
   static_assert(N == 16 || N == 32, "");
@@ -196,17 +263,18 @@ __global__ void __launch_bounds__(kPtThreads, 1)
   constexpr int kStages = S::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-  uint8_t *sq = smem, *skv = smem + 2 * S::kTile;
+  uint8_t *sq = smem, *sk = smem + 2 * S::kTile, *sv = sk + kStages * S::kTile;
   int *mark = reinterpret_cast<int *>(smem + S::kMarkOff);
   uint64_t *q_full = reinterpret_cast<uint64_t *>(smem + S::kBarOff);
-  uint64_t *full = q_full + 2, *empty = full + kStages, *s_full = empty + kStages, *p_full = s_full + 2, *pv_done = p_full + 2;
-  uint64_t *look = pv_done + 2, *clean = look + kStages, *done = clean + kStages;
+  uint64_t *k_full = q_full + 2, *k_empty = k_full + kStages, *v_full = k_empty + kStages, *v_empty = v_full + kStages;
+  uint64_t *look = v_empty + kStages, *clean = look + kStages;
+  uint64_t *s_full = clean + kStages, *p_full = s_full + S::kScores, *o_done = p_full + 2 * S::kScores, *done = o_done + 2;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(done + 1);
   int *has_work = reinterpret_cast<int *>(tmem_slot + 1);
   volatile int *marked = has_work + 1;
   PtWork *shared_work = reinterpret_cast<PtWork *>(has_work + 2);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   pdl_wait();
   pdl_launch_dependents();
   const int head = blockIdx.x % p.heads;
@@ -223,8 +291,12 @@ __global__ void __launch_bounds__(kPtThreads, 1)
     if (lane == 0) *shared_work = w, *has_work = any, *marked = 0;
   }
   if (threadIdx.x == 32) {
-    for (int i = 0; i < 2; ++i) mbar_init(&q_full[i], 1), mbar_init(&s_full[i], 1), mbar_init(&p_full[i], 128), mbar_init(&pv_done[i], 1);
-    for (int i = 0; i < kStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1), mbar_init(&look[i], 1), mbar_init(&clean[i], 64);
+    for (int i = 0; i < 2; ++i) mbar_init(&q_full[i], 1), mbar_init(&o_done[i], 1);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1), mbar_init(&v_full[i], 1), mbar_init(&v_empty[i], 1);
+      mbar_init(&look[i], 1), mbar_init(&clean[i], 64);
+    }
+    for (int i = 0; i < S::kScores; ++i) mbar_init(&s_full[i], 1), mbar_init(&p_full[2 * i], 128), mbar_init(&p_full[2 * i + 1], 128);
     mbar_init(done, 1);
     fence_barrier_init();
     fence_proxy_async();
@@ -234,11 +306,16 @@ __global__ void __launch_bounds__(kPtThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  const PtWork w = *shared_work;
+  // Broadcast, so that the compiler knows that they are the same in all of a warp
+  // and keeps what follows from them in uniform registers.
+  const auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
+  const uint32_t tmem = uniform(*tmem_slot);
+  const PtWork w = {uniform(shared_work->seq),  uniform(shared_work->q0),    uniform(shared_work->rows),  uniform(shared_work->k0),
+                    uniform(shared_work->keys), uniform(shared_work->token), uniform(shared_work->first), uniform(shared_work->last)};
+  const bool any_work = uniform(*has_work) != 0;
   // tile i: its tokens and the blocks that its rows see of this CTA's
-  const int tokens[2] = {*has_work ? min(p.tokens, w.rows - w.token) : 0,
-                         *has_work && p.tiles > 1 ? min(max(w.rows - w.token - p.tokens, 0), p.tokens) : 0};
+  const int tokens[2] = {any_work ? min(p.tokens, w.rows - w.token) : 0,
+                         any_work && p.tiles > 1 ? min(max(w.rows - w.token - p.tokens, 0), p.tokens) : 0};
   int ends[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -247,121 +324,163 @@ __global__ void __launch_bounds__(kPtThreads, 1)
   }
   const int end = max(ends[0], ends[1]);
   // blocks from here on hold positions that some row does not see
-  const int edge = *has_work ? pt_limit(w, p.causal, w.token) / kPtKeys : 0;
+  const int edge = any_work ? pt_limit(w, p.causal, w.token) / kPtKeys : 0;
+  // The products go through the blocks, tile by tile; number n is block j of tile
+  // i, its scores in buffer n % kScores.
+  const int both = min(ends[0], ends[1]);  // blocks before it are both tiles'
+  const int products = ends[0] + ends[1] - 2 * w.first;
 
-  if (warp == kPtLoad) {
-    if (lane == 0 && w.first < end) {
-      tma_prefetch_desc(&mq), tma_prefetch_desc(&mk), tma_prefetch_desc(&mv);
-      const uint32_t q_bytes = static_cast<uint32_t>(p.group * p.tokens) * D * 2;
-      const auto load_q = [&](int i) {
-        mbar_arrive_expect_tx(&q_full[i], q_bytes);
-        for (int c = 0; c < D / 64; ++c)
-          tma_load_4d(sq + i * S::kTile + c * S::kHalf, &mq, c * 64, 0, head, w.q0 + w.token + i * p.tokens, &q_full[i]);
-      };
-      if (ends[0] > w.first) load_q(0);
-      int n = 0;  // loads so far
-      for (int j = w.first; j < end; ++j) {
-        bool ok = true;
-        for (int kv = 0; kv < 2 && ok; ++kv, ++n) {
-          const int st = n % kStages;
-          if (n >= kStages) ok = mbar_wait(&empty[st], ((n / kStages) - 1) & 1, p.err, kSpinLimitCycles);
-          if (!ok) break;
-          mbar_arrive_expect_tx(&full[st], S::kTile);
+  // The block's 384 threads have 168 registers each: 256 take 208, 128 keep 88.
+  if (warp >= kPtMma) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kPtLoad) {
+      if (lane == 0 && w.first < end) {
+        tma_prefetch_desc(&mq), tma_prefetch_desc(&mk), tma_prefetch_desc(&mv);
+        const uint32_t q_bytes = static_cast<uint32_t>(p.group * p.tokens) * D * 2;
+        const auto load_q = [&](int i) {
+          mbar_arrive_expect_tx(&q_full[i], q_bytes);
           for (int c = 0; c < D / 64; ++c)
-            tma_load_3d(skv + st * S::kTile + c * S::kHalf, kv ? &mv : &mk, c * 64, head, w.k0 + j * kPtKeys, &full[st]);
-          // The stage's earlier copies have landed: only now is the parity of its barrier one to wait for.
-          if (kv && j >= edge) mbar_arrive_cta(&look[st]);
-          if (n == 0 && ends[1] > w.first) load_q(1);
-        }
-        if (!ok) break;
-      }
-      // a later wait gave up, here or in another warp: the copies still have to land before the CTA ends
-      for (int i = 0; i < 2; ++i)
-        if (ends[i] > w.first) mbar_drain(&q_full[i], 0);
-      for (int i = max(0, n - kStages); i < n; ++i) mbar_drain(&full[i % kStages], (i / kStages) & 1);
-    }
-  } else if (warp == kPtMma) {
-    if (lane == 0 && w.first < end) {
-      constexpr uint32_t kIdS = pt_idesc<T>(kPtKeys, false), kIdO = pt_idesc<T>(D, true);
-      const uint64_t dq = umma_desc_sw128(smem_u32(sq)), dk = umma_desc_sw128(smem_u32(skv)), dv = pt_desc_v(smem_u32(skv));
-      const auto scores = [&](int i, int st) {
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = (k / 4 * S::kHalf + k % 4 * 32) >> 4;
-          umma_bf16(tmem + i * 128, dq + ((i * S::kTile) >> 4) + off, dk + ((st * S::kTile) >> 4) + off, kIdS, k > 0);
-        }
-        umma_commit(&s_full[i]);
-      };
-      bool ok = mbar_wait(&full[0], 0, p.err, kSpinLimitCycles);
-      for (int i = 0; i < 2 && ok; ++i) {
-        if (ends[i] <= w.first) continue;
-        ok = mbar_wait(&q_full[i], 0, p.err, kSpinLimitCycles);
-        tc_fence_after();
-        if (ok) scores(i, 0);
-      }
-      umma_commit(&empty[0]);
-      for (int j = w.first; j < end && ok; ++j) {
-        const int n = 2 * (j - w.first), sv = (n + 1) % kStages, sk = (n + 2) % kStages;
-        const uint32_t par = (j - w.first) & 1;
-        ok = mbar_wait(&full[sv], ((n + 1) / kStages) & 1, p.err, kSpinLimitCycles);
-        if (ok && j >= edge) ok = mbar_wait(&clean[sv], (j - max(edge, w.first)) / (kStages / 2) & 1, p.err, kSpinLimitCycles);
-        if (ok && j + 1 < end) ok = mbar_wait(&full[sk], ((n + 2) / kStages) & 1, p.err, kSpinLimitCycles);
-        for (int i = 0; i < 2 && ok; ++i) {
-          if (j >= ends[i]) continue;
-          ok = mbar_wait(&p_full[i], par, p.err, kSpinLimitCycles);
-          tc_fence_after();
+            tma_load_4d(sq + i * S::kTile + c * S::kHalf, &mq, c * 64, 0, head, w.q0 + w.token + i * p.tokens, &q_full[i]);
+        };
+        if (ends[0] > w.first) load_q(0);
+        int n = 0;  // blocks so far, keys and values
+        bool ok = true;
+        for (int j = w.first; j < end && ok; ++j, ++n) {
+          const int st = n % kStages;
+          const uint32_t before = ((n / kStages) - 1) & 1;
+          if (n >= kStages) ok = mbar_wait(&k_empty[st], before, p.err, kSpinLimitCycles);
           if (!ok) break;
+          mbar_arrive_expect_tx(&k_full[st], S::kTile);
+          for (int c = 0; c < D / 64; ++c) tma_load_3d(sk + st * S::kTile + c * S::kHalf, &mk, c * 64, head, w.k0 + j * kPtKeys, &k_full[st]);
+          if (n == 0 && ends[1] > w.first) load_q(1);
+          if (n >= kStages) ok = mbar_wait(&v_empty[st], before, p.err, kSpinLimitCycles);
+          if (!ok) {
+            mbar_drain(&k_full[st], (n / kStages) & 1);
+            break;
+          }
+          mbar_arrive_expect_tx(&v_full[st], S::kTile);
+          for (int c = 0; c < D / 64; ++c) tma_load_3d(sv + st * S::kTile + c * S::kHalf, &mv, c * 64, head, w.k0 + j * kPtKeys, &v_full[st]);
+          // The stage's earlier copies have landed: only now is the parity of its barrier one to wait for.
+          if (j >= edge) mbar_arrive_cta(&look[st]);
+        }
+        // a wait gave up, here or in another warp: the copies still have to land before the CTA ends
+        for (int i = 0; i < 2; ++i)
+          if (ends[i] > w.first) mbar_drain(&q_full[i], 0);
+        for (int i = max(0, n - kStages); i < n; ++i) {
+          mbar_drain(&k_full[i % kStages], (i / kStages) & 1);
+          mbar_drain(&v_full[i % kStages], (i / kStages) & 1);
+        }
+      }
+    } else if (warp == kPtMma) {
+      if (w.first < end) {
+        const uint32_t lead = elect_one();
+        constexpr uint32_t kIdS = pt_idesc<T>(kPtKeys, false), kIdO = pt_idesc<T>(D, true);
+        const uint64_t dq = umma_desc_sw128(smem_u32(sq)), dk = umma_desc_sw128(smem_u32(sk)), dv = pt_desc_v(smem_u32(sv));
+        const uint32_t bars = smem_u32(q_full);
+        const auto at = [&](const uint64_t *bar) { return bars + static_cast<uint32_t>(bar - q_full) * 8; };
+        PtWaits waits = {p.err, kSpinLimitCycles};
+        // The next scores are of block qj of tile qi, in buffer q_buf, with keys of
+        // stage q_st; the next product with values has the same of its own.
+        int qj = w.first, qi = qj < ends[0] ? 0 : 1, q_buf = 0, q_st = 0;
+        int pj = qj, pi = qi, p_buf = 0, p_st = 0;
+        uint32_t q_phase = 0, p_phase = 0, v_phase = 0;
+        const auto scores = [&]() {
+          if (qi == 0 || qj >= ends[0]) pt_wait(waits, at(k_full) + q_st * 8, q_phase);
+          if (qj == w.first) pt_wait(waits, at(q_full) + qi * 8, 0);
+          tc_fence_after();
+          const uint64_t a = dq + qi * (S::kTile >> 4), b = dk + q_st * (S::kTile >> 4);
+          const uint32_t d = tmem + q_buf * 128;
 #pragma unroll
-          for (int k = 0; k < kPtKeys / 16; ++k)
-            umma_ta(tmem + 256 + i * D, tmem + i * 128 + k * 8, dv + ((sv * S::kTile + k * 2048) >> 4), kIdO, j > w.first || k > 0);
-          umma_commit(&pv_done[i]);
-          // P's columns are read before the next scores, issued behind, are written
-          if (j + 1 < ends[i]) scores(i, sk);
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = (k / 4 * S::kHalf + k % 4 * 32) >> 4;
+            pt_mma_ss(lead, d, a + off, b + off, kIdS, k > 0);
+          }
+          pt_commit(lead, at(s_full) + q_buf * 8);
+          q_buf = q_buf + 1 == S::kScores ? 0 : q_buf + 1;
+          if (qi == 0 && qj < ends[1]) {
+            qi = 1;
+          } else {  // the block's last
+            pt_commit(lead, at(k_empty) + q_st * 8);
+            ++qj;
+            qi = qj < ends[0] ? 0 : 1;
+            if (++q_st == kStages) q_st = 0, q_phase ^= 1;
+          }
+        };
+#pragma unroll 1
+        for (int n = 0; n < S::kScores && n < products; ++n) scores();
+#pragma unroll 1
+        for (int n = 0; n < products; ++n) {
+          if (pi == 0 || pj >= ends[0]) {
+            pt_wait(waits, at(v_full) + p_st * 8, v_phase);
+            if (pj >= edge) pt_wait(waits, at(clean) + p_st * 8, (pj - max(edge, w.first)) / kStages & 1);
+          }
+          const uint64_t b = dv + p_st * (S::kTile >> 4);
+          const uint32_t d = tmem + S::kSumCol + pi * D, a = tmem + p_buf * 128;
+          const uint32_t more = pj > w.first;
+          pt_wait(waits, at(p_full) + p_buf * 16, p_phase);
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < kPtKeys / 32; ++k) pt_mma_ts(lead, d, a + k * 8, b + ((k * 2048) >> 4), kIdO, k > 0 ? 1u : more);
+          pt_wait(waits, at(p_full) + p_buf * 16 + 8, p_phase);
+          tc_fence_after();
+#pragma unroll
+          for (int k = kPtKeys / 32; k < kPtKeys / 16; ++k) pt_mma_ts(lead, d, a + k * 8, b + ((k * 2048) >> 4), kIdO, 1);
+          pt_commit(lead, at(o_done) + pi * 8);
+          if (++p_buf == S::kScores) p_buf = 0, p_phase ^= 1;
+          if (pi == 0 && pj < ends[1]) {
+            pi = 1;
+          } else {  // the block's last
+            pt_commit(lead, at(v_empty) + p_st * 8);
+            ++pj;
+            pi = pj < ends[0] ? 0 : 1;
+            if (++p_st == kStages) p_st = 0, v_phase ^= 1;
+          }
+          // P's columns are read before the scores that are issued behind are written over them
+          if (n + S::kScores < products) scores();
         }
-        umma_commit(&empty[sv]);
-        if (j + 1 < end) umma_commit(&empty[sk]);
+        pt_commit(lead, at(done));
+        mbar_drain(done, 0);
       }
-      umma_commit(done);
-      mbar_drain(done, 0);
-    }
-  } else if (warp >= kPtScrub) {
-    // Values of positions that some row does not see: zero past the sequence's
-    // end, and where they are not finite, which a weight of 0 would not hide;
-    // the rows that see those take them from `mark`.
-    for (int j = max(edge, w.first); j < end; ++j) {
-      const int n = 2 * (j - w.first) + 1, st = n % kStages;
-      if (!__all_sync(0xffffffffu, mbar_wait(&look[st], (j - max(edge, w.first)) / (kStages / 2) & 1, p.err, kSpinLimitCycles) &&
-                                       mbar_wait(&full[st], (n / kStages) & 1, p.err, kSpinLimitCycles)))
-        break;
-      const int held = w.keys - j * kPtKeys;
-      for (int c = threadIdx.x - kPtScrub * 32; c < S::kTile / 16; c += 64) {
-        uint4 *at = reinterpret_cast<uint4 *>(skv + st * S::kTile + c * 16);
-        const int row = c / 8 % 128;
-        if (row >= held) {
-          *at = make_uint4(0, 0, 0, 0);
-          continue;
+    } else if (warp >= kPtScrub) {
+      // Values of positions that some row does not see: zero past the sequence's
+      // end, and where they are not finite, which a weight of 0 would not hide;
+      // the rows that see those take them from `mark`.
+      for (int j = max(edge, w.first); j < end; ++j) {
+        const int n = j - w.first, st = n % kStages;
+        if (!__all_sync(0xffffffffu, mbar_wait(&look[st], (j - max(edge, w.first)) / kStages & 1, p.err, kSpinLimitCycles) &&
+                                         mbar_wait(&v_full[st], (n / kStages) & 1, p.err, kSpinLimitCycles)))
+          break;
+        const int held = w.keys - j * kPtKeys;
+        for (int c = threadIdx.x - kPtScrub * 32; c < S::kTile / 16; c += 64) {
+          uint4 *at = reinterpret_cast<uint4 *>(sv + st * S::kTile + c * 16);
+          const int row = c / 8 % 128;
+          if (row >= held) {
+            *at = make_uint4(0, 0, 0, 0);
+            continue;
+          }
+          const uint4 v = *at;
+          const uint32_t m = 0x7fff7fffu;
+          const uint32_t most = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
+          if (max(most & 0xffff, most >> 16) < PtType<T>::kInf) continue;
+          uint16_t *e = reinterpret_cast<uint16_t *>(at);
+          const int dim = c / 1024 * 64 + ((c & 7) ^ (row & 7)) * 8;
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t u = e[i] & 0x7fff;
+            if (u < PtType<T>::kInf) continue;
+            atomicMin(&mark[(u > PtType<T>::kInf ? 0 : e[i] >> 15 ? 2 : 1) * D + dim + i], j * kPtKeys + row);
+            e[i] = 0;
+            *marked = 1;
+          }
         }
-        const uint4 v = *at;
-        const uint32_t m = 0x7fff7fffu;
-        const uint32_t most = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
-        if (max(most & 0xffff, most >> 16) < PtType<T>::kInf) continue;
-        uint16_t *e = reinterpret_cast<uint16_t *>(at);
-        const int dim = c / 1024 * 64 + ((c & 7) ^ (row & 7)) * 8;
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t u = e[i] & 0x7fff;
-          if (u < PtType<T>::kInf) continue;
-          atomicMin(&mark[(u > PtType<T>::kInf ? 0 : e[i] >> 15 ? 2 : 1) * D + dim + i], j * kPtKeys + row);
-          e[i] = 0;
-          *marked = 1;
-        }
+        fence_proxy_async();
+        mbar_arrive_cta(&clean[st]);
       }
-      fence_proxy_async();
-      mbar_arrive_cta(&clean[st]);
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int i = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + i * 128 + lanes, to = tmem + 256 + i * D + lanes;
+    const uint32_t to = tmem + S::kSumCol + i * D + lanes;
     const int token = row / p.group, h = head * p.group + row % p.group, index = w.token + i * p.tokens + token;
     const bool live = token < tokens[i];
     const int limit = live ? pt_limit(w, p.causal, index) : 0;
@@ -369,16 +488,29 @@ __global__ void __launch_bounds__(kPtThreads, 1)
     const int least = tokens[i] ? pt_limit(w, p.causal, w.token + i * p.tokens) : 0;
     const float c = p.scale * 1.4426950408889634f;
     float ref = -INFINITY, l = 0.f;
-    bool ok = true;
-    for (int j = w.first; j < ends[i]; ++j) {
-      const uint32_t par = (j - w.first) & 1;
-      ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i], par, p.err, kSpinLimitCycles));
-      if (!ok) break;
+    PtWaits waits = {p.err, kSpinLimitCycles};
+    // Waits until the products of the tile's block j are in its sums.  Every
+    // block's in turn: a barrier tells a phase from the one before it, not from
+    // the one before that.
+    int waited = w.first;
+    const auto added = [&](int j) {
+      if (waited > j) return;
+      waited = j + 1;
+      pt_wait(waits, smem_u32(&o_done[i]), (j - w.first) & 1);
       tc_fence_after();
-      float s[4][32];
+    };
+    int buf = w.first < both ? i : 0;  // of the scores, and the parity of its barrier
+    uint32_t phase = 0;
+    for (int j = w.first; j < ends[i]; ++j) {
+      const uint32_t ts = tmem + buf * 128 + lanes;
+      pt_wait(waits, smem_u32(s_full) + buf * 8, phase);
+      tc_fence_after();
+      float s[4][32], mx[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) tmem_ld32(ts + q * 32, s[q]);
       tmem_ld_wait();
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tmem_loaded(s[q]);
       if ((j + 1) * kPtKeys > least) {
         const int seen = limit - j * kPtKeys;
 #pragma unroll
@@ -387,13 +519,12 @@ __global__ void __launch_bounds__(kPtThreads, 1)
           for (int e = 0; e < 32; ++e)
             if (q * 32 + e >= seen) s[q][e] = -INFINITY;
       }
-      float mx[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        mx[q] = s[q][0];
+        float m0 = max3(s[q][0], s[q][1], s[q][2]), m1 = max3(s[q][3], s[q][4], s[q][5]);
 #pragma unroll
-        for (int e = 1; e < 31; e += 2) mx[q] = max3(mx[q], s[q][e], s[q][e + 1]);
-        mx[q] = fmaxf(mx[q], s[q][31]);
+        for (int e = 6; e < 30; e += 4) m0 = max3(m0, s[q][e], s[q][e + 1]), m1 = max3(m1, s[q][e + 2], s[q][e + 3]);
+        mx[q] = max3(fmaxf(m0, m1), s[q][30], s[q][31]);
       }
       const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
       if (j == w.first) {
@@ -403,20 +534,23 @@ __global__ void __launch_bounds__(kPtThreads, 1)
         const float keep = ref == -INFINITY ? 0.f : ex2((ref - next) * c);
         ref = next;
         l *= keep;
-        ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[i], par ^ 1, p.err, kSpinLimitCycles));
-        if (!ok) break;
-        tc_fence_after();
+        added(j - 1);
 #pragma unroll
-        for (int q = 0; q < D / 16; ++q) {
-          float o[16];
-          tmem_ld16(to + q * 16, o);
+        for (int q = 0; q < D / 32; ++q) {
+          float o[32];
+          tmem_ld32(to + q * 32, o);
+          tmem_ld_wait();
+          tmem_loaded(o);
+          uint32_t kept[32];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] *= keep;
-          tmem_st16(to + q * 16, o);
+          for (int e = 0; e < 32; ++e) kept[e] = __float_as_uint(o[e] * keep);
+          tmem_st(to + q * 32, kept);
         }
       }
       const float base = ref == -INFINITY ? 0.f : PtType<T>::kBias - ref * c;
-      float2 sum = make_float2(0.f, 0.f);
+      float2 sums[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sums[q] = make_float2(0.f, 0.f);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         uint32_t packed[16];
@@ -424,29 +558,36 @@ __global__ void __launch_bounds__(kPtThreads, 1)
         for (int e = 0; e < 16; ++e) {
           const float2 y = fma2(make_float2(s[q][2 * e], s[q][2 * e + 1]), make_float2(c, c), make_float2(base, base));
           const float2 x = make_float2(ex2(y.x), ex2(y.y));
-          sum = add2(sum, x);
+          sums[e % 4] = add2(sums[e % 4], x);
           packed[e] = X::pack(x.x, x.y);
         }
         tmem_st(ts + q * 16, packed);
+        if (q == 1 && j > w.first) added(j - 1);
+        if (q % 2) {  // half of the weights: their product may begin
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive_cta(&p_full[2 * buf + q / 2]);
+        }
       }
+      const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
       l += sum.x + sum.y;
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive_cta(&p_full[i]);
+      // the next block's number is two on while both tiles have one, else the next
+      buf += j + 1 < both ? 2 : j + 1 == both ? 2 - i : 1;
+      if (buf >= S::kScores) buf -= S::kScores, phase ^= 1;
     }
-    if (ok && ends[i] > w.first) ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[i], (ends[i] - 1 - w.first) & 1, p.err, kSpinLimitCycles));
-    tc_fence_after();
+    if (ends[i] > w.first) added(ends[i] - 1);
     const bool whole = gridDim.y == 1;
     const long long at = (static_cast<long long>(w.q0 + index)) * p.n_heads + h;
     const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
     const bool fix = *marked;
-    if (tokens[i] && ok) {
+    if (tokens[i]) {
 #pragma unroll
       for (int q = 0; q < D / 32; ++q) {
         float o[32];
         if (ends[i] > w.first) {
           tmem_ld32(to + q * 32, o);
           tmem_ld_wait();
+          tmem_loaded(o);
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
