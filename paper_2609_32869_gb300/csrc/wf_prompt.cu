@@ -487,14 +487,16 @@ __global__ void __launch_bounds__(kPtThreads, 1)
     // the least of the tile's limits: blocks below it need no mask
     const int least = tokens[i] ? pt_limit(w, p.causal, w.token + i * p.tokens) : 0;
     const float c = p.scale * 1.4426950408889634f;
-    float ref = -INFINITY, l = 0.f;
+    float ref = -INFINITY, base = 0.f, l = 0.f;  // weights are 2^(score c + base)
+    bool unset = true;  // some row of the warp has no reference
     PtWaits waits = {p.err, kSpinLimitCycles};
     // Waits until the products of the tile's block j are in its sums.  Every
     // block's in turn: a barrier tells a phase from the one before it, not from
     // the one before that.
     int waited = w.first;
     const auto added = [&](int j) {
-      if (waited > j) return;
+      // (with two buffers and two tiles a tile's scores are behind its last products)
+      if (waited > j || (S::kScores == 2 && j + 1 < both)) return;
       waited = j + 1;
       pt_wait(waits, smem_u32(&o_done[i]), (j - w.first) & 1);
       tc_fence_after();
@@ -505,35 +507,39 @@ __global__ void __launch_bounds__(kPtThreads, 1)
       const uint32_t ts = tmem + buf * 128 + lanes;
       pt_wait(waits, smem_u32(s_full) + buf * 8, phase);
       tc_fence_after();
-      float s[4][32], mx[4];
+      float s[4][32];
+      const int seen = limit - j * kPtKeys;
+      const bool mask = (j + 1) * kPtKeys > least;
+      const auto load = [&](int q) {
+        tmem_ld32(ts + q * 32, s[q]);
+      };
+      // (one branch around all of it: a select for each column would cost as much as the rest)
+      const auto loaded = [&](int first, int last) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) tmem_ld32(ts + q * 32, s[q]);
-      tmem_ld_wait();
+        for (int q = first; q < last; ++q) tmem_loaded(s[q]);
+        if (mask) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) tmem_loaded(s[q]);
-      if ((j + 1) * kPtKeys > least) {
-        const int seen = limit - j * kPtKeys;
+          for (int q = first; q < last; ++q)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (q * 32 + e >= seen) s[q][e] = -INFINITY;
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
+            for (int e = 0; e < 32; ++e)
+              if (q * 32 + e >= seen) s[q][e] = -INFINITY;
+        }
+      };
+      const auto largest = [&](int q) {
         float m0 = max3(s[q][0], s[q][1], s[q][2]), m1 = max3(s[q][3], s[q][4], s[q][5]);
 #pragma unroll
         for (int e = 6; e < 30; e += 4) m0 = max3(m0, s[q][e], s[q][e + 1]), m1 = max3(m1, s[q][e + 2], s[q][e + 3]);
-        mx[q] = max3(fmaxf(m0, m1), s[q][30], s[q][31]);
-      }
-      const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-      if (j == w.first) {
-        ref = top;
-      } else if (__any_sync(0xffffffffu, (top - ref) * c > 8.f)) {
-        const float next = fmaxf(top, ref);
+        return max3(fmaxf(m0, m1), s[q][30], s[q][31]);
+      };
+      // Brings the reference up to the block's maximum, and the sums with it.
+      const auto raise = [&]() {
+        const float next = fmaxf(fmaxf(max3(largest(0), largest(1), largest(2)), largest(3)), ref);
         const float keep = ref == -INFINITY ? 0.f : ex2((ref - next) * c);
         ref = next;
+        base = ref == -INFINITY ? 0.f : PtType<T>::kBias - ref * c;
+        unset = __any_sync(0xffffffffu, ref == -INFINITY);
         l *= keep;
+        if (j == w.first) return;
         added(j - 1);
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
@@ -546,29 +552,64 @@ __global__ void __launch_bounds__(kPtThreads, 1)
           for (int e = 0; e < 32; ++e) kept[e] = __float_as_uint(o[e] * keep);
           tmem_st(to + q * 32, kept);
         }
-      }
-      const float base = ref == -INFINITY ? 0.f : PtType<T>::kBias - ref * c;
+      };
+      uint32_t packed[32];
       float2 sums[4];
+      // Weights of 64 columns: pair by pair in three steps that are some pairs
+      // apart, so that no instruction waits for the one before it and the
+      // exponentials, which take the longest, have the others between them.
+      const auto weights = [&](int half, auto between) {
+        constexpr int kAhead = 6, kBehind = 4;
+        float(&x)[2][32] = *reinterpret_cast<float(*)[2][32]>(&s[2 * half]);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sums[q] = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t packed[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float2 y = fma2(make_float2(s[q][2 * e], s[q][2 * e + 1]), make_float2(c, c), make_float2(base, base));
-          const float2 x = make_float2(ex2(y.x), ex2(y.y));
-          sums[e % 4] = add2(sums[e % 4], x);
-          packed[e] = X::pack(x.x, x.y);
+        for (int g = -kAhead; g < 32 + kBehind; ++g) {
+          const int f = g + kAhead, h = g - kBehind;
+          if (f < 32) {
+            const float2 y = fma2(make_float2(x[f / 16][f % 16 * 2], x[f / 16][f % 16 * 2 + 1]), make_float2(c, c), make_float2(base, base));
+            x[f / 16][f % 16 * 2] = y.x, x[f / 16][f % 16 * 2 + 1] = y.y;
+          }
+          if (g >= 0 && g < 32) x[g / 16][g % 16 * 2] = ex2(x[g / 16][g % 16 * 2]);
+          if (h >= 0) {
+            const float2 v = make_float2(x[h / 16][h % 16 * 2], x[h / 16][h % 16 * 2 + 1]);
+            sums[h % 4] = half == 0 && h < 4 ? v : add2(sums[h % 4], v);
+            packed[h] = X::pack(v.x, v.y);
+          }
+          if (g >= 0 && g < 32) x[g / 16][g % 16 * 2 + 1] = ex2(x[g / 16][g % 16 * 2 + 1]);
+          between(g);
         }
-        tmem_st(ts + q * 16, packed);
-        if (q == 1 && j > w.first) added(j - 1);
-        if (q % 2) {  // half of the weights: their product may begin
-          tmem_st_wait();
-          tc_fence_before();
-          mbar_arrive_cta(&p_full[2 * buf + q / 2]);
+      };
+      const auto nothing = [](int) {};
+      load(0), load(1), load(2), load(3);
+      tmem_ld_wait();
+      loaded(0, 4);
+      // A row's reference is the maximum of its first block, and then stands
+      // while the weights stay below 2^16, which the first half's sum and the
+      // second half's maximum tell before any of them is handed over.
+      if (unset) raise();
+      weights(0, nothing);
+      {
+        const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
+        const float most = fmaxf(largest(2), largest(3));
+        if (__any_sync(0xffffffffu, sum.x + sum.y > 65000.f || fmaf(most, c, base) > 15.9f)) {
+          load(0), load(1);
+          tmem_ld_wait();
+          loaded(0, 2);
+          raise();
+          weights(0, nothing);
         }
       }
+      if (j > w.first) added(j - 1);
+      tmem_st(ts, packed);
+      weights(1, [&](int g) {
+        if (g != 2) return;  // the stores have had time; the product of the first half may begin
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive_cta(&p_full[2 * buf]);
+      });
+      tmem_st(ts + 32, packed);
+      tmem_st_wait();
+      tc_fence_before();
+      mbar_arrive_cta(&p_full[2 * buf + 1]);
       const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
       l += sum.x + sum.y;
       // the next block's number is two on while both tiles have one, else the next
