@@ -21,7 +21,6 @@
 
 namespace wf {
 
-constexpr int kPtKeys = 128;     // keys of a block
 constexpr int kPtThreads = 384;  // four warps a tile, one for the products, one for the copies, two that look V over
 constexpr int kPtMma = 8, kPtLoad = 9, kPtScrub = 10;  // warps
 
@@ -38,20 +37,29 @@ struct PromptParams {
   uint32_t *err;
 };
 
+// At 128 dims a CTA has the SM: blocks of 128 keys, all of TMEM.  At 64 dims
+// the exponentials are as much work as the products and eight warps do not
+// keep their unit busy, so two CTAs share the SM, with blocks of 64 keys:
+// 32 x 1500 frames, 20 heads took 442 us with one CTA, 128 keys and a third
+// buffer of scores.
 template <int D>
 struct PtShape {
-  static constexpr int kHalf = 16384;            // 128 rows of 64 dims
-  static constexpr int kTile = kHalf * D / 64;   // queries, keys or values
-  static constexpr int kStages = D == 64 ? 4 : 2;  // of keys, and of values
-  // Buffers of scores in TMEM beside the tiles' sums: with a third one the scores
-  // of a tile's next block are there before its last ones are done with.
-  static constexpr int kScores = D == 64 ? 3 : 2;
-  static constexpr int kSumCol = kScores * 128;
-  static constexpr int kMarkOff = 2 * kTile + 2 * kStages * kTile;  // [3][D] first position of a value that is not finite
+  static constexpr int kKeys = D == 64 ? 64 : 128;  // of a block
+  static constexpr int kParts = kKeys / 64;         // in which a block's weights are handed over
+  static constexpr int kPerSm = D == 64 ? 2 : 1;
+  static constexpr int kHalf = 16384;               // 128 rows of 64 dims
+  static constexpr int kTile = kHalf * D / 64;      // queries
+  static constexpr int kKvHalf = kKeys * 128, kKv = kKvHalf * D / 64;  // keys or values
+  static constexpr int kStages = D == 64 ? 4 : 2;   // of keys, and of values
+  static constexpr int kScores = 2;                 // buffers of scores in TMEM, before the tiles' sums
+  static constexpr int kSumCol = kScores * kKeys;
+  static constexpr uint32_t kCols = D == 64 ? 256 : 512;
+  static constexpr int kRegsMore = D == 64 ? 96 : 208, kRegsLess = D == 64 ? 48 : 88;
+  static constexpr int kMarkOff = 2 * kTile + 2 * kStages * kKv;  // [3][D] first position of a value that is not finite
   static constexpr int kBarOff = kMarkOff + 3 * D * 4;
-  static constexpr int kBars = 2 + 6 * kStages + 3 * kScores + 2 + 1;
+  static constexpr int kBars = 2 + 6 * kStages + (1 + kParts) * kScores + 2 + 1;
   static constexpr int kSmem = 1024 + kBarOff + kBars * 8 + 64;
-  static constexpr uint32_t kCols = 512;
+  static_assert(kSumCol + 2 * D <= static_cast<int>(kCols), "");
 };
 
 // A warp's waits on barriers, all lanes together.  After one that gave up the
@@ -255,20 +263,20 @@ struct PtType<__half> {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kPtThreads, 1)
+__global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
     prompt_attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                             const PromptParams p) {
   using X = Type16<T>;
   using S = PtShape<D>;
-  constexpr int kStages = S::kStages;
+  constexpr int kStages = S::kStages, kKeys = S::kKeys, kParts = S::kParts;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-  uint8_t *sq = smem, *sk = smem + 2 * S::kTile, *sv = sk + kStages * S::kTile;
+  uint8_t *sq = smem, *sk = smem + 2 * S::kTile, *sv = sk + kStages * S::kKv;
   int *mark = reinterpret_cast<int *>(smem + S::kMarkOff);
   uint64_t *q_full = reinterpret_cast<uint64_t *>(smem + S::kBarOff);
   uint64_t *k_full = q_full + 2, *k_empty = k_full + kStages, *v_full = k_empty + kStages, *v_empty = v_full + kStages;
   uint64_t *look = v_empty + kStages, *clean = look + kStages;
-  uint64_t *s_full = clean + kStages, *p_full = s_full + S::kScores, *o_done = p_full + 2 * S::kScores, *done = o_done + 2;
+  uint64_t *s_full = clean + kStages, *p_full = s_full + S::kScores, *o_done = p_full + kParts * S::kScores, *done = o_done + 2;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(done + 1);
   int *has_work = reinterpret_cast<int *>(tmem_slot + 1);
   volatile int *marked = has_work + 1;
@@ -284,7 +292,7 @@ __global__ void __launch_bounds__(kPtThreads, 1)
     if (any) {
       // key blocks that any row of this CTA sees, and this split's share of them
       const int last_token = min(w.token + p.tokens * p.tiles, w.rows) - 1;
-      const int blocks = (pt_limit(w, p.causal, last_token) + kPtKeys - 1) / kPtKeys;
+      const int blocks = (pt_limit(w, p.causal, last_token) + kKeys - 1) / kKeys;
       const int share = (blocks + gridDim.y - 1) / gridDim.y;
       w.first = min(static_cast<int>(blockIdx.y) * share, blocks), w.last = min(w.first + share, blocks);
     }
@@ -296,7 +304,8 @@ __global__ void __launch_bounds__(kPtThreads, 1)
       mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1), mbar_init(&v_full[i], 1), mbar_init(&v_empty[i], 1);
       mbar_init(&look[i], 1), mbar_init(&clean[i], 64);
     }
-    for (int i = 0; i < S::kScores; ++i) mbar_init(&s_full[i], 1), mbar_init(&p_full[2 * i], 128), mbar_init(&p_full[2 * i + 1], 128);
+    for (int i = 0; i < S::kScores; ++i) mbar_init(&s_full[i], 1);
+    for (int i = 0; i < kParts * S::kScores; ++i) mbar_init(&p_full[i], 128);
     mbar_init(done, 1);
     fence_barrier_init();
     fence_proxy_async();
@@ -320,19 +329,21 @@ __global__ void __launch_bounds__(kPtThreads, 1)
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int seen = tokens[i] ? pt_limit(w, p.causal, w.token + i * p.tokens + tokens[i] - 1) : 0;
-    ends[i] = max(min((seen + kPtKeys - 1) / kPtKeys, w.last), w.first);
+    ends[i] = max(min((seen + kKeys - 1) / kKeys, w.last), w.first);
   }
   const int end = max(ends[0], ends[1]);
   // blocks from here on hold positions that some row does not see
-  const int edge = any_work ? pt_limit(w, p.causal, w.token) / kPtKeys : 0;
+  const int edge = any_work ? pt_limit(w, p.causal, w.token) / kKeys : 0;
   // The products go through the blocks, tile by tile; number n is block j of tile
   // i, its scores in buffer n % kScores.
   const int both = min(ends[0], ends[1]);  // blocks before it are both tiles'
   const int products = ends[0] + ends[1] - 2 * w.first;
 
-  // The block's 384 threads have 168 registers each: 256 take 208, 128 keep 88.
+  // The block's 384 threads were launched with 168 registers each, or 80 where
+  // there are two CTAs: 256 take 208 (96), 128 keep 88 (48).
+  static_assert(256 * S::kRegsMore + 128 * S::kRegsLess == kPtThreads * (S::kPerSm == 1 ? 168 : 80), "");
   if (warp >= kPtMma) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kRegsLess));
     if (warp == kPtLoad) {
       if (lane == 0 && w.first < end) {
         tma_prefetch_desc(&mq), tma_prefetch_desc(&mk), tma_prefetch_desc(&mv);
@@ -350,16 +361,16 @@ __global__ void __launch_bounds__(kPtThreads, 1)
           const uint32_t before = ((n / kStages) - 1) & 1;
           if (n >= kStages) ok = mbar_wait(&k_empty[st], before, p.err, kSpinLimitCycles);
           if (!ok) break;
-          mbar_arrive_expect_tx(&k_full[st], S::kTile);
-          for (int c = 0; c < D / 64; ++c) tma_load_3d(sk + st * S::kTile + c * S::kHalf, &mk, c * 64, head, w.k0 + j * kPtKeys, &k_full[st]);
+          mbar_arrive_expect_tx(&k_full[st], S::kKv);
+          for (int c = 0; c < D / 64; ++c) tma_load_3d(sk + st * S::kKv + c * S::kKvHalf, &mk, c * 64, head, w.k0 + j * kKeys, &k_full[st]);
           if (n == 0 && ends[1] > w.first) load_q(1);
           if (n >= kStages) ok = mbar_wait(&v_empty[st], before, p.err, kSpinLimitCycles);
           if (!ok) {
             mbar_drain(&k_full[st], (n / kStages) & 1);
             break;
           }
-          mbar_arrive_expect_tx(&v_full[st], S::kTile);
-          for (int c = 0; c < D / 64; ++c) tma_load_3d(sv + st * S::kTile + c * S::kHalf, &mv, c * 64, head, w.k0 + j * kPtKeys, &v_full[st]);
+          mbar_arrive_expect_tx(&v_full[st], S::kKv);
+          for (int c = 0; c < D / 64; ++c) tma_load_3d(sv + st * S::kKv + c * S::kKvHalf, &mv, c * 64, head, w.k0 + j * kKeys, &v_full[st]);
           // The stage's earlier copies have landed: only now is the parity of its barrier one to wait for.
           if (j >= edge) mbar_arrive_cta(&look[st]);
         }
@@ -374,7 +385,7 @@ __global__ void __launch_bounds__(kPtThreads, 1)
     } else if (warp == kPtMma) {
       if (w.first < end) {
         const uint32_t lead = elect_one();
-        constexpr uint32_t kIdS = pt_idesc<T>(kPtKeys, false), kIdO = pt_idesc<T>(D, true);
+        constexpr uint32_t kIdS = pt_idesc<T>(kKeys, false), kIdO = pt_idesc<T>(D, true);
         const uint64_t dq = umma_desc_sw128(smem_u32(sq)), dk = umma_desc_sw128(smem_u32(sk)), dv = pt_desc_v(smem_u32(sv));
         const uint32_t bars = smem_u32(q_full);
         const auto at = [&](const uint64_t *bar) { return bars + static_cast<uint32_t>(bar - q_full) * 8; };
@@ -388,12 +399,11 @@ __global__ void __launch_bounds__(kPtThreads, 1)
           if (qi == 0 || qj >= ends[0]) pt_wait(waits, at(k_full) + q_st * 8, q_phase);
           if (qj == w.first) pt_wait(waits, at(q_full) + qi * 8, 0);
           tc_fence_after();
-          const uint64_t a = dq + qi * (S::kTile >> 4), b = dk + q_st * (S::kTile >> 4);
-          const uint32_t d = tmem + q_buf * 128;
+          const uint64_t a = dq + qi * (S::kTile >> 4), b = dk + q_st * (S::kKv >> 4);
+          const uint32_t d = tmem + q_buf * kKeys;
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
-            const uint32_t off = (k / 4 * S::kHalf + k % 4 * 32) >> 4;
-            pt_mma_ss(lead, d, a + off, b + off, kIdS, k > 0);
+            pt_mma_ss(lead, d, a + ((k / 4 * S::kHalf + k % 4 * 32) >> 4), b + ((k / 4 * S::kKvHalf + k % 4 * 32) >> 4), kIdS, k > 0);
           }
           pt_commit(lead, at(s_full) + q_buf * 8);
           q_buf = q_buf + 1 == S::kScores ? 0 : q_buf + 1;
@@ -414,17 +424,16 @@ __global__ void __launch_bounds__(kPtThreads, 1)
             pt_wait(waits, at(v_full) + p_st * 8, v_phase);
             if (pj >= edge) pt_wait(waits, at(clean) + p_st * 8, (pj - max(edge, w.first)) / kStages & 1);
           }
-          const uint64_t b = dv + p_st * (S::kTile >> 4);
-          const uint32_t d = tmem + S::kSumCol + pi * D, a = tmem + p_buf * 128;
+          const uint64_t b = dv + p_st * (S::kKv >> 4);
+          const uint32_t d = tmem + S::kSumCol + pi * D, a = tmem + p_buf * kKeys;
           const uint32_t more = pj > w.first;
-          pt_wait(waits, at(p_full) + p_buf * 16, p_phase);
-          tc_fence_after();
 #pragma unroll
-          for (int k = 0; k < kPtKeys / 32; ++k) pt_mma_ts(lead, d, a + k * 8, b + ((k * 2048) >> 4), kIdO, k > 0 ? 1u : more);
-          pt_wait(waits, at(p_full) + p_buf * 16 + 8, p_phase);
-          tc_fence_after();
+          for (int h = 0; h < kParts; ++h) {
+            pt_wait(waits, at(p_full) + (p_buf * kParts + h) * 8, p_phase);
+            tc_fence_after();
 #pragma unroll
-          for (int k = kPtKeys / 32; k < kPtKeys / 16; ++k) pt_mma_ts(lead, d, a + k * 8, b + ((k * 2048) >> 4), kIdO, 1);
+            for (int k = 4 * h; k < 4 * h + 4; ++k) pt_mma_ts(lead, d, a + k * 8, b + ((k * 2048) >> 4), kIdO, k > 0 ? 1u : more);
+          }
           pt_commit(lead, at(o_done) + pi * 8);
           if (++p_buf == S::kScores) p_buf = 0, p_phase ^= 1;
           if (pi == 0 && pj < ends[1]) {
@@ -450,10 +459,10 @@ __global__ void __launch_bounds__(kPtThreads, 1)
         if (!__all_sync(0xffffffffu, mbar_wait(&look[st], (j - max(edge, w.first)) / kStages & 1, p.err, kSpinLimitCycles) &&
                                          mbar_wait(&v_full[st], (n / kStages) & 1, p.err, kSpinLimitCycles)))
           break;
-        const int held = w.keys - j * kPtKeys;
-        for (int c = threadIdx.x - kPtScrub * 32; c < S::kTile / 16; c += 64) {
-          uint4 *at = reinterpret_cast<uint4 *>(sv + st * S::kTile + c * 16);
-          const int row = c / 8 % 128;
+        const int held = w.keys - j * kKeys;
+        for (int c = threadIdx.x - kPtScrub * 32; c < S::kKv / 16; c += 64) {
+          uint4 *at = reinterpret_cast<uint4 *>(sv + st * S::kKv + c * 16);
+          const int row = c / 8 % kKeys;
           if (row >= held) {
             *at = make_uint4(0, 0, 0, 0);
             continue;
@@ -463,11 +472,11 @@ __global__ void __launch_bounds__(kPtThreads, 1)
           const uint32_t most = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
           if (max(most & 0xffff, most >> 16) < PtType<T>::kInf) continue;
           uint16_t *e = reinterpret_cast<uint16_t *>(at);
-          const int dim = c / 1024 * 64 + ((c & 7) ^ (row & 7)) * 8;
+          const int dim = c / (8 * kKeys) * 64 + ((c & 7) ^ (row & 7)) * 8;
           for (int i = 0; i < 8; ++i) {
             const uint32_t u = e[i] & 0x7fff;
             if (u < PtType<T>::kInf) continue;
-            atomicMin(&mark[(u > PtType<T>::kInf ? 0 : e[i] >> 15 ? 2 : 1) * D + dim + i], j * kPtKeys + row);
+            atomicMin(&mark[(u > PtType<T>::kInf ? 0 : e[i] >> 15 ? 2 : 1) * D + dim + i], j * kKeys + row);
             e[i] = 0;
             *marked = 1;
           }
@@ -477,7 +486,7 @@ __global__ void __launch_bounds__(kPtThreads, 1)
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kRegsMore));
     const int i = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t to = tmem + S::kSumCol + i * D + lanes;
@@ -504,12 +513,12 @@ __global__ void __launch_bounds__(kPtThreads, 1)
     int buf = w.first < both ? i : 0;  // of the scores, and the parity of its barrier
     uint32_t phase = 0;
     for (int j = w.first; j < ends[i]; ++j) {
-      const uint32_t ts = tmem + buf * 128 + lanes;
+      const uint32_t ts = tmem + buf * kKeys + lanes;
       pt_wait(waits, smem_u32(s_full) + buf * 8, phase);
       tc_fence_after();
-      float s[4][32];
-      const int seen = limit - j * kPtKeys;
-      const bool mask = (j + 1) * kPtKeys > least;
+      float s[2 * kParts][32];
+      const int seen = limit - j * kKeys;
+      const bool mask = (j + 1) * kKeys > least;
       const auto load = [&](int q) {
         tmem_ld32(ts + q * 32, s[q]);
       };
@@ -533,7 +542,8 @@ __global__ void __launch_bounds__(kPtThreads, 1)
       };
       // Brings the reference up to the block's maximum, and the sums with it.
       const auto raise = [&]() {
-        const float next = fmaxf(fmaxf(max3(largest(0), largest(1), largest(2)), largest(3)), ref);
+        float next = max3(largest(0), largest(1), ref);
+        if constexpr (kParts == 2) next = max3(largest(2), largest(3), next);
         const float keep = ref == -INFINITY ? 0.f : ex2((ref - next) * c);
         ref = next;
         base = ref == -INFINITY ? 0.f : PtType<T>::kBias - ref * c;
@@ -552,6 +562,10 @@ __global__ void __launch_bounds__(kPtThreads, 1)
           for (int e = 0; e < 32; ++e) kept[e] = __float_as_uint(o[e] * keep);
           tmem_st(to + q * 32, kept);
         }
+        // (read again rather than held in registers meanwhile)
+        load(0), load(1);
+        tmem_ld_wait();
+        loaded(0, 2);
       };
       uint32_t packed[32];
       float2 sums[4];
@@ -579,18 +593,20 @@ __global__ void __launch_bounds__(kPtThreads, 1)
         }
       };
       const auto nothing = [](int) {};
-      load(0), load(1), load(2), load(3);
+#pragma unroll
+      for (int q = 0; q < 2 * kParts; ++q) load(q);
       tmem_ld_wait();
-      loaded(0, 4);
+      loaded(0, 2 * kParts);
       // A row's reference is the maximum of its first block, and then stands
-      // while the weights stay below 2^16, which the first half's sum and the
-      // second half's maximum tell before any of them is handed over.
+      // while the weights stay below 2^16, which the first part's sum and the
+      // second part's maximum tell before any of them is handed over.
       if (unset) raise();
       weights(0, nothing);
       {
         const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
-        const float most = fmaxf(largest(2), largest(3));
-        if (__any_sync(0xffffffffu, sum.x + sum.y > 65000.f || fmaf(most, c, base) > 15.9f)) {
+        bool above = sum.x + sum.y > 65000.f;
+        if constexpr (kParts == 2) above |= fmaf(fmaxf(largest(2), largest(3)), c, base) > 15.9f;
+        if (__any_sync(0xffffffffu, above)) {
           load(0), load(1);
           tmem_ld_wait();
           loaded(0, 2);
@@ -600,16 +616,18 @@ __global__ void __launch_bounds__(kPtThreads, 1)
       }
       if (j > w.first) added(j - 1);
       tmem_st(ts, packed);
-      weights(1, [&](int g) {
-        if (g != 2) return;  // the stores have had time; the product of the first half may begin
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive_cta(&p_full[2 * buf]);
-      });
-      tmem_st(ts + 32, packed);
+      if constexpr (kParts == 2) {
+        weights(1, [&](int g) {
+          if (g != 2) return;  // the stores have had time; the product of the first part may begin
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive_cta(&p_full[2 * buf]);
+        });
+        tmem_st(ts + 32, packed);
+      }
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive_cta(&p_full[2 * buf + 1]);
+      mbar_arrive_cta(&p_full[kParts * buf + kParts - 1]);
       const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
       l += sum.x + sum.y;
       // the next block's number is two on while both tiles have one, else the next
@@ -722,9 +740,8 @@ static PtPlan pt_plan(int64_t n_seq, int64_t n_q, int64_t max_k, int64_t heads, 
   const auto items = [&](int tiles) { return std::min(n_q, n_q / (a.tokens * tiles) + n_seq); };
   a.tiles = items(2) * heads >= kSms ? 2 : 1;
   a.items = items(a.tiles);
-  // Few rows behind many keys: cut until there are four CTAs an SM, eight blocks of keys each at least.
-  const int64_t blocks = (max_k + kPtKeys - 1) / kPtKeys;
-  a.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({blocks / 8, kSms * 4 / std::max<int64_t>(1, a.items * heads), 64})));
+  // Few rows behind many keys: cut until there are four CTAs an SM, 1024 keys each at least.
+  a.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({max_k / 1024, kSms * 4 / std::max<int64_t>(1, a.items * heads), 64})));
   return a;
 }
 
@@ -819,7 +836,7 @@ wf_status wf_prompt_attention(const void *d_q, int64_t q_stride, const void *d_k
   for (int i = 0; i < 2; ++i) {  // keys, values: dims, heads, rows
     const cuuint64_t size[3] = {dim, static_cast<cuuint64_t>(n_kv_heads), static_cast<cuuint64_t>(std::max(n_k, 1))};
     const cuuint64_t stride[2] = {dim * 2, static_cast<cuuint64_t>(i ? v_stride : k_stride) * 2};
-    const cuuint32_t box[3] = {64, 1, kPtKeys};
+    const cuuint32_t box[3] = {64, 1, static_cast<cuuint32_t>(head_dim == 64 ? PtShape<64>::kKeys : PtShape<128>::kKeys)};
     if (encode(i ? &mv : &mk, type, 3, const_cast<void *>(i ? d_v : d_k), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return WF_ERR_CUDA;
