@@ -50,14 +50,14 @@ struct PtShape {
   static constexpr int kHalf = 16384;               // 128 rows of 64 dims
   static constexpr int kTile = kHalf * D / 64;      // queries
   static constexpr int kKvHalf = kKeys * 128, kKv = kKvHalf * D / 64;  // keys or values
-  static constexpr int kStages = D == 64 ? 4 : 2;   // of keys, and of values
+  static constexpr int kKStages = D == 64 ? 4 : 2, kVStages = D == 64 ? 4 : 3;
   static constexpr int kScores = 2;                 // buffers of scores in TMEM, before the tiles' sums
   static constexpr int kSumCol = kScores * kKeys;
   static constexpr uint32_t kCols = D == 64 ? 256 : 512;
   static constexpr int kRegsMore = D == 64 ? 96 : 208, kRegsLess = D == 64 ? 48 : 88;
-  static constexpr int kMarkOff = 2 * kTile + 2 * kStages * kKv;  // [3][D] first position of a value that is not finite
+  static constexpr int kMarkOff = 2 * kTile + (kKStages + kVStages) * kKv;  // [3][D] first position of a value that is not finite
   static constexpr int kBarOff = kMarkOff + 3 * D * 4;
-  static constexpr int kBars = 2 + 6 * kStages + (1 + kParts) * kScores + 2 + 1;
+  static constexpr int kBars = 2 + 2 * kKStages + 4 * kVStages + (1 + kParts) * kScores + 2 + 1;
   static constexpr int kSmem = 1024 + kBarOff + kBars * 8 + 64;
   static_assert(kSumCol + 2 * D <= static_cast<int>(kCols), "");
 };
@@ -268,15 +268,15 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
                             const PromptParams p) {
   using X = Type16<T>;
   using S = PtShape<D>;
-  constexpr int kStages = S::kStages, kKeys = S::kKeys, kParts = S::kParts;
+  constexpr int kKStages = S::kKStages, kVStages = S::kVStages, kKeys = S::kKeys, kParts = S::kParts;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-  uint8_t *sq = smem, *sk = smem + 2 * S::kTile, *sv = sk + kStages * S::kKv;
+  uint8_t *sq = smem, *sk = smem + 2 * S::kTile, *sv = sk + kKStages * S::kKv;
   int *mark = reinterpret_cast<int *>(smem + S::kMarkOff);
   uint64_t *q_full = reinterpret_cast<uint64_t *>(smem + S::kBarOff);
-  uint64_t *k_full = q_full + 2, *k_empty = k_full + kStages, *v_full = k_empty + kStages, *v_empty = v_full + kStages;
-  uint64_t *look = v_empty + kStages, *clean = look + kStages;
-  uint64_t *s_full = clean + kStages, *p_full = s_full + S::kScores, *o_done = p_full + kParts * S::kScores, *done = o_done + 2;
+  uint64_t *k_full = q_full + 2, *k_empty = k_full + kKStages, *v_full = k_empty + kKStages, *v_empty = v_full + kVStages;
+  uint64_t *look = v_empty + kVStages, *clean = look + kVStages;
+  uint64_t *s_full = clean + kVStages, *p_full = s_full + S::kScores, *o_done = p_full + kParts * S::kScores, *done = o_done + 2;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(done + 1);
   int *has_work = reinterpret_cast<int *>(tmem_slot + 1);
   volatile int *marked = has_work + 1;
@@ -300,12 +300,13 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
   }
   if (threadIdx.x == 32) {
     for (int i = 0; i < 2; ++i) mbar_init(&q_full[i], 1), mbar_init(&o_done[i], 1);
-    for (int i = 0; i < kStages; ++i) {
-      mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1), mbar_init(&v_full[i], 1), mbar_init(&v_empty[i], 1);
+    for (int i = 0; i < kKStages; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
+    for (int i = 0; i < kVStages; ++i) {
+      mbar_init(&v_full[i], 1), mbar_init(&v_empty[i], 1);
       mbar_init(&look[i], 1), mbar_init(&clean[i], 64);
     }
     for (int i = 0; i < S::kScores; ++i) mbar_init(&s_full[i], 1);
-    for (int i = 0; i < kParts * S::kScores; ++i) mbar_init(&p_full[i], 128);
+    for (int i = 0; i < kParts * S::kScores; ++i) mbar_init(&p_full[i], 4);
     mbar_init(done, 1);
     fence_barrier_init();
     fence_proxy_async();
@@ -357,30 +358,27 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
         int n = 0;  // blocks so far, keys and values
         bool ok = true;
         for (int j = w.first; j < end && ok; ++j, ++n) {
-          const int st = n % kStages;
-          const uint32_t before = ((n / kStages) - 1) & 1;
-          if (n >= kStages) ok = mbar_wait(&k_empty[st], before, p.err, kSpinLimitCycles);
+          const int ks = n % kKStages, vs = n % kVStages;
+          if (n >= kKStages) ok = mbar_wait(&k_empty[ks], ((n / kKStages) - 1) & 1, p.err, kSpinLimitCycles);
           if (!ok) break;
-          mbar_arrive_expect_tx(&k_full[st], S::kKv);
-          for (int c = 0; c < D / 64; ++c) tma_load_3d(sk + st * S::kKv + c * S::kKvHalf, &mk, c * 64, head, w.k0 + j * kKeys, &k_full[st]);
+          mbar_arrive_expect_tx(&k_full[ks], S::kKv);
+          for (int c = 0; c < D / 64; ++c) tma_load_3d(sk + ks * S::kKv + c * S::kKvHalf, &mk, c * 64, head, w.k0 + j * kKeys, &k_full[ks]);
           if (n == 0 && ends[1] > w.first) load_q(1);
-          if (n >= kStages) ok = mbar_wait(&v_empty[st], before, p.err, kSpinLimitCycles);
+          if (n >= kVStages) ok = mbar_wait(&v_empty[vs], ((n / kVStages) - 1) & 1, p.err, kSpinLimitCycles);
           if (!ok) {
-            mbar_drain(&k_full[st], (n / kStages) & 1);
+            mbar_drain(&k_full[ks], (n / kKStages) & 1);
             break;
           }
-          mbar_arrive_expect_tx(&v_full[st], S::kKv);
-          for (int c = 0; c < D / 64; ++c) tma_load_3d(sv + st * S::kKv + c * S::kKvHalf, &mv, c * 64, head, w.k0 + j * kKeys, &v_full[st]);
+          mbar_arrive_expect_tx(&v_full[vs], S::kKv);
+          for (int c = 0; c < D / 64; ++c) tma_load_3d(sv + vs * S::kKv + c * S::kKvHalf, &mv, c * 64, head, w.k0 + j * kKeys, &v_full[vs]);
           // The stage's earlier copies have landed: only now is the parity of its barrier one to wait for.
-          if (j >= edge) mbar_arrive_cta(&look[st]);
+          if (j >= edge) mbar_arrive_cta(&look[vs]);
         }
         // a wait gave up, here or in another warp: the copies still have to land before the CTA ends
         for (int i = 0; i < 2; ++i)
           if (ends[i] > w.first) mbar_drain(&q_full[i], 0);
-        for (int i = max(0, n - kStages); i < n; ++i) {
-          mbar_drain(&k_full[i % kStages], (i / kStages) & 1);
-          mbar_drain(&v_full[i % kStages], (i / kStages) & 1);
-        }
+        for (int i = max(0, n - kKStages); i < n; ++i) mbar_drain(&k_full[i % kKStages], (i / kKStages) & 1);
+        for (int i = max(0, n - kVStages); i < n; ++i) mbar_drain(&v_full[i % kVStages], (i / kVStages) & 1);
       }
     } else if (warp == kPtMma) {
       if (w.first < end) {
@@ -395,17 +393,19 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
         int qj = w.first, qi = qj < ends[0] ? 0 : 1, q_buf = 0, q_st = 0;
         int pj = qj, pi = qi, p_buf = 0, p_st = 0;
         uint32_t q_phase = 0, p_phase = 0, v_phase = 0;
-        const auto scores = [&]() {
+        const auto scores_inputs = [&]() {
           if (qi == 0 || qj >= ends[0]) pt_wait(waits, at(k_full) + q_st * 8, q_phase);
           if (qj == w.first) pt_wait(waits, at(q_full) + qi * 8, 0);
-          tc_fence_after();
+        };
+        const auto scores = [&]() {
           const uint64_t a = dq + qi * (S::kTile >> 4), b = dk + q_st * (S::kKv >> 4);
           const uint32_t d = tmem + q_buf * kKeys;
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
+          for (int k = 0; k < D / 16; ++k)
             pt_mma_ss(lead, d, a + ((k / 4 * S::kHalf + k % 4 * 32) >> 4), b + ((k / 4 * S::kKvHalf + k % 4 * 32) >> 4), kIdS, k > 0);
-          }
           pt_commit(lead, at(s_full) + q_buf * 8);
+        };
+        const auto scores_issued = [&]() {
           q_buf = q_buf + 1 == S::kScores ? 0 : q_buf + 1;
           if (qi == 0 && qj < ends[1]) {
             qi = 1;
@@ -413,16 +413,19 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
             pt_commit(lead, at(k_empty) + q_st * 8);
             ++qj;
             qi = qj < ends[0] ? 0 : 1;
-            if (++q_st == kStages) q_st = 0, q_phase ^= 1;
+            if (++q_st == kKStages) q_st = 0, q_phase ^= 1;
           }
         };
 #pragma unroll 1
-        for (int n = 0; n < S::kScores && n < products; ++n) scores();
+        for (int n = 0; n < S::kScores && n < products; ++n) scores_inputs(), tc_fence_after(), scores(), scores_issued();
 #pragma unroll 1
         for (int n = 0; n < products; ++n) {
+          // what can be told afterwards is: the way from a block's weights to its
+          // tile's next scores is the longest there is
+          const bool more_scores = n + S::kScores < products;
           if (pi == 0 || pj >= ends[0]) {
             pt_wait(waits, at(v_full) + p_st * 8, v_phase);
-            if (pj >= edge) pt_wait(waits, at(clean) + p_st * 8, (pj - max(edge, w.first)) / kStages & 1);
+            if (pj >= edge) pt_wait(waits, at(clean) + p_st * 8, (pj - max(edge, w.first)) / kVStages & 1);
           }
           const uint64_t b = dv + p_st * (S::kKv >> 4);
           const uint32_t d = tmem + S::kSumCol + pi * D, a = tmem + p_buf * kKeys;
@@ -435,17 +438,19 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
             for (int k = 4 * h; k < 4 * h + 4; ++k) pt_mma_ts(lead, d, a + k * 8, b + ((k * 2048) >> 4), kIdO, k > 0 ? 1u : more);
           }
           pt_commit(lead, at(o_done) + pi * 8);
+          const bool block_done = pi == 1 || pj >= ends[1];
+          if (block_done) pt_commit(lead, at(v_empty) + p_st * 8);
+          // P's columns are read before the scores that are issued behind are written over them
+          if (more_scores) scores_inputs(), scores();
           if (++p_buf == S::kScores) p_buf = 0, p_phase ^= 1;
-          if (pi == 0 && pj < ends[1]) {
+          if (!block_done) {
             pi = 1;
-          } else {  // the block's last
-            pt_commit(lead, at(v_empty) + p_st * 8);
+          } else {
             ++pj;
             pi = pj < ends[0] ? 0 : 1;
-            if (++p_st == kStages) p_st = 0, v_phase ^= 1;
+            if (++p_st == kVStages) p_st = 0, v_phase ^= 1;
           }
-          // P's columns are read before the scores that are issued behind are written over them
-          if (n + S::kScores < products) scores();
+          if (more_scores) scores_issued();
         }
         pt_commit(lead, at(done));
         mbar_drain(done, 0);
@@ -455,9 +460,9 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
       // end, and where they are not finite, which a weight of 0 would not hide;
       // the rows that see those take them from `mark`.
       for (int j = max(edge, w.first); j < end; ++j) {
-        const int n = j - w.first, st = n % kStages;
-        if (!__all_sync(0xffffffffu, mbar_wait(&look[st], (j - max(edge, w.first)) / kStages & 1, p.err, kSpinLimitCycles) &&
-                                         mbar_wait(&v_full[st], (n / kStages) & 1, p.err, kSpinLimitCycles)))
+        const int n = j - w.first, st = n % kVStages;
+        if (!__all_sync(0xffffffffu, mbar_wait(&look[st], (j - max(edge, w.first)) / kVStages & 1, p.err, kSpinLimitCycles) &&
+                                         mbar_wait(&v_full[st], (n / kVStages) & 1, p.err, kSpinLimitCycles)))
           break;
         const int held = w.keys - j * kKeys;
         for (int c = threadIdx.x - kPtScrub * 32; c < S::kKv / 16; c += 64) {
@@ -540,11 +545,13 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
         for (int e = 6; e < 30; e += 4) m0 = max3(m0, s[q][e], s[q][e + 1]), m1 = max3(m1, s[q][e + 2], s[q][e + 3]);
         return max3(fmaxf(m0, m1), s[q][30], s[q][31]);
       };
-      // Brings the reference up to the block's maximum, and the sums with it.
-      const auto raise = [&]() {
+      // Brings the reference up to the block's maximum, and the sums with it, where
+      // `mine`: a row's bits do not turn on what the others of its warp hold.
+      const auto raise = [&](bool mine) {
         float next = max3(largest(0), largest(1), ref);
         if constexpr (kParts == 2) next = max3(largest(2), largest(3), next);
-        const float keep = ref == -INFINITY ? 0.f : ex2((ref - next) * c);
+        if (!mine) next = ref;
+        const float keep = !mine ? 1.f : ref == -INFINITY ? 0.f : ex2((ref - next) * c);
         ref = next;
         base = ref == -INFINITY ? 0.f : PtType<T>::kBias - ref * c;
         unset = __any_sync(0xffffffffu, ref == -INFINITY);
@@ -593,6 +600,12 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
         }
       };
       const auto nothing = [](int) {};
+      const auto hand_over = [&](int part) {
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(&p_full[kParts * buf + part]);
+      };
 #pragma unroll
       for (int q = 0; q < 2 * kParts; ++q) load(q);
       tmem_ld_wait();
@@ -600,7 +613,7 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
       // A row's reference is the maximum of its first block, and then stands
       // while the weights stay below 2^16, which the first part's sum and the
       // second part's maximum tell before any of them is handed over.
-      if (unset) raise();
+      if (unset) raise(ref == -INFINITY);
       weights(0, nothing);
       {
         const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
@@ -610,7 +623,7 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
           load(0), load(1);
           tmem_ld_wait();
           loaded(0, 2);
-          raise();
+          raise(above);
           weights(0, nothing);
         }
       }
@@ -619,15 +632,11 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
       if constexpr (kParts == 2) {
         weights(1, [&](int g) {
           if (g != 2) return;  // the stores have had time; the product of the first part may begin
-          tmem_st_wait();
-          tc_fence_before();
-          mbar_arrive_cta(&p_full[2 * buf]);
+          hand_over(0);
         });
         tmem_st(ts + 32, packed);
       }
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive_cta(&p_full[kParts * buf + kParts - 1]);
+      hand_over(kParts - 1);
       const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
       l += sum.x + sum.y;
       // the next block's number is two on while both tiles have one, else the next
