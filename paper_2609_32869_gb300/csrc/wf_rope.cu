@@ -50,73 +50,102 @@ __device__ __forceinline__ float2 rope_angle(int pos, uint64_t turns, float gain
   return make_float2(quarter == 1 || quarter == 2 ? -cs : cs, quarter >= 2 ? -sn : sn);
 }
 
-// A unit is VEC pairs of a head, two vectors: the same dims of both halves, or
-// 2 VEC dims in a row where pairs are neighbours; or two vectors of dims that
-// do not turn.  A thread keeps its row's cos and sin of one unit in registers and
-// takes that unit of several heads, the next one's loads in flight; a CTA works
-// out each (row, pair)'s angle once.
+// A unit is VEC pairs of a head, two vectors: the same dims of both halves, or,
+// where pairs are neighbours, vectors `turned` apart, so that a warp's accesses
+// are without gaps; or two vectors of dims that do not turn.  A thread keeps its
+// row's cos and sin of one unit in registers and takes that unit of several
+// heads, the next one's loads in flight; a CTA works out each (row, pair)'s angle once.
+//   16384 rows of 40 heads x 128, bf16, neighbours: 64 us, 5.2 TB/s; at three CTAs
+//     an SM (76 registers instead of 64) 68, with two units ahead 71 to 83
+//   6001 rows of 40 heads x 64, fp32, 32 dims turn: 21 us, 5.9 TB/s; with one unit ahead 22.7
+//   80 rows of 40 heads x 64, bf16: 5.5 us, the call and two dependent reads
 template <typename T, int VEC, bool kHalf>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_constant__ RopeParams p) {
   using V = RopeVec<T, VEC>;
+  constexpr int kAhead = VEC == 8 ? 1 : 2;  // units on their way
   __shared__ float2 turn[kRopePairs];
   pdl_wait();
   pdl_launch_dependents();
   const int pairs = p.table.rot_dim / 2, dim = p.table.head_dim, rot = p.table.rot_dim;
   const long long row0 = static_cast<long long>(blockIdx.x) * p.rows;
   const int rows = static_cast<int>(min(static_cast<long long>(p.rows), p.n - row0));
+  const int columns = blockDim.x / (p.rows * p.slots);
+  const int col = threadIdx.x % columns, slot = threadIdx.x / columns % p.slots, r = threadIdx.x / (columns * p.slots);
+  const bool live = r < rows;
+  const long long row = row0 + (live ? r : 0);
+  const T *q = static_cast<const T *>(p.q) + row * p.q_stride, *k = static_cast<const T *>(p.k) + row * p.k_stride;
+  T *q_out = static_cast<T *>(p.q_out) + row * p.q_out_stride, *k_out = static_cast<T *>(p.k_out) + row * p.k_out_stride;
+  const int first = blockIdx.y * p.per_y + slot, last = min(p.heads, (static_cast<int>(blockIdx.y) + 1) * p.per_y);
+  V x[kAhead] = {}, y[kAhead] = {};
+  int a = 0, b = 0;
+  bool two = false;
+  const auto unit = [&](int u) {
+    const bool turns = u < p.turned;
+    const int i = turns ? u : u - p.turned, apart = turns ? p.turned : p.units - p.turned, from = turns ? 0 : rot;
+    a = from + i * VEC;
+    b = turns && kHalf ? a + pairs : from + (i + apart) * VEC;
+    if (VEC == 1 && !kHalf && turns) a = 2 * i, b = 2 * i + 1;
+    two = b + VEC <= dim;  // (dims that do not turn may be an odd number of vectors)
+  };
+  const auto load = [&](int h, int s) {
+    const T *src = h < p.hq ? q + static_cast<long long>(h) * dim : k + static_cast<long long>(h - p.hq) * dim;
+    x[s] = *reinterpret_cast<const V *>(src + a);
+    if (two) y[s] = *reinterpret_cast<const V *>(src + b);
+  };
+  const auto start = [&]() {
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s)
+      if (first + s * p.slots < last) load(first + s * p.slots, s);
+  };
+  unit(col);
+  if (live) start();  // on their way while the angles are worked out
   for (int i = threadIdx.x; i < rows * pairs; i += blockDim.x) {
-    const int r = i / pairs;
-    float2 t = rope_angle(p.pos[row0 + r], p.table.turns[i - r * pairs], p.table.gain);
+    const int ri = i / pairs;
+    float2 t = rope_angle(p.pos[row0 + ri], p.table.turns[i - ri * pairs], p.table.gain);
     if (p.adjoint) t.y = -t.y;
     turn[i] = t;
   }
   __syncthreads();
-  const int columns = blockDim.x / (p.rows * p.slots);
-  const int col = threadIdx.x % columns, slot = threadIdx.x / columns % p.slots, r = threadIdx.x / (columns * p.slots);
-  if (r >= rows) return;
-  const long long row = row0 + r;
-  const T *q = static_cast<const T *>(p.q) + row * p.q_stride, *k = static_cast<const T *>(p.k) + row * p.k_stride;
-  T *q_out = static_cast<T *>(p.q_out) + row * p.q_out_stride, *k_out = static_cast<T *>(p.k_out) + row * p.k_out_stride;
-  const int first = blockIdx.y * p.per_y + slot, last = min(p.heads, (static_cast<int>(blockIdx.y) + 1) * p.per_y);
+  if (!live) return;
   for (int u = col; u < p.units; u += columns) {
     const bool turns = u < p.turned;
-    const int a = turns ? (kHalf ? u * VEC : 2 * u * VEC) : rot + (u - p.turned) * 2 * VEC;
-    const int b = turns && kHalf ? a + pairs : a + VEC;
-    const bool two = b + VEC <= dim;  // (dims that do not turn may be an odd number of vectors)
     float2 cs[VEC];
     if (turns) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) cs[e] = turn[r * pairs + u * VEC + e];
+      for (int e = 0; e < VEC; ++e)
+        cs[e] = turn[r * pairs + (kHalf || VEC == 1 ? u * VEC + e : (2 * e < VEC ? u : u + p.turned) * (VEC / 2) + e % ((VEC + 1) / 2))];
     }
-    V x = {}, y = {};
-    const auto load = [&](int h) {
-      const T *src = h < p.hq ? q + static_cast<long long>(h) * dim : k + static_cast<long long>(h - p.hq) * dim;
-      x = *reinterpret_cast<const V *>(src + a);
-      if (two) y = *reinterpret_cast<const V *>(src + b);
-    };
-    if (first < last) load(first);
-    for (int h = first; h < last; h += p.slots) {
-      const V cx = x, cy = y;
-      if (h + p.slots < last) load(h + p.slots);
-      T *dst = h < p.hq ? q_out + static_cast<long long>(h) * dim : k_out + static_cast<long long>(h - p.hq) * dim;
-      V ox = cx, oy = cy;
-      if (turns) {
+    if (u != col) {
+      unit(u);
+      start();
+    }
+    for (int h0 = first; h0 < last; h0 += kAhead * p.slots) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          // elements e of both vectors, or 2e and 2e + 1 of the two in a row
-          const T &i0 = kHalf || VEC == 1 ? cx.v[e] : (2 * e < VEC ? cx.v[2 * e % VEC] : cy.v[2 * e % VEC]);
-          const T &i1 = kHalf || VEC == 1 ? cy.v[e] : (2 * e < VEC ? cx.v[(2 * e + 1) % VEC] : cy.v[(2 * e + 1) % VEC]);
-          T &o0 = kHalf || VEC == 1 ? ox.v[e] : (2 * e < VEC ? ox.v[2 * e % VEC] : oy.v[2 * e % VEC]);
-          T &o1 = kHalf || VEC == 1 ? oy.v[e] : (2 * e < VEC ? ox.v[(2 * e + 1) % VEC] : oy.v[(2 * e + 1) % VEC]);
-          const float f0 = rope_up(i0), f1 = rope_up(i1);
-          rope_down(fmaf(f0, cs[e].x, -f1 * cs[e].y), o0);
-          rope_down(fmaf(f0, cs[e].y, f1 * cs[e].x), o1);
+      for (int s = 0; s < kAhead; ++s) {
+        const int h = h0 + s * p.slots;
+        if (h >= last) break;
+        const V cx = x[s], cy = y[s];
+        if (h + kAhead * p.slots < last) load(h + kAhead * p.slots, s);
+        T *dst = h < p.hq ? q_out + static_cast<long long>(h) * dim : k_out + static_cast<long long>(h - p.hq) * dim;
+        V ox = cx, oy = cy;
+        if (turns) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            // elements e of both vectors, or 2e and 2e + 1 of the two in a row
+            const T &i0 = kHalf || VEC == 1 ? cx.v[e] : (2 * e < VEC ? cx.v[2 * e % VEC] : cy.v[2 * e % VEC]);
+            const T &i1 = kHalf || VEC == 1 ? cy.v[e] : (2 * e < VEC ? cx.v[(2 * e + 1) % VEC] : cy.v[(2 * e + 1) % VEC]);
+            T &o0 = kHalf || VEC == 1 ? ox.v[e] : (2 * e < VEC ? ox.v[2 * e % VEC] : oy.v[2 * e % VEC]);
+            T &o1 = kHalf || VEC == 1 ? oy.v[e] : (2 * e < VEC ? ox.v[(2 * e + 1) % VEC] : oy.v[(2 * e + 1) % VEC]);
+            const float f0 = rope_up(i0), f1 = rope_up(i1);
+            rope_down(fmaf(f0, cs[e].x, -f1 * cs[e].y), o0);
+            rope_down(fmaf(f0, cs[e].y, f1 * cs[e].x), o1);
+          }
+        } else if (!(h < p.hq ? p.q_copy : p.k_copy)) {
+          continue;
         }
-      } else if (!(h < p.hq ? p.q_copy : p.k_copy)) {
-        continue;
+        *reinterpret_cast<V *>(dst + a) = ox;
+        if (two) *reinterpret_cast<V *>(dst + b) = oy;
       }
-      *reinterpret_cast<V *>(dst + a) = ox;
-      if (two) *reinterpret_cast<V *>(dst + b) = oy;
     }
   }
 }
