@@ -23,47 +23,58 @@ struct Kv8RowParams {
   uint32_t *err;
 };
 
-// The positions of a run of rows of one record: of lane l < 16 the row of
-// position l (-1: none).
+// The slots of a CTA's first 32 rows, a lane each (-1 past the last), and as bits
+// those of its own rows that open a run.  Rows of a record that follow one
+// another are one run; `ascending`: as far as their positions ascend.
+struct Kv8Rows {
+  int slot;
+  uint32_t openers;
+};
+__device__ __forceinline__ Kv8Rows kv8_rows(const Kv8RowParams &p, int row0, int lane, bool ascending) {
+  Kv8Rows r;
+  r.slot = row0 + lane < p.n ? p.slots[row0 + lane] : -1;
+  const int first = row0 > 0 ? p.slots[row0 - 1] : -1, up = __shfl_up_sync(0xffffffffu, r.slot, 1), before = lane == 0 ? first : up;
+  const bool mine = lane < p.rows && row0 + lane < p.n;
+  const bool opens = r.slot < 0 ? ascending : before < 0 || before >> 4 != r.slot >> 4 || (ascending && before >= r.slot);
+  r.openers = __ballot_sync(0xffffffffu, mine && opens);
+  return r;
+}
+// Bit n (from 0) of those that are set.
+__device__ __forceinline__ int nth_bit(uint32_t bits, int n) {
+  for (; n > 0; --n) bits &= bits - 1;
+  return __ffs(bits) - 1;
+}
+
+// The positions of the run of rows that row `first` of the CTA opens: of lane
+// l < 16 the row of position l (-1: none).
 struct Kv8Run {
   int slot;      // the first row's
   int row;
   uint32_t has;  // positions with a row
 };
-
-// Of the rows of this CTA those that open a run, as bits.  Rows of a record
-// that follow one another are one run; `ascending`: as far as their positions ascend.
-__device__ __forceinline__ uint32_t kv8_openers(const Kv8RowParams &p, int row0, int lane, bool ascending) {
-  const int row = row0 + lane;
-  bool opens = false;
-  if (lane < p.rows && row < p.n) {
-    const int slot = p.slots[row], before = row > 0 ? p.slots[row - 1] : -1;
-    opens = slot < 0 ? ascending : before < 0 || before >> 4 != slot >> 4 || (ascending && before >= slot);
-  }
-  return __ballot_sync(0xffffffffu, opens);
-}
-
-__device__ __forceinline__ Kv8Run kv8_run(const Kv8RowParams &p, int first, int lane, bool ascending) {
+__device__ __forceinline__ Kv8Run kv8_run(const Kv8RowParams &p, const Kv8Rows &rows, int row0, int first, int lane, bool ascending) {
   Kv8Run r;
-  r.slot = p.slots[first];
+  r.slot = __shfl_sync(0xffffffffu, rows.slot, first);
   r.row = -1;
-  for (int at = first;; at += 32) {
-    const int slot = at + lane < p.n ? p.slots[at + lane] : -1;
-    bool in = slot >= 0 && slot >> 4 == r.slot >> 4;
+  int at = row0 + first, slot = __shfl_sync(0xffffffffu, rows.slot, (lane + first) & 31), most = 32 - first;
+  for (;;) {  // (again only for more rows than a record has positions)
+    bool in = lane < most && slot >= 0 && slot >> 4 == r.slot >> 4;
     if (ascending) {
       const int before = __shfl_up_sync(0xffffffffu, slot, 1);
       in = in && (lane == 0 || before < slot);
     }
     const uint32_t out = ~__ballot_sync(0xffffffffu, in);
     const int count = out ? __ffs(out) - 1 : 32;
-    const int start = r.slot & 15, straight = __all_sync(0xffffffffu, lane >= count || slot == r.slot + lane);
-    if (at == first && straight) {
-      if (lane >= start && lane - start < count) r.row = first + lane - start;
+    const int start = r.slot & 15;
+    if (at == row0 + first && __all_sync(0xffffffffu, lane >= count || slot == r.slot + lane)) {
+      if (lane >= start && lane - start < count) r.row = at + lane - start;
     } else {
       for (int c = 0; c < count; ++c)
         if ((__shfl_sync(0xffffffffu, slot, c) & 15) == lane) r.row = at + c;
     }
-    if (count < 32 || ascending) break;
+    if (count < most || ascending) break;
+    at += most, most = 32;
+    slot = at + lane < p.n ? p.slots[at + lane] : -1;
   }
   r.has = __ballot_sync(0xffffffffu, lane < 16 && r.row >= 0);
   return r;
@@ -90,21 +101,54 @@ __device__ __forceinline__ int kv8_exponent(float most) {
   return most == 0.f ? kKv8Low : min(max(e, kKv8Low), kKv8High);
 }
 
+// The power of two of a record's values, from the rows that a warp's lanes hold; what
+// is not finite becomes NaN and does not count.
+template <typename T, int G>
+__device__ __forceinline__ int kv8_most(uint4 (&w)[G][4]) {
+  uint32_t most2 = 0;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t m = 0x7fff7fffu;
+      most2 = max_u16x2(max_u16x2(max_u16x2(w[g][i].x & m, w[g][i].y & m), max_u16x2(w[g][i].z & m, w[g][i].w & m)), most2);
+    }
+  uint32_t most = __reduce_max_sync(0xffffffffu, max(most2 & 0xffff, most2 >> 16));
+  if (most >= Kv8Limits<T>::kInf) {
+    most = 0;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t *u = reinterpret_cast<uint32_t *>(&w[g][i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t lo = u[j] & 0x7fff, hi = u[j] >> 16 & 0x7fff;
+          if (lo < Kv8Limits<T>::kInf) most = max(most, lo); else u[j] |= 0x7fff;
+          if (hi < Kv8Limits<T>::kInf) most = max(most, hi); else u[j] |= 0x7fff0000u;
+        }
+      }
+    most = __reduce_max_sync(0xffffffffu, most);
+  }
+  return kv8_exponent(Type16<T>::lo(most));
+}
+
 // One warp per record and head.  Lane 4 r + t holds the dims 8r .. 8r + 7 of
 // every group for the positions 2t, 2t + 1, 2t + 8, 2t + 9: its 32 bytes of value
-// codes, and pieces of 8 bytes of the key codes.
+// codes, and pieces of 8 bytes of the key codes.  Every load, of rows and of
+// what a record keeps, is on its way before the first is used.
 template <typename T, int G>
-__global__ void __launch_bounds__(kK8Warps * 32, G == 1 ? 6 : 4) kv8_store_kernel(const Kv8RowParams p) {
+__global__ void __launch_bounds__(kK8Warps * 32, G == 1 ? 6 : 3) kv8_store_kernel(const Kv8RowParams p) {
   using X = Type16<T>;
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
   const int row0 = blockIdx.x * p.rows, head0 = blockIdx.y * p.heads, heads = min(p.heads, p.pool.heads - head0);
-  const uint32_t openers = kv8_openers(p, row0, lane, false);
-  const int units = __popc(openers) * heads;
+  const Kv8Rows rows = kv8_rows(p, row0, lane, false);
+  const int units = __popc(rows.openers) * heads;
   for (int unit = warp; unit < units; unit += kK8Warps) {
     const int head = head0 + unit % heads;
-    const Kv8Run run = kv8_run(p, row0 + static_cast<int>(__fns(openers, 0, unit / heads + 1)), lane, false);
+    const Kv8Run run = kv8_run(p, rows, row0, nth_bit(rows.openers, unit / heads), lane, false);
     const int block = run.slot >> p.pool.bs_shift;
     if (block >= p.pool.n_blocks) {
       if (lane == 0) set_error(p.err, WF_DEV_ERR_PAGE);
@@ -112,85 +156,68 @@ __global__ void __launch_bounds__(kK8Warps * 32, G == 1 ? 6 : 4) kv8_store_kerne
     }
     unsigned char *rec = kv8_record(p.pool, block, head, (run.slot & (p.pool.bs - 1)) >> 4);
     const uint32_t kept = (1u << (__ffs(run.has) - 1)) - 1;
-    int row[4];
+    uint4 w[2][G][4], had_v[G][2];
+    uint2 had_k[G][4];
+    uint2 held = make_uint2(0, 0);
+    bool keeps[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) row[i] = __shfl_sync(0xffffffffu, run.row, 2 * t + i % 2 + i / 2 * 8);
-    float4 scales;
+    for (int i = 0; i < 4; ++i) {
+      const int pos = 2 * t + i % 2 + i / 2 * 8;
+      const long long row = __shfl_sync(0xffffffffu, run.row, pos);
+      keeps[i] = kept >> pos & 1;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        w[0][g][i] = w[1][g][i] = make_uint4(0, 0, 0, 0);
+        if (row >= 0) {
+          w[0][g][i] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.k) + row * p.k_stride + head * (G * 64) + g * 64 + r * 8);
+          w[1][g][i] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.v) + row * p.v_stride + head * (G * 64) + g * 64 + r * 8);
+        }
+        if (keeps[i]) had_k[g][i] = *reinterpret_cast<const uint2 *>(rec + g * kKv8Group + pos * 64 + r * 8);
+      }
+    }
+    if (kept) {
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) had_v[g][h] = *reinterpret_cast<const uint4 *>(rec + g * kKv8Group + 1024 + h * 512 + lane * 16);
+      held = *reinterpret_cast<const uint2 *>(rec + G * kKv8Group);
+    }
+    float scales[2];
     // keys, then values
 #pragma unroll
     for (int is_v = 0; is_v < 2; ++is_v) {
-      const T *src = static_cast<const T *>(is_v ? p.v : p.k) + head * (G * 64) + r * 8;
-      const long long stride = is_v ? p.v_stride : p.k_stride;
-      uint4 w[G][4];
-#pragma unroll
-      for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          w[g][i] = row[i] >= 0 ? *reinterpret_cast<const uint4 *>(src + row[i] * stride + g * 64) : make_uint4(0, 0, 0, 0);
-      uint32_t most2 = 0;
-#pragma unroll
-      for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t m = 0x7fff7fffu;
-          most2 = max_u16x2(max_u16x2(max_u16x2(w[g][i].x & m, w[g][i].y & m), max_u16x2(w[g][i].z & m, w[g][i].w & m)), most2);
-        }
-      uint32_t most = __reduce_max_sync(0xffffffffu, max(most2 & 0xffff, most2 >> 16));
-      if (most >= Kv8Limits<T>::kInf) {  // values that are not finite: NaN, and not counted
-        most = 0;
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t *u = reinterpret_cast<uint32_t *>(&w[g][i]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t lo = u[j] & 0x7fff, hi = u[j] >> 16 & 0x7fff;
-              if (lo < Kv8Limits<T>::kInf) most = max(most, lo); else u[j] |= 0x7fff;
-              if (hi < Kv8Limits<T>::kInf) most = max(most, hi); else u[j] |= 0x7fff0000u;
-            }
-          }
-        most = __reduce_max_sync(0xffffffffu, most);
-      }
-      int e = kv8_exponent(X::lo(most));
+      int e = kv8_most<T, G>(w[is_v]);
       float back = 1.f;
       if (kept) {
-        const uint32_t held = *reinterpret_cast<const uint32_t *>(rec + G * kKv8Group + is_v * 4);
-        const int old = min(max(static_cast<int>(held >> 23 & 255) - 127, kKv8Low), kKv8High);
+        const int old = min(max(static_cast<int>((is_v ? held.y : held.x) >> 23 & 255) - 127, kKv8Low), kKv8High);
         e = max(e, old);
         back = two_to(old - e);
       }
       const float scale = two_to(-e);
-      if (is_v) scales.y = two_to(e); else scales.x = two_to(e);
+      scales[is_v] = two_to(e);
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         float x[4][8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t *u = reinterpret_cast<const uint32_t *>(&w[g][i]);
+          const uint32_t *u = reinterpret_cast<const uint32_t *>(&w[is_v][g][i]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[i][2 * j] = X::lo(u[j]) * scale, x[i][2 * j + 1] = X::hi(u[j]) * scale;
         }
         if (!is_v) {
-          unsigned char *at = rec + g * kKv8Group + r * 8;
-          if (kept) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int pos = 2 * t + i % 2 + i / 2 * 8;
-              if (!(kept >> pos & 1)) continue;
-              const uint2 c = *reinterpret_cast<const uint2 *>(at + pos * 64);
+          for (int i = 0; i < 4; ++i) {
+            if (keeps[i]) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                const float2 f = codes_to_f32((j < 2 ? c.x : c.y) >> (j % 2 * 16));
+                const float2 f = codes_to_f32((j < 2 ? had_k[g][i].x : had_k[g][i].y) >> (j % 2 * 16));
                 x[i][2 * j] = f.x * back, x[i][2 * j + 1] = f.y * back;
               }
             }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
             const int pos = 2 * t + i % 2 + i / 2 * 8;
-            *reinterpret_cast<uint2 *>(at + pos * 64) = make_uint2(f32_to_codes(x[i][0], x[i][1]) | f32_to_codes(x[i][2], x[i][3]) << 16,
-                                                                   f32_to_codes(x[i][4], x[i][5]) | f32_to_codes(x[i][6], x[i][7]) << 16);
+            *reinterpret_cast<uint2 *>(rec + g * kKv8Group + pos * 64 + r * 8) =
+                make_uint2(f32_to_codes(x[i][0], x[i][1]) | f32_to_codes(x[i][2], x[i][3]) << 16,
+                           f32_to_codes(x[i][4], x[i][5]) | f32_to_codes(x[i][6], x[i][7]) << 16);
           }
         } else {
           uint4 *at = reinterpret_cast<uint4 *>(rec + g * kKv8Group + 1024 + lane * 16);
@@ -198,14 +225,13 @@ __global__ void __launch_bounds__(kK8Warps * 32, G == 1 ? 6 : 4) kv8_store_kerne
           for (int h = 0; h < 2; ++h) {
             uint32_t c[4];
             if (kept) {
-              const uint4 had = at[h * 32];
-              c[0] = had.x, c[1] = had.y, c[2] = had.z, c[3] = had.w;
+              c[0] = had_v[g][h].x, c[1] = had_v[g][h].y, c[2] = had_v[g][h].z, c[3] = had_v[g][h].w;
 #pragma unroll
               for (int j = 0; j < 8; ++j) {  // 16 bits: [odd dim][a]
                 const int dim = j % 2 * 4 + 2 * h + j / 4, i = j / 2 % 2 * 2;
                 const float2 f = codes_to_f32(c[j / 2] >> (j % 2 * 16));
-                if (kept >> (2 * t + i * 4) & 1) x[i][dim] = f.x * back;
-                if (kept >> (2 * t + 1 + i * 4) & 1) x[i + 1][dim] = f.y * back;
+                if (keeps[i]) x[i][dim] = f.x * back;
+                if (keeps[i + 1]) x[i + 1][dim] = f.y * back;
               }
             }
 #pragma unroll
@@ -219,8 +245,7 @@ __global__ void __launch_bounds__(kK8Warps * 32, G == 1 ? 6 : 4) kv8_store_kerne
       }
     }
     __syncwarp();  // every lane has read the old scales
-    if (lane == 0) *reinterpret_cast<float4 *>(rec + G * kKv8Group) = make_float4(scales.x, scales.y, 0.f, 0.f);
-    __syncwarp();
+    if (lane == 0) *reinterpret_cast<float4 *>(rec + G * kKv8Group) = make_float4(scales[0], scales[1], 0.f, 0.f);
   }
 }
 
@@ -231,12 +256,13 @@ __global__ void __launch_bounds__(kK8Warps * 32) kv8_load_kernel(const Kv8RowPar
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
   const int row0 = blockIdx.x * p.rows, head0 = blockIdx.y * p.heads, heads = min(p.heads, p.pool.heads - head0);
-  const uint32_t openers = kv8_openers(p, row0, lane, true);
-  const int units = __popc(openers) * heads;
+  const Kv8Rows rows = kv8_rows(p, row0, lane, true);
+  const int units = __popc(rows.openers) * heads;
   for (int unit = warp; unit < units; unit += kK8Warps) {
-    const int head = head0 + unit % heads, first = row0 + static_cast<int>(__fns(openers, 0, unit / heads + 1));
+    const int head = head0 + unit % heads, nth = nth_bit(rows.openers, unit / heads);
+    const long long first = row0 + nth;
     T *k = static_cast<T *>(p.k_out) + head * (G * 64) + r * 8, *v = static_cast<T *>(p.v_out) + head * (G * 64) + r * 8;
-    const int slot = p.slots[first], block = slot >> p.pool.bs_shift;
+    const int slot = __shfl_sync(0xffffffffu, rows.slot, nth), block = slot >> p.pool.bs_shift;
     const bool none = slot < 0, out = !none && block >= p.pool.n_blocks;
     if (out && lane == 0) set_error(p.err, WF_DEV_ERR_PAGE);
     if (none) {  // a row of its own
@@ -245,7 +271,7 @@ __global__ void __launch_bounds__(kK8Warps * 32) kv8_load_kernel(const Kv8RowPar
         if (t < 2) *reinterpret_cast<uint4 *>((t ? v : k) + first * (t ? p.v_stride : p.k_stride) + g * 64) = make_uint4(0, 0, 0, 0);
       continue;
     }
-    const Kv8Run run = kv8_run(p, first, lane, true);
+    const Kv8Run run = kv8_run(p, rows, row0, nth, lane, true);
     const unsigned char *rec = kv8_record(p.pool, out ? 0 : block, head, (slot & (p.pool.bs - 1)) >> 4);
     const float2 scale = *reinterpret_cast<const float2 *>(rec + G * kKv8Group);
 #pragma unroll
@@ -255,7 +281,8 @@ __global__ void __launch_bounds__(kK8Warps * 32) kv8_load_kernel(const Kv8RowPar
       const uint32_t c[2][4] = {{va.x, va.y, va.z, va.w}, {vb.x, vb.y, vb.z, vb.w}};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int pos = 2 * t + i % 2 + i / 2 * 8, row = __shfl_sync(0xffffffffu, run.row, pos);
+        const int pos = 2 * t + i % 2 + i / 2 * 8;
+        const long long row = __shfl_sync(0xffffffffu, run.row, pos);
         if (row < 0) continue;
         const uint2 kc = *reinterpret_cast<const uint2 *>(rec + g * kKv8Group + pos * 64 + r * 8);
         uint32_t ko[4], vo[4];
@@ -295,11 +322,13 @@ static wf_status kv8_rows(const wf_kv8_pool *pool, int32_t layer, const void *k,
 
 static wf_status kv8_rows_launch(const void *fn, Kv8RowParams *p, void *stream) {
   if (p->n == 0) return WF_OK;
-  // Few rows and heads: about one record and head a warp, if each row is a
-  // record's only one.  Many: 16 rows a CTA, which are a record or two of a
-  // prompt, and eight heads, two a warp.
-  const bool few = static_cast<int64_t>(p->n) * p->pool.heads <= kSms * 64;
-  p->rows = few ? 4 : 16, p->heads = few ? 1 : std::min(p->pool.heads, 8);
+  // A warp takes about one record and head while there are SMs for it: of rows
+  // that are each a record's only one (few of them, a decode step) four a CTA
+  // and head, of a prompt's 16, a record or two; then up to eight heads a CTA.
+  // 80 rows with 680 read back, 20 heads: 8.2 us; with eight heads from the start 14.
+  const int64_t tiles = (static_cast<int64_t>(p->n) + 15) / 16;
+  p->rows = static_cast<int64_t>(p->n) * p->pool.heads <= kSms * 64 ? 4 : 16;
+  p->heads = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({tiles * p->pool.heads / (kSms * 16), 8, p->pool.heads})));
   const dim3 grid((p->n + p->rows - 1) / p->rows, (p->pool.heads + p->heads - 1) / p->heads);
   void *args[] = {p};
   return launch_pdl(fn, grid, kK8Warps * 32, 0, args, static_cast<cudaStream_t>(stream)) == cudaSuccess ? WF_OK : WF_ERR_CUDA;
