@@ -213,10 +213,11 @@ __device__ __forceinline__ bool pt_find(const PromptParams &p, int item, int lan
   int before = 0;
   for (int base = 0; base < p.n_seq; base += 32) {
     const int i = base + lane;
-    int a = 0, b = 0;
+    int a = 0, b = 0, rk0 = 0, rk1 = 0;
     bool bad = false;
     if (i < p.n_seq) {
       const int ra = p.q_start[i], rb = p.q_start[i + 1];
+      rk0 = p.k_start[i], rk1 = p.k_start[i + 1];
       a = min(max(ra, 0), p.n_q), b = min(max(rb, a), p.n_q);
       bad = a != ra || b != rb;
     }
@@ -236,7 +237,7 @@ __device__ __forceinline__ bool pt_find(const PromptParams &p, int item, int lan
       w.rows = __shfl_sync(0xffffffffu, b, src) - w.q0;
       const int end = __shfl_sync(0xffffffffu, before + sum, src);
       w.token = (end - 1 - item) * per;
-      const int rk0 = p.k_start[w.seq], rk1 = p.k_start[w.seq + 1];
+      rk0 = __shfl_sync(0xffffffffu, rk0, src), rk1 = __shfl_sync(0xffffffffu, rk1, src);
       w.k0 = min(max(rk0, 0), p.n_k);
       const int k1 = min(max(rk1, w.k0), p.n_k);
       w.keys = min(k1 - w.k0, p.max_k);
@@ -613,19 +614,18 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
       // A row's reference is the maximum of its first block, and then stands
       // while the weights stay below 2^16, which the first part's sum and the
       // second part's maximum tell before any of them is handed over.
-      if (unset) raise(ref == -INFINITY);
-      weights(0, nothing);
-      {
+      bool low = unset && ref == -INFINITY;  // the row's reference has to be raised
+      if (unset) raise(low);
+      for (bool again = false;; again = true) {
+        weights(0, nothing);
         const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
-        bool above = sum.x + sum.y > 65000.f;
-        if constexpr (kParts == 2) above |= fmaf(fmaxf(largest(2), largest(3)), c, base) > 15.9f;
-        if (__any_sync(0xffffffffu, above)) {
-          load(0), load(1);
-          tmem_ld_wait();
-          loaded(0, 2);
-          raise(above);
-          weights(0, nothing);
-        }
+        low = sum.x + sum.y > 65000.f;
+        if constexpr (kParts == 2) low |= fmaf(fmaxf(largest(2), largest(3)), c, base) > 15.9f;
+        if (again || !__any_sync(0xffffffffu, low)) break;  // (infinite scores stay above)
+        load(0), load(1);
+        tmem_ld_wait();
+        loaded(0, 2);
+        raise(low);
       }
       if (j > w.first) added(j - 1);
       tmem_st(ts, packed);
