@@ -316,6 +316,7 @@ static wf_status kv8_rows(const wf_kv8_pool *pool, int32_t layer, const void *k,
   const int64_t d = static_cast<int64_t>(pool->n_kv_heads) * pool->head_dim;
   if (!k || !v || !d_slots || n < 0 || !aligned16(k) || !aligned16(v) || k_stride % 8 || v_stride % 8 || k_stride < d || v_stride < d)
     return WF_ERR_INVALID;
+  if (n > INT32_MAX - 64) return WF_ERR_UNSUPPORTED;
   p->k_stride = k_stride, p->v_stride = v_stride, p->slots = d_slots, p->n = n;
   return WF_OK;
 }

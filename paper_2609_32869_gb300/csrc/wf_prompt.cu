@@ -37,11 +37,14 @@ struct PromptParams {
   uint32_t *err;
 };
 
-// At 128 dims a CTA has the SM: blocks of 128 keys, all of TMEM.  At 64 dims
-// the exponentials are as much work as the products and eight warps do not
-// keep their unit busy, so two CTAs share the SM, with blocks of 64 keys:
-// 32 x 1500 frames, 20 heads took 442 us with one CTA, 128 keys and a third
-// buffer of scores.
+// At 128 dims a CTA has the SM: blocks of 128 keys, all of TMEM; the products
+// take as long as the tensor unit's way to shared memory, 128 bytes a clock.  At
+// 64 dims what a tile waits for is the way from a block's weights to its next
+// scores (without any exponentials the case below takes 360 us), so two CTAs
+// share the SM, with blocks of 64 keys, and four tiles' ways overlap.
+//   32 x 1500 frames, 20 heads: 380 us.  One CTA with 128 keys and a third buffer
+//   of scores 442; one with weights beside the scores, so that the next ones are
+//   there when a softmax ends: three tiles and 64 keys 414, two and 128 479.
 template <int D>
 struct PtShape {
   static constexpr int kKeys = D == 64 ? 64 : 128;  // of a block
@@ -54,7 +57,8 @@ struct PtShape {
   static constexpr int kScores = 2;                 // buffers of scores in TMEM, before the tiles' sums
   static constexpr int kSumCol = kScores * kKeys;
   static constexpr uint32_t kCols = D == 64 ? 256 : 512;
-  static constexpr int kRegsMore = D == 64 ? 96 : 208, kRegsLess = D == 64 ? 48 : 88;
+  static constexpr int kRegs = D == 64 ? 80 : 168, kRegsMore = D == 64 ? 96 : 208, kRegsLess = D == 64 ? 48 : 88;
+  static_assert(256 * kRegsMore + 128 * kRegsLess == kPtThreads * kRegs && kPerSm * kPtThreads * kRegs <= 65536, "");
   static constexpr int kMarkOff = 2 * kTile + (kKStages + kVStages) * kKv;  // [3][D] first position of a value that is not finite
   static constexpr int kBarOff = kMarkOff + 3 * D * 4;
   static constexpr int kBars = 2 + 2 * kKStages + 4 * kVStages + (1 + kParts) * kScores + 2 + 1;
@@ -237,6 +241,7 @@ __device__ __forceinline__ bool pt_find(const PromptParams &p, int item, int lan
       w.rows = __shfl_sync(0xffffffffu, b, src) - w.q0;
       const int end = __shfl_sync(0xffffffffu, before + sum, src);
       w.token = (end - 1 - item) * per;
+      if (w.token < 0 || w.token >= w.rows) return false;  // (starts that are none)
       rk0 = __shfl_sync(0xffffffffu, rk0, src), rk1 = __shfl_sync(0xffffffffu, rk1, src);
       w.k0 = min(max(rk0, 0), p.n_k);
       const int k1 = min(max(rk1, w.k0), p.n_k);
@@ -284,6 +289,7 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
   PtWork *shared_work = reinterpret_cast<PtWork *>(has_work + 2);
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  if (threadIdx.x == kPtLoad * 32) tma_prefetch_desc(&mq), tma_prefetch_desc(&mk), tma_prefetch_desc(&mv);
   pdl_wait();
   pdl_launch_dependents();
   const int head = blockIdx.x % p.heads;
@@ -341,14 +347,12 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
   const int both = min(ends[0], ends[1]);  // blocks before it are both tiles'
   const int products = ends[0] + ends[1] - 2 * w.first;
 
-  // The block's 384 threads were launched with 168 registers each, or 80 where
-  // there are two CTAs: 256 take 208 (96), 128 keep 88 (48).
-  static_assert(256 * S::kRegsMore + 128 * S::kRegsLess == kPtThreads * (S::kPerSm == 1 ? 168 : 80), "");
+  // The block's registers go to the softmax: kRegs a thread at launch, kRegsMore
+  // for its 256 threads and kRegsLess for the other 128, the same sum.
   if (warp >= kPtMma) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kRegsLess));
     if (warp == kPtLoad) {
       if (lane == 0 && w.first < end) {
-        tma_prefetch_desc(&mq), tma_prefetch_desc(&mk), tma_prefetch_desc(&mv);
         const uint32_t q_bytes = static_cast<uint32_t>(p.group * p.tokens) * D * 2;
         const auto load_q = [&](int i) {
           mbar_arrive_expect_tx(&q_full[i], q_bytes);
@@ -775,6 +779,10 @@ static cudaError_t pt_launch(const CUtensorMap &mq, const CUtensorMap &mk, const
   if (!ready.get(current_device(), [&]() -> int {
         e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, PtShape<D>::kSmem);
         if (e == cudaSuccess) e = prefer_max_shared(fn);
+        // a softmax warp waits for its registers, so the launch has to bring as many as the split counts on
+        cudaFuncAttributes attr;
+        if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, fn);
+        if (e == cudaSuccess && attr.numRegs != PtShape<D>::kRegs) e = cudaErrorInvalidKernelImage;
         return e == cudaSuccess;
       }))
     return e;
@@ -814,6 +822,7 @@ wf_status wf_prompt_attention(const void *d_q, int64_t q_stride, const void *d_k
       out_stride % 8 || q_stride < qd || k_stride < kd || v_stride < kd || out_stride < qd || (reinterpret_cast<uintptr_t>(d_lse) & 3))
     return WF_ERR_INVALID;
   if (n_q == 0) return WF_OK;
+  if (n_q > 1 << 30 || n_k > 1 << 30 || max_k > 1 << 30) return WF_ERR_UNSUPPORTED;
   const int group = n_heads / n_kv_heads;
   const PtPlan a = pt_plan(n_seq, n_q, max_k, n_kv_heads, group);
   if (a.items * n_kv_heads > INT32_MAX || static_cast<int64_t>(n_q) * n_heads > INT32_MAX * 4LL) return WF_ERR_UNSUPPORTED;
