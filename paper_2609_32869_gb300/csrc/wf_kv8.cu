@@ -137,6 +137,8 @@ __device__ __forceinline__ int kv8_most(uint4 (&w)[G][4]) {
 // every group for the positions 2t, 2t + 1, 2t + 8, 2t + 9: its 32 bytes of value
 // codes, and pieces of 8 bytes of the key codes.  Every load, of rows and of
 // what a record keeps, is on its way before the first is used.
+//   48000 rows of 20 heads x 64, bf16, records of their own: 63 us, 5.9 TB/s, by
+//     HBM (read back in as long); with a record's loads one after another 70
 template <typename T, int G>
 __global__ void __launch_bounds__(kK8Warps * 32, G == 1 ? 6 : 3) kv8_store_kernel(const Kv8RowParams p) {
   using X = Type16<T>;

@@ -50,6 +50,13 @@ __device__ __forceinline__ uint32_t flags_f16(uint32_t two) { return (two & 0x80
 // steps of 32 positions of a unit through a ring of its own in shared memory
 // (one bulk copy per record, an mbarrier per stage; no other warp is waited for)
 // and keeps a running reference, sum and weighted values.
+//   96 sequences x 9 rows x 20 heads, 1500 positions, bf16: 68 us, 5.5 TB/s, by HBM
+//     and 3.2 rounds of CTAs that take four (cut in two, the halves joined over a
+//     cluster, 92; at three CTAs an SM 74, at five, which spill, 110)
+//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 39 us,
+//     5.7 TB/s, by HBM; of that the join 2 us (with a third stage, two CTAs an SM, 47)
+//   5 rows of one sequence, 1500 positions, 20 heads, bf16: 5.9 us, by the launch
+//     and one chain of reads
 template <typename T, int G, int NT>
 __global__ void __launch_bounds__(kAtThreads, K8Shape<G, NT>::kBlocks) kv8_attention_kernel(const PagedAttnParams<Kv8Pool> p) {
   using X = Type16<T>;
