@@ -441,6 +441,8 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
             pt_wait(waits, at(v_full) + p_st * 8, v_phase);
             if (pj >= edge) pt_wait(waits, at(clean) + p_st * 8, (pj - max(edge, w.first)) / kVStages & 1);
           }
+          // with 64 dims the keys are there long before the weights are, and the look at their barrier costs less here
+          if (D == 64 && more_scores) scores_inputs();
           const uint64_t b = dv + p_st * (S::kKv >> 4);
           const uint32_t d = tmem + S::kSumCol + pi * D, a = tmem + p_buf * kKeys;
           const uint32_t more = pj > w.first;
@@ -455,7 +457,8 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
           const bool block_done = pi == 1 || pj >= ends[1];
           if (block_done) pt_commit(lead, at(v_empty) + p_st * 8);
           // P's columns are read before the scores that are issued behind are written over them
-          if (more_scores) scores_inputs(), scores();
+          if (D != 64 && more_scores) scores_inputs();
+          if (more_scores) scores();
           if (++p_buf == S::kScores) p_buf = 0, p_phase ^= 1;
           if (!block_done) {
             pi = 1;
@@ -479,25 +482,35 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
                                          mbar_wait(&v_full[st], (n / kVStages) & 1, p.err, kSpinLimitCycles)))
           break;
         const int held = w.keys - j * kKeys;
-        for (int c = threadIdx.x - kPtScrub * 32; c < S::kKv / 16; c += 64) {
-          uint4 *at = reinterpret_cast<uint4 *>(sv + st * S::kKv + c * 16);
-          const int row = c / 8 % kKeys;
-          if (row >= held) {
-            *at = make_uint4(0, 0, 0, 0);
-            continue;
+        // (some vectors at a time, all of them on their way before the first is looked at)
+        constexpr int kBatch = D / 16;
+        for (int c0 = threadIdx.x - kPtScrub * 32; c0 < S::kKv / 16; c0 += 64 * kBatch) {
+          uint4 v[kBatch];
+          uint4 *at = reinterpret_cast<uint4 *>(sv + st * S::kKv + c0 * 16);
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) v[b] = at[b * 64];
+          uint32_t odd = 0;
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            const uint32_t m = 0x7fff7fffu;
+            const uint32_t most = __vmaxu2(__vmaxu2(v[b].x & m, v[b].y & m), __vmaxu2(v[b].z & m, v[b].w & m));
+            if ((c0 + b * 64) / 8 % kKeys >= held) {
+              at[b * 64] = make_uint4(0, 0, 0, 0);
+            } else if (max(most & 0xffff, most >> 16) >= PtType<T>::kInf) {
+              odd |= 1u << b;
+            }
           }
-          const uint4 v = *at;
-          const uint32_t m = 0x7fff7fffu;
-          const uint32_t most = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
-          if (max(most & 0xffff, most >> 16) < PtType<T>::kInf) continue;
-          uint16_t *e = reinterpret_cast<uint16_t *>(at);
-          const int dim = c / (8 * kKeys) * 64 + ((c & 7) ^ (row & 7)) * 8;
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t u = e[i] & 0x7fff;
-            if (u < PtType<T>::kInf) continue;
-            atomicMin(&mark[(u > PtType<T>::kInf ? 0 : e[i] >> 15 ? 2 : 1) * D + dim + i], j * kKeys + row);
-            e[i] = 0;
-            *marked = 1;
+          for (; odd; odd &= odd - 1) {
+            const int c = c0 + (__ffs(odd) - 1) * 64, row = c / 8 % kKeys;
+            uint16_t *e = reinterpret_cast<uint16_t *>(sv + st * S::kKv + c * 16);
+            const int dim = c / (8 * kKeys) * 64 + ((c & 7) ^ (row & 7)) * 8;
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t u = e[i] & 0x7fff;
+              if (u < PtType<T>::kInf) continue;
+              atomicMin(&mark[(u > PtType<T>::kInf ? 0 : e[i] >> 15 ? 2 : 1) * D + dim + i], j * kKeys + row);
+              e[i] = 0;
+              *marked = 1;
+            }
           }
         }
         fence_proxy_async();
