@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
         l *= keep;
         if (j == w.first) return;
         added(j - 1);
-#pragma unroll
+#pragma unroll 1
         for (int q = 0; q < D / 32; ++q) {
           float o[32];
           tmem_ld32(to + q * 32, o);
@@ -675,7 +675,35 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
     const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
     const bool fix = *marked;
     if (tokens[i]) {
+      // A lane has a row, and rows are apart in memory.  With 128 dims 32 rows of 256
+      // bytes at a time go through the tile's queries, which nothing reads any more,
+      // each 16 bytes at their place xor the row, and leave in whole rows: 1% of a
+      // long prompt, 5% where keys are split.  (With 64 the registers for it cost the
+      // loop above more than that.)
+      uint8_t *stage = sq + i * S::kTile + (warp & 3) * (S::kTile / 4);
+      uint8_t *dst = !live ? nullptr
+                     : whole ? reinterpret_cast<uint8_t *>(static_cast<T *>(p.out) + (w.q0 + index) * p.out_stride + static_cast<long long>(h) * D)
+                             : reinterpret_cast<uint8_t *>(p.part_o + (static_cast<long long>(blockIdx.y) * p.n_q * p.n_heads + at) * D);
+      const auto put = [&](int chunk, uint4 v) {
+        if constexpr (D == 64) {
+          if (live) *reinterpret_cast<uint4 *>(dst + chunk * 16) = v;
+        } else {
+          *reinterpret_cast<uint4 *>(stage + lane * 256 + (chunk % 16 ^ (lane & 7)) * 16) = v;
+        }
+      };
+      const auto leave = [&](int offset) {
+        if constexpr (D == 64) return;
+        __syncwarp();
 #pragma unroll
+        for (int r = 0; r < 32; r += 2) {
+          const int from = r + lane / 16, chunk = lane % 16;
+          uint8_t *to_row = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), from));
+          const uint4 v = *reinterpret_cast<const uint4 *>(stage + from * 256 + (chunk ^ (from & 7)) * 16);
+          if (to_row) *reinterpret_cast<uint4 *>(to_row + offset + chunk * 16) = v;
+        }
+        __syncwarp();
+      };
+#pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
         float o[32];
         if (ends[i] > w.first) {
@@ -686,7 +714,6 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
-        if (!live) continue;
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0.f : o[e] * inv;
         if (fix) {
@@ -697,15 +724,16 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
           }
         }
         if (whole) {
-          uint4 *dst = reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + (w.q0 + index) * p.out_stride + static_cast<long long>(h) * D + q * 32);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            dst[e] = make_uint4(X::pack(o[8 * e], o[8 * e + 1]), X::pack(o[8 * e + 2], o[8 * e + 3]), X::pack(o[8 * e + 4], o[8 * e + 5]),
-                                X::pack(o[8 * e + 6], o[8 * e + 7]));
+            put(q * 4 + e, make_uint4(X::pack(o[8 * e], o[8 * e + 1]), X::pack(o[8 * e + 2], o[8 * e + 3]), X::pack(o[8 * e + 4], o[8 * e + 5]),
+                                      X::pack(o[8 * e + 6], o[8 * e + 7])));
+          if (q + 1 == D / 32) leave(0);
         } else {
-          float4 *dst = reinterpret_cast<float4 *>(p.part_o + (static_cast<long long>(blockIdx.y) * p.n_q * p.n_heads + at) * D + q * 32);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          for (int e = 0; e < 8; ++e)
+            put(q * 8 + e, make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]), __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3])));
+          if (q % 2) leave(q / 2 * 256);
         }
       }
       if (live) {
