@@ -625,7 +625,8 @@ size_t wf_kv8_block_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_d
  *   d_slots   int32 [n]: block * block_size + position % block_size; a negative
  *             slot skips its row.  Rows of the same 16 positions follow one
  *             another in the call, as wf_page_plan gives them (the same
- *             position twice: the later row holds)
+ *             position twice: the later row holds), with at most 31 rows in a
+ *             row skipped between them
  * Positions are appended: of a record that a call writes to, those before the
  * first one written are kept, those after that are not written become zeros.
  * A kept record's e never falls; where it grows, codes are rounded again.

@@ -113,16 +113,17 @@ class Cache:
         return self.record(slot, head)[32 * self.dim:32 * self.dim + 8].copy().view(np.float32).astype(np.float64)
 
     def store(self, slots, k, v):
-        """Rows k, v [n, heads, dim] float64 at slots, record by record."""
+        """Rows k, v [n, heads, dim] float64 at slots, record by record; up to 31 skipped rows between a record's do not part them."""
         i = 0
         while i < len(slots):
             if slots[i] < 0:
                 i += 1
                 continue
-            j = i
-            while j < len(slots) and slots[j] >= 0 and slots[j] // 16 == slots[i] // 16:
+            j, last = i, i
+            while j < len(slots) and j - last <= 32 and (slots[j] < 0 or slots[j] // 16 == slots[i] // 16):
+                last = j if slots[j] >= 0 else last
                 j += 1
-            rows = {int(slots[r]) % 16: r for r in range(i, j)}
+            rows = {int(slots[r]) % 16: r for r in range(i, last + 1) if slots[r] >= 0}
             for h in range(self.heads):
                 for is_v, x in enumerate((k, v)):
                     self._write(int(slots[i]), h, is_v, {p: x[r, h] for p, r in rows.items()})

@@ -25,7 +25,10 @@ struct Kv8RowParams {
 
 // The slots of a CTA's first 32 rows, a lane each (-1 past the last), and as bits
 // those of its own rows that open a run.  Rows of a record that follow one
-// another are one run; `ascending`: as far as their positions ascend.
+// another are one run, rows that are skipped between them or not (up to
+// kK8Skips in a row); `ascending`: rows directly behind one another, as far as
+// their positions ascend.
+constexpr int kK8Skips = 31;
 struct Kv8Rows {
   int slot;
   uint32_t openers;
@@ -33,9 +36,19 @@ struct Kv8Rows {
 __device__ __forceinline__ Kv8Rows kv8_rows(const Kv8RowParams &p, int row0, int lane, bool ascending) {
   Kv8Rows r;
   r.slot = row0 + lane < p.n ? p.slots[row0 + lane] : -1;
-  const int first = row0 > 0 ? p.slots[row0 - 1] : -1, up = __shfl_up_sync(0xffffffffu, r.slot, 1), before = lane == 0 ? first : up;
+  const int back = row0 - 32 + lane >= 0 ? p.slots[row0 - 32 + lane] : -1;
+  int before, apart = 1;
+  if (ascending) {
+    const int first = __shfl_sync(0xffffffffu, back, 31), up = __shfl_up_sync(0xffffffffu, r.slot, 1);
+    before = lane == 0 ? first : up;
+  } else {  // the nearest that is not skipped
+    const uint32_t here = __ballot_sync(0xffffffffu, r.slot >= 0) & ((1u << lane) - 1), there = __ballot_sync(0xffffffffu, back >= 0);
+    const int at = 31 - __clz(here ? here : there ? there : 1u);
+    const int near = __shfl_sync(0xffffffffu, r.slot, at), far = __shfl_sync(0xffffffffu, back, at);
+    before = here ? near : far, apart = (here ? 0 : 32) + lane - at;
+  }
   const bool mine = lane < p.rows && row0 + lane < p.n;
-  const bool opens = r.slot < 0 ? ascending : before < 0 || before >> 4 != r.slot >> 4 || (ascending && before >= r.slot);
+  const bool opens = r.slot < 0 ? ascending : before < 0 || apart > kK8Skips + 1 || before >> 4 != r.slot >> 4 || (ascending && before >= r.slot);
   r.openers = __ballot_sync(0xffffffffu, mine && opens);
   return r;
 }
@@ -56,21 +69,27 @@ __device__ __forceinline__ Kv8Run kv8_run(const Kv8RowParams &p, const Kv8Rows &
   Kv8Run r;
   r.slot = __shfl_sync(0xffffffffu, rows.slot, first);
   r.row = -1;
-  int at = row0 + first, slot = __shfl_sync(0xffffffffu, rows.slot, (lane + first) & 31), most = 32 - first;
-  for (;;) {  // (again only for more rows than a record has positions)
-    bool in = lane < most && slot >= 0 && slot >> 4 == r.slot >> 4;
+  int at = row0 + first, slot = __shfl_sync(0xffffffffu, rows.slot, (lane + first) & 31), most = 32 - first, latest = at;
+  for (;;) {  // (again only for more rows than a record has positions, or where rows are skipped)
+    const bool same = slot >= 0 && slot >> 4 == r.slot >> 4;
+    bool in = lane < most && at + lane < p.n && (same || (slot < 0 && !ascending));
     if (ascending) {
       const int before = __shfl_up_sync(0xffffffffu, slot, 1);
       in = in && (lane == 0 || before < slot);
     }
     const uint32_t out = ~__ballot_sync(0xffffffffu, in);
     const int count = out ? __ffs(out) - 1 : 32;
+    uint32_t which = __ballot_sync(0xffffffffu, same && lane < count);
+    if (which == 0 || at + __ffs(which) - 1 - latest > kK8Skips + 1) break;
+    latest = at + 31 - __clz(which);
     const int start = r.slot & 15;
     if (at == row0 + first && __all_sync(0xffffffffu, lane >= count || slot == r.slot + lane)) {
       if (lane >= start && lane - start < count) r.row = at + lane - start;
     } else {
-      for (int c = 0; c < count; ++c)
+      for (; which; which &= which - 1) {
+        const int c = __ffs(which) - 1;
         if ((__shfl_sync(0xffffffffu, slot, c) & 15) == lane) r.row = at + c;
+      }
     }
     if (count < most || ascending) break;
     at += most, most = 32;

@@ -75,6 +75,41 @@ def test_store_and_load(dtype, heads, dim, calls):
         assert (out[len(see):] == 7).all() and (out[:, heads * dim:] == 7).all()
 
 
+# slots of a call whose rows are partly skipped, as of a block of proposals of which some are taken
+SKIPPED = [
+    [3, -1, 4, -1, -1, 5, 6],
+    [-1] * 5 + [0] + [-1] * 31 + [1] + [-1] * 31 + [2, 16, -1, 17] + [-1] * 70,  # as many as may be
+    [0, 1] + [-1] * 3 + [2] + [-1] * 20 + [3, -1, 3, -2, 5] + [-1] * 14 + [33, -1, 34, 64, -1, 65] + [-1] * 14 + [66],  # over several CTAs' rows
+    [-1] * 60 + [40] + [-1] * 9 + [41] + [-1] * 9 + [42] + [-1] * 9 + [43] + [-1] * 9 + [44] + [-1] * 9 + [45, 48],
+    [20, -1, 21] * 9 + [-1, 22],
+    [-1] * 100,
+]
+
+
+@pytest.mark.parametrize("heads,copies", [(2, 1), (24, 1), (2, 2500)])
+@pytest.mark.parametrize("case", range(len(SKIPPED)))
+def test_rows_that_are_skipped_do_not_part_a_record(heads, copies, case):
+    """Byte for byte as the restatement, in few rows and (`copies`, each in blocks of its own) in many a CTA."""
+    import torch
+    from paper_2609_32869_gb300 import binding as B
+    rng = np.random.default_rng(case)
+    slots, dim, blocks = SKIPPED[case], 64, 3
+    n = len(slots)
+    c = op.Cache(blocks, 32, heads, dim, fill=0x38)
+    c.raw[..., 32 * dim:] = np.array([1.0, 0.5, 0, 0], np.float32).view(np.uint8)
+    raw = torch.from_numpy(c.raw.copy()).cuda().repeat(copies, 1, 1, 1)
+    x = _rows(torch, rng, n, 2 * heads, dim, "bf16")
+    k, v = x[:, :heads].reshape(n, -1), x[:, heads:].reshape(n, -1)
+    many = [s + 32 * blocks * i if s >= 0 else s for i in range(copies) for s in slots]
+    pool = B.kv8_pool(raw, 1, blocks * copies, 32, heads, dim, B.WF_BF16)
+    kk, vv = k.repeat(copies, 1), v.repeat(copies, 1)
+    B.wf_kv8_store(pool, 0, kk, heads * dim, vv, heads * dim, _i32(torch, many), n * copies)
+    c.store(slots, _f64(k).reshape(n, heads, dim), _f64(v).reshape(n, heads, dim))
+    got = raw.cpu().numpy().reshape((copies,) + c.raw.shape)
+    np.testing.assert_array_equal(got[0], c.raw)
+    assert (got == got[0]).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_values_at_the_ends_of_the_range(dtype):
     """All zero, tiny, huge, not finite: one record each, and such a row behind an ordinary one."""
