@@ -241,7 +241,7 @@ wf_status wf_rope(const wf_rope_table *table, const void *d_q, int64_t q_stride,
   p.slots = std::max(1, std::min(p.heads, kRopeThreads / (p.rows * columns)));
   // Few rows: a grid row for every `slots` heads, so that a thread takes one.
   p.per_y = n <= kSms * 4 ? p.slots : p.heads;
-  const dim3 grid((n + p.rows - 1) / p.rows, (p.heads + p.per_y - 1) / p.per_y);
+  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(n) + p.rows - 1) / p.rows), (p.heads + p.per_y - 1) / p.per_y);
   const void *fn = dtype == WF_F32 ? rope_fn<float>(vec, half) : dtype == WF_F16 ? rope_fn<__half>(vec, half) : rope_fn<__nv_bfloat16>(vec, half);
   void *args[] = {&p};
   return launch_pdl(fn, grid, p.rows * columns * p.slots, 0, args, static_cast<cudaStream_t>(stream)) == cudaSuccess ? WF_OK : WF_ERR_CUDA;

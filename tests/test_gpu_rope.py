@@ -144,3 +144,22 @@ def test_nan_stays_in_its_pair():
     B.wf_rope(B.wf_rope_init(64, 32), x, 64, 1, None, 0, 0, torch.tensor([5, 6], dtype=torch.int32, device="cuda"), 2, B.WF_F32, False, out, 64, None, 0)
     assert sorted(torch.isnan(out[0]).nonzero()[:, 0].tolist()) == [3, 19] and out[1, 40] == float("inf")
     assert torch.isfinite(out).sum() == 128 - 3
+
+
+def test_as_many_rows_as_an_int_counts():
+    """2^31 - 1 rows of one pair, in place: the first, some and the last turned by their positions."""
+    import torch
+    from paper_2609_32869_gb300 import binding as B
+    n = 2 ** 31 - 1
+    if torch.cuda.mem_get_info()[0] < 24 * 2 ** 30:
+        pytest.skip("24 GiB needed")
+    x = torch.ones(n, 2, dtype=torch.float16, device="cuda")
+    pos = torch.zeros(n, dtype=torch.int32, device="cuda")
+    at = torch.tensor([0, 1, 7, 2 ** 30 + 3, n - 9, n - 8, n - 2, n - 1], device="cuda")
+    pos[at] = torch.arange(1, len(at) + 1, dtype=torch.int32, device="cuda")
+    B.wf_rope(B.wf_rope_init(2), x, 2, 1, None, 0, 0, pos, n, B.WF_F16, False, x, 2, None, 0)
+    p = np.arange(1, len(at) + 1, dtype=np.float64)
+    want = np.stack([np.cos(p) - np.sin(p), np.sin(p) + np.cos(p)], 1)
+    # half a step of fp16 and fp32 arithmetic
+    assert (np.abs(x[at].double().cpu().numpy() - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -20).all()
+    assert (x[at[-1] - 6:at[-1] - 1] == 1).all()
