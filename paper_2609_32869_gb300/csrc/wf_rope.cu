@@ -38,6 +38,25 @@ __device__ __forceinline__ void rope_down(float x, float &y) { y = x; }
 __device__ __forceinline__ void rope_down(float x, __nv_bfloat16 &y) { y = __float2bfloat16_rn(x); }
 __device__ __forceinline__ void rope_down(float x, __half &y) { y = __float2half_rn(x); }
 
+// Whole 16 bytes pass as a stream: they are read once, and what is written is
+// more than L2 holds or, of few rows, stays in it all the same (2% of a large call).
+template <typename V>
+__device__ __forceinline__ V rope_load(const V *p) {
+  if constexpr (sizeof(V) == 16) {
+    const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p));
+    return *reinterpret_cast<const V *>(&u);
+  } else {
+    return *p;
+  }
+}
+template <typename V>
+__device__ __forceinline__ void rope_store(V *p, const V &v) {
+  if constexpr (sizeof(V) == 16)
+    __stcs(reinterpret_cast<uint4 *>(p), *reinterpret_cast<const uint4 *>(&v));
+  else
+    *p = v;
+}
+
 // gain cos and gain sin of pos * turns.
 __device__ __forceinline__ float2 rope_angle(int pos, uint64_t turns, float gain) {
   const uint32_t at = static_cast<uint32_t>((static_cast<uint64_t>(static_cast<int64_t>(pos)) * turns) >> 32);
@@ -55,9 +74,9 @@ __device__ __forceinline__ float2 rope_angle(int pos, uint64_t turns, float gain
 // are without gaps; or two vectors of dims that do not turn.  A thread keeps its
 // row's cos and sin of one unit in registers and takes that unit of several
 // heads, the next one's loads in flight; a CTA works out each (row, pair)'s angle once.
-//   16384 rows of 40 heads x 128, bf16, neighbours: 64 us, 5.2 TB/s; at three CTAs
+//   16384 rows of 40 heads x 128, bf16, neighbours: 60.5 us, 5.5 TB/s; at three CTAs
 //     an SM (76 registers instead of 64) 68, with two units ahead 71 to 83
-//   6001 rows of 40 heads x 64, fp32, 32 dims turn: 21 us, 5.9 TB/s; with one unit ahead 22.7
+//   6001 rows of 40 heads x 64, fp32, 32 dims turn: 20.7 us, 5.9 TB/s; with one unit ahead 22.7
 //   80 rows of 40 heads x 64, bf16: 5.5 us, the call and two dependent reads
 template <typename T, int VEC, bool kHalf>
 __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_constant__ RopeParams p) {
@@ -89,8 +108,8 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_cons
   };
   const auto load = [&](int h, int s) {
     const T *src = h < p.hq ? q + static_cast<long long>(h) * dim : k + static_cast<long long>(h - p.hq) * dim;
-    x[s] = *reinterpret_cast<const V *>(src + a);
-    if (two) y[s] = *reinterpret_cast<const V *>(src + b);
+    x[s] = rope_load(reinterpret_cast<const V *>(src + a));
+    if (two) y[s] = rope_load(reinterpret_cast<const V *>(src + b));
   };
   const auto start = [&]() {
 #pragma unroll
@@ -143,8 +162,8 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_cons
         } else if (!(h < p.hq ? p.q_copy : p.k_copy)) {
           continue;
         }
-        *reinterpret_cast<V *>(dst + a) = ox;
-        if (two) *reinterpret_cast<V *>(dst + b) = oy;
+        rope_store(reinterpret_cast<V *>(dst + a), ox);
+        if (two) rope_store(reinterpret_cast<V *>(dst + b), oy);
       }
     }
   }
@@ -235,9 +254,18 @@ wf_status wf_rope(const wf_rope_table *table, const void *d_q, int64_t q_stride,
   const bool copies = p.q_copy || (n_kv_heads && p.k_copy);
   p.units = p.turned + (copies ? static_cast<int>((dim - rot) / vec + 1) / 2 : 0);
   const int columns = std::min(p.units, kRopeThreads);
-  // Rows of a CTA: as many as fill it while there are still eight CTAs an SM.
+  // Rows of a CTA: rounds of four CTAs an SM, each as long as its rows' bytes and about
+  // 12 KB more for a CTA's start; as few of that as can be, of at least one whole round.
+  // (16384 rows of 40 heads, bf16: 128 dims with 4 rows, 7 rounds, 60.5 us, 8 rows, 4 rounds, 63;
+  // 64 dims with 4 rows 37.1, with 8 34.0)
+  const int64_t row_bytes = static_cast<int64_t>(p.units) * 2 * vec * size * p.heads;
+  constexpr int kRound = kSms * 4;
   p.rows = 1;
-  while (p.rows < 8 && p.rows * 2 * (rot / 2) <= kRopePairs && p.rows * 2 * columns <= kRopeThreads && n / (p.rows * 2) >= kSms * 8) p.rows *= 2;
+  int64_t least = INT64_MAX;
+  for (int rows = 1; rows <= 8 && rows * (rot / 2) <= kRopePairs && rows * columns <= kRopeThreads && (rows == 1 || n / rows >= kRound); rows *= 2) {
+    const int64_t ctas = (static_cast<int64_t>(n) + rows - 1) / rows, cost = (ctas + kRound - 1) / kRound * (rows * row_bytes + 12288);
+    if (cost <= least) least = cost, p.rows = rows;
+  }
   p.slots = std::max(1, std::min(p.heads, kRopeThreads / (p.rows * columns)));
   // Few rows: a grid row for every `slots` heads, so that a thread takes one.
   p.per_y = n <= kSms * 4 ? p.slots : p.heads;
