@@ -566,7 +566,7 @@ wf_status wf_rope(const wf_rope_table *table, const void *d_q, int64_t q_stride,
  *   d_q_start, d_k_start  int32 [n_seq + 1]  sequence i has the query rows
  *            d_q_start[i] .. d_q_start[i + 1] - 1 and the keys d_k_start[i] ..
  *            d_k_start[i + 1] - 1, both ascending; each may be empty
- *   max_k    a bound on a sequence's keys; what is past it is not seen
+ *   max_k    a bound on a sequence's keys; one of more is taken to end there
  *            (WF_DEV_ERR_CAPACITY)
  *   causal   nonzero: of r query rows and t keys, row j sees the first
  *            t - (r - 1 - j): the queries are the last rows (t > r: keys that
