@@ -384,3 +384,21 @@ def test_sequences_may_share_one_table_row():
     got, err = _run(torch, B, c, "f16", q, table, [5, 70, 96], 1, 2, True, 0.1, 96, stride=0)
     assert err == 0
     _check(torch, c, "f16", q, np.repeat(table, 3, 0), [5, 70, 96], 1, 2, True, 0.1, got)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_shared_row_is_read_as_far_as_lengths_go(dim):
+    """A bound far above the lengths: what lies behind the row's columns is no block, and no error."""
+    import torch
+    from paper_2609_32869_gb300 import binding as B
+    rng = np.random.default_rng(3)
+    c = _cache(rng, 4, 16, 1, dim)
+    q = _round(torch, rng.normal(0, 1, (3, 2, dim)), "bf16")
+    table = np.array([[2, 0] + [10 ** 6] * 40])
+    lens = [0, 7, 32]
+    got, err = _run(torch, B, c, "bf16", q, table, lens, 1, 2, True, 0.1, 600, stride=0)
+    assert err == 0 and not got[0].any()
+    _check(torch, c, "bf16", q, np.repeat(table, 3, 0), lens, 1, 2, True, 0.1, got)
+    got, err = _run(torch, B, c, "bf16", q, np.repeat(table, 3, 0), lens, 1, 2, True, 0.1, 600)
+    assert err == 0 and not got[0].any()
+    _check(torch, c, "bf16", q, np.repeat(table, 3, 0), lens, 1, 2, True, 0.1, got)
