@@ -772,12 +772,13 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const PromptParams p, 
     const float2 ml = p.part_ml[k * rows + at];
     // (nothing seen: zeros; only NaN scores: a sum of NaN)
     const float f = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2((ml.x - m) * c);
-    if (f == 0.f) continue;
+    // What is not finite stays so however small the part's factor: an infinity times a 0 would be NaN.
+    const auto share = [f](float v) { return isinf(v) ? v : f * v; };
     l += f * ml.y;
 #pragma unroll
     for (int g = 0; g < D / 64; ++g) {
       const float2 v = *reinterpret_cast<const float2 *>(p.part_o + (k * rows + at) * D + g * 64 + lane * 2);
-      o[g].x += f * v.x, o[g].y += f * v.y;
+      o[g].x += share(v.x), o[g].y += share(v.y);
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
