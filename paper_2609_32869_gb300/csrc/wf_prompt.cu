@@ -719,8 +719,10 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
         if (fix) {
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
-            const bool nan = mark[q * 32 + e] < limit, up = mark[D + q * 32 + e] < limit, down = mark[2 * D + q * 32 + e] < limit;
-            if (nan || up || down) o[e] = nan || (up && down) ? NAN : up ? INFINITY : -INFINITY;
+            // added, not put in their place: the row may be NaN already, or hold the opposite infinity
+            if (mark[q * 32 + e] < limit) o[e] = NAN;
+            if (mark[D + q * 32 + e] < limit) o[e] += INFINITY;
+            if (mark[2 * D + q * 32 + e] < limit) o[e] -= INFINITY;
           }
         }
         if (whole) {
