@@ -50,12 +50,12 @@ __device__ __forceinline__ uint32_t flags_f16(uint32_t two) { return (two & 0x80
 // steps of 32 positions of a unit through a ring of its own in shared memory
 // (one bulk copy per record, an mbarrier per stage; no other warp is waited for)
 // and keeps a running reference, sum and weighted values.
-//   96 sequences x 9 rows x 20 heads, 1500 positions, bf16: 67.6 us, 5.6 TB/s, by HBM
+//   96 sequences x 9 rows x 20 heads, 1500 positions, bf16: 68 us, 5.5 TB/s, by HBM
 //     and 3.2 rounds of CTAs that take four (cut in two, the halves joined over a
 //     cluster, 92; at three CTAs an SM 74, at five, which spill, 110)
-//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 39.7 us,
+//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 39 us,
 //     5.7 TB/s, by HBM; of that the join 2 us (with a third stage, two CTAs an SM, 47)
-//   5 rows of one sequence, 1500 positions, 20 heads, bf16: 5.6 us, by the launch
+//   5 rows of one sequence, 1500 positions, 20 heads, bf16: 5.9 us, by the launch
 //     and one chain of reads
 template <typename T, int G, int NT>
 __global__ void __launch_bounds__(kAtThreads, K8Shape<G, NT>::kBlocks) kv8_attention_kernel(const PagedAttnParams<Kv8Pool> p) {
@@ -77,29 +77,25 @@ __global__ void __launch_bounds__(kAtThreads, K8Shape<G, NT>::kBlocks) kv8_atten
   const int head = blockIdx.x % p.pool.heads, seq = blockIdx.x / p.pool.heads;
   const int row0 = blockIdx.z * kRows, rows = p.rps * p.group;  // rows of this key/value head: j * group + query head
   const int32_t *table = p.table + static_cast<long long>(seq) * p.table_stride;
-  const int begin = blockIdx.y * p.chunk, first = begin + warp * kTile, my_pos = first + (lane & (kSub - 1)) * 16;
-  // The first table entry is read beside the length that says whether it counts: one
-  // read less in the chain of a CTA's start, 68.5 to 67.6 us in the first case below
-  // (of 128 dims it gains nothing, where most chunks of short sequences have no positions).
-  const int32_t *entry = table + (my_pos >> p.pool.bs_shift);
-  int next_block = G == 1 && lane < kSub && my_pos < p.sure ? *entry : -1;
   const int raw_len = p.len[seq], len = clamp_len(p, raw_len);
   if (raw_len != len && threadIdx.x == 0) set_error(p.err, raw_len < 0 ? WF_DEV_ERR_PAGE : WF_DEV_ERR_CAPACITY);
   // positions that any row of this unit sees, and this CTA's share of them
   const int seen = row_limit(p, min(row0 + kRows, rows) - 1, len);
-  const int end = begin + min(seen - begin, p.chunk);
+  const int begin = blockIdx.y * p.chunk, end = begin + min(seen - begin, p.chunk);
   if (begin >= end && blockIdx.y > 0 && !p.cluster) return;
 
   // The ring: step i of this warp is positions begin + (warp + i kAtWarps) 32.
   // Lane k < 2 loads record k; four steps are whole blocks, so its place in a
   // block never changes and its table entry moves by whole blocks.
+  const int first = begin + warp * kTile;
   constexpr int stride = kAtWarps * kTile;
   const int steps = first < end ? (end - first + stride - 1) / stride : 0;
-  const int table_step = stride >> p.pool.bs_shift;
+  const int my_pos = first + (lane & (kSub - 1)) * 16, table_step = stride >> p.pool.bs_shift;
+  const int32_t *entry = table + (my_pos >> p.pool.bs_shift);
   const unsigned char *my_base = kv8_record(p.pool, 0, head, (my_pos & (p.pool.bs - 1)) >> 4);
   // steps in which this lane's record has positions to load
   const int my_steps = lane < kSub && my_pos < end ? (end - my_pos + stride - 1) / stride : 0;
-  if (my_steps > 0 && (G > 1 || my_pos >= p.sure)) next_block = *entry;
+  int next_block = my_steps > 0 ? *entry : -1;
   int to_issue = 0, issue_stage = 0;
   uint32_t there_bits = 0;  // kSub bits a stage: records that were loaded
   auto issue = [&]() {

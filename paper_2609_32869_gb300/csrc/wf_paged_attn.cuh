@@ -18,7 +18,6 @@ struct PagedAttnParams {
   long long q_stride, out_stride;
   const int32_t *table, *len;
   int table_stride, n_seq, rps, group, causal, max_len;
-  int sure;  // positions that surely have a table column, whatever the lengths
   uint32_t group_inv;  // 2^32 / group, rounded up (group > 1)
   float scale;
   // A unit is (sequence, key/value head, group of query rows); it is cut into
@@ -281,7 +280,6 @@ wf_status paged_args(const CPool &pool, const void *d_q, int64_t q_stride, const
   p->q = d_q, p->out = d_out, p->q_stride = q_stride, p->out_stride = out_stride;
   p->table = d_table, p->len = d_len, p->table_stride = table_stride;
   p->n_seq = n_seq, p->rps = rps, p->group = group;
-  p->sure = table_stride ? max_len : 0;
   p->group_inv = static_cast<uint32_t>(((1ull << 32) + group - 1) / group);
   p->causal = causal != 0, p->max_len = max_len, p->scale = scale, p->err = d_err;
   const AtPlan a = at_plan(n_seq, pool.n_kv_heads, rows, max_len);
