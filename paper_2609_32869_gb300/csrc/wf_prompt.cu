@@ -300,7 +300,6 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == kPtLoad * 32) tma_prefetch_desc(&mq), tma_prefetch_desc(&mk), tma_prefetch_desc(&mv);
   pdl_wait();
-  pdl_launch_dependents();
   const int head = blockIdx.x % p.heads;
   if (warp == 0) {
     PtWork w = {};
@@ -332,6 +331,9 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // Not before this CTA has its TMEM: a kernel that follows may take its own before it
+  // waits for this one, and each would then wait for the other.
+  pdl_launch_dependents();
   // Broadcast, so that the compiler knows that they are the same in all of a warp
   // and keeps what follows from them in uniform registers.
   const auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
