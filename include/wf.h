@@ -576,8 +576,10 @@ wf_status wf_rope(const wf_rope_table *table, const void *d_q, int64_t q_stride,
  * A row that sees nothing is zeros (lse -inf).  Rows before the first
  * sequence and behind the last are left as they were.  Keys and values that a
  * row does not see, in its sequence or outside it, do not reach it whatever
- * they hold.  Starts that descend or leave the buffers are clamped
- * (WF_DEV_ERR_PAGE).  Strides are in elements, multiples of 8, pointers
+ * they hold.  Starts that descend or leave the buffers are told of
+ * (WF_DEV_ERR_PAGE); query starts count as the least ascending ones that are
+ * no lower, cut off at the last, and keys as those from a start to the next
+ * one, all within the buffers.  Strides are in elements, multiples of 8, pointers
  * 16-byte aligned; d_out overlaps no input.  scale is above 0 and finite.
  * Scores, softmax and sums are fp32; a weight is rounded to dtype for the
  * second product.  Results do not depend on timing.  d_scratch (16-byte

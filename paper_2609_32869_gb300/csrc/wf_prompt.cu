@@ -218,23 +218,47 @@ __device__ __forceinline__ void tmem_st(uint32_t at, const uint32_t (&r)[N]) {
   }
 }
 
+// The query rows that starts may name: from the first start to the last.
+struct PtRange {
+  int from, to;
+};
+__device__ __forceinline__ PtRange pt_range(const PromptParams &p, int first, int last) {
+  PtRange r;
+  r.from = min(max(first, 0), p.n_q);
+  r.to = max(min(last, p.n_q), r.from);
+  return r;
+}
+
 // The sequence and first token of work item `item` (a warp; every lane gets it).
 // Items number each sequence's groups of `per` tokens, the last group first.
+// Starts that are none are brought into pt_range and made ascending, so that no
+// two sequences have a row in common and there are no more items than CTAs for them.
 // False: there is no such item.
 __device__ __forceinline__ bool pt_find(const PromptParams &p, int item, int lane, PtWork &w) {
   const int per = p.tokens * p.tiles;
-  int before = 0;
+  const int end_row = p.q_start[p.n_seq];
+  int before = 0, latest = 0;  // latest: of starts that are none, the largest so far
+  bool bent = false;
   for (int base = 0; base < p.n_seq; base += 32) {
     const int i = base + lane;
     int a = 0, b = 0, rk0 = 0, rk1 = 0;
-    bool bad = false;
     if (i < p.n_seq) {
-      const int ra = p.q_start[i], rb = p.q_start[i + 1];
+      a = p.q_start[i], b = p.q_start[i + 1];
       rk0 = p.k_start[i], rk1 = p.k_start[i + 1];
-      a = min(max(ra, 0), p.n_q), b = min(max(rb, a), p.n_q);
-      bad = a != ra || b != rb;
     }
-    if (bad) set_error(p.err, WF_DEV_ERR_PAGE);
+    // (every pair up to here in order and none above the last start: so is the whole)
+    bent |= __any_sync(0xffffffffu, i < p.n_seq && (a < 0 || b < a || b > end_row || end_row > p.n_q)) != 0;
+    if (bent) {
+      const PtRange range = pt_range(p, p.q_start[0], end_row);
+      int most = i < p.n_seq ? max(a, latest) : 0;
+      for (int off = 1; off < 32; off <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, most, off);
+        if (lane >= off) most = max(most, v);
+      }
+      a = min(max(most, range.from), range.to), b = i < p.n_seq ? min(max(most, b), range.to) : a;
+      b = max(b, a);
+      latest = __shfl_sync(0xffffffffu, most, 31);
+    }
     const int groups = (b - a + per - 1) / per;
     int sum = groups;
 #pragma unroll
@@ -250,18 +274,26 @@ __device__ __forceinline__ bool pt_find(const PromptParams &p, int item, int lan
       w.rows = __shfl_sync(0xffffffffu, b, src) - w.q0;
       const int end = __shfl_sync(0xffffffffu, before + sum, src);
       w.token = (end - 1 - item) * per;
-      if (w.token < 0 || w.token >= w.rows) return false;  // (starts that are none)
       rk0 = __shfl_sync(0xffffffffu, rk0, src), rk1 = __shfl_sync(0xffffffffu, rk1, src);
       w.k0 = min(max(rk0, 0), p.n_k);
       const int k1 = min(max(rk1, w.k0), p.n_k);
       w.keys = min(k1 - w.k0, p.max_k);
-      if (lane == 0 && (w.k0 != rk0 || k1 != rk1)) set_error(p.err, WF_DEV_ERR_PAGE);
       if (lane == 0 && k1 - w.k0 > p.max_k) set_error(p.err, WF_DEV_ERR_CAPACITY);
       return true;
     }
     before += __shfl_sync(0xffffffffu, sum, 31);
   }
   return false;
+}
+
+// Tells of starts that descend or leave the buffers (a warp).
+__device__ __forceinline__ void pt_check_starts(const PromptParams &p, int lane) {
+  bool bad = false;
+  for (int i = lane; i < p.n_seq; i += 32) {
+    const int a = p.q_start[i], b = p.q_start[i + 1], k0 = p.k_start[i], k1 = p.k_start[i + 1];
+    bad |= a < 0 || b < a || b > p.n_q || k0 < 0 || k1 < k0 || k1 > p.n_k;
+  }
+  if (bad) set_error(p.err, WF_DEV_ERR_PAGE);
 }
 
 template <typename T>
@@ -518,6 +550,7 @@ __global__ void __launch_bounds__(kPtThreads, PtShape<D>::kPerSm)
         fence_proxy_async();
         mbar_arrive_cta(&clean[st]);
       }
+      if (blockIdx.x == 0 && blockIdx.y == 0 && warp == kPtScrub) pt_check_starts(p, lane);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kRegsMore));
@@ -767,7 +800,8 @@ __global__ void __launch_bounds__(128) prompt_join_kernel(const PromptParams p, 
   const long long rows = static_cast<long long>(p.n_q) * p.n_heads, at = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
   if (at >= rows) return;
   const int row = static_cast<int>(at / p.n_heads), h = static_cast<int>(at % p.n_heads);
-  if (row < p.q_start[0] || row >= p.q_start[p.n_seq]) return;
+  const PtRange range = pt_range(p, p.q_start[0], p.q_start[p.n_seq]);
+  if (row < range.from || row >= range.to) return;
   float m = -INFINITY, l = 0.f;
   for (int k = 0; k < splits; ++k) m = fmaxf(m, p.part_ml[k * rows + at].x);
   const float c = p.scale * 1.4426950408889634f;
