@@ -532,8 +532,11 @@ typedef struct wf_rope_spec {
 
 /* What a spec comes to, a plain value that the caller keeps and passes by
  * address.  turns[i] is pair i's turn per position, a fraction of 2^64: an
- * angle is pos * turns[i] in 64-bit integers, so that far positions lose
- * nothing (2^-32 of a turn, whatever the position). */
+ * angle is pos * turns[i] in 64-bit integers, of which the calls use the upper
+ * 32 (2^-32 of a turn, whatever the position).  The turn itself is computed in
+ * doubles: a plain one is off by up to (5 + ln base) 2^-53 of it and 2^-64 of
+ * a whole one, which an angle has as many times as it has turns and positions:
+ * it may pass 2^-28 of a turn from some 2^23 positions on. */
 typedef struct wf_rope_table {
   int32_t head_dim, rot_dim, layout;
   float gain;
