@@ -41,7 +41,7 @@ def _compare(dtype, dim, hq, hkv, q, k, v, lens, keys, causal, scale, out, lse, 
         assert (err <= tol).all(), (r, t, np.argwhere(~(err <= tol))[:5], pick)
         got = lse[a + pick].double().cpu().numpy()[:, pick_h]
         f = np.isfinite(wl)
-        assert (np.isfinite(got) == f).all() and (np.abs(got - wl)[f] <= (2 * dx + 2.0 ** -22 * np.abs(wl))[f]).all()
+        assert (np.isfinite(got) == f).all() and (np.abs(got[f] - wl[f]) <= 2 * dx[f] + 2.0 ** -22 * np.abs(wl[f])).all()
         a, b = a + r, b + t
     for x in (out, lse):
         assert (x[:GAP] == 7).all() and (x[a:] == 7).all()
@@ -142,3 +142,20 @@ def test_keys_cut_up(dtype, dim, r, t, causal):
         dx = 2.0 ** -24 * (dim + 16) * scale * np.abs(_np(q, hq, dim)[GAP + j]).max(-1) * np.abs(_np(k, hkv, dim)[GAP:GAP + t]).sum(-1).max() + 2.0 ** -20
         assert (np.abs(x - y) <= 2 * (1 + u) * (u + 2 * dx[:, None]) * mass[0] + 2 * u * np.maximum(np.abs(x), np.abs(y)) + 2.0 ** -23).all()
         assert (alone[:GAP + j] == 7).all() and (alone[GAP + j + 1:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens,keys,causal", [
+    ([2300], [2100], True), ([5, 3, 40, 0, 70], [5000, 3, 0, 9, 1029], True), ([33, 1], [2047, 4100], False), ([1] * 9, [1, 0, 2049, 5, 1024, 1025, 64, 4099, 2], True)])
+def test_keys_cut_up_of_ragged_sequences(dtype, dim, lens, keys, causal):
+    """Sequences whose keys end in an early part, that have none, and rows that see nothing of some parts or of any."""
+    import torch
+    from paper_2609_32869_gb300 import binding as B
+    hq, hkv = 2, 1
+    rng = np.random.default_rng(len(lens))
+    q, k, v = _make(torch, rng, dtype, dim, hq, hkv, lens, keys)
+    assert B.wf_prompt_attention_scratch_bytes(len(lens), q.shape[0], max(keys), hq, hkv, dim) > 0
+    out, lse, err = _run(torch, B, dtype, dim, hq, hkv, q, k, v, _starts(torch, lens), _starts(torch, keys), len(lens), causal, dim ** -0.5, max(keys))
+    assert err == 0
+    _check(dtype, dim, hq, hkv, q, k, v, lens, keys, causal, dim ** -0.5, out, lse, rows=60)
