@@ -579,7 +579,10 @@ wf_status wf_rope(const wf_rope_table *table, const void *d_q, int64_t q_stride,
  * A row that sees nothing is zeros (lse -inf).  Rows before the first
  * sequence and behind the last are left as they were.  Keys and values that a
  * row does not see, in its sequence or outside it, do not reach it whatever
- * they hold.  Starts that descend or leave the buffers are told of
+ * they hold.  A value that it sees and is not finite makes that dim of the row
+ * not finite, NaN where there is a NaN or both infinities (an infinity whose
+ * weight is 0 in fp32 may be NaN too); a score that is NaN makes all dims NaN.
+ * Starts that descend or leave the buffers are told of
  * (WF_DEV_ERR_PAGE); query starts count as the least ascending ones that are
  * no lower, cut off at the last, and keys as those from a start to the next
  * one, all within the buffers.  Strides are in elements, multiples of 8, pointers

@@ -158,6 +158,7 @@ __device__ __forceinline__ int kv8_most(uint4 (&w)[G][4]) {
 // what a record keeps, is on its way before the first is used.
 //   48000 rows of 20 heads x 64, bf16, records of their own: 63 us, 5.9 TB/s, by
 //     HBM (read back in as long); with a record's loads one after another 70
+//     (fp16 keeps 28 bytes a thread in memory at six CTAs an SM)
 template <typename T, int G>
 __global__ void __launch_bounds__(kK8Warps * 32, G == 1 ? 6 : 3) kv8_store_kernel(const Kv8RowParams p) {
   using X = Type16<T>;

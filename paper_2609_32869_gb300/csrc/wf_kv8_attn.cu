@@ -52,8 +52,8 @@ __device__ __forceinline__ uint32_t flags_f16(uint32_t two) { return (two & 0x80
 // and keeps a running reference, sum and weighted values.
 //   96 sequences x 9 rows x 20 heads, 1500 positions, bf16: 68 us, 5.5 TB/s, by HBM
 //     and 3.2 rounds of CTAs that take four (cut in two, the halves joined over a
-//     cluster, 92; at three CTAs an SM 74, at five, which spill, 110)
-//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 39 us,
+//     cluster, 92; at three CTAs an SM 74, at five, which spill at length, 110; at four 8 bytes)
+//   6 sequences of 5000 to 65001 positions, 32 heads on 8, 128 wide, fp16: 39.6 us,
 //     5.7 TB/s, by HBM; of that the join 2 us (with a third stage, two CTAs an SM, 47)
 //   5 rows of one sequence, 1500 positions, 20 heads, bf16: 5.9 us, by the launch
 //     and one chain of reads

@@ -8,15 +8,17 @@
 // columns that its S was read from.  Four warps a tile turn S into P, a thread a
 // row: no shuffles.  A row's weights are relative to the maximum of its first
 // block, and O is rescaled only where a later weight would pass 2^16, so that no
-// maximum is taken of most blocks.
-//   one prompt of 8192 tokens, 32 heads on 8, 128 wide, causal, bf16: 357 us,
+// maximum is taken of most blocks.  A weight is rounded to the rows' type, as the
+// product's two operands are of one type: up to 2^-8 of it in bf16, 2^-11 in fp16; its
+// row's sum is of the weights in fp32.
+//   one prompt of 8192 tokens, 32 heads on 8, 128 wide, causal, bf16: 356 us,
 //     1.54 PFLOP/s, by the tensor unit and shared memory (58% busy at 4096 tokens),
 //     and the way from a tile's weights to its next scores
-//   32 x 1500 frames, 20 heads, 64 wide: 378 us, 0.97 PFLOP/s, by that way (the tensor unit works 66% of the time)
-//   16 prompts of 5 to 224 tokens, 20 heads, 64 wide: 10.7 us, two rounds of CTAs
+//   32 x 1500 frames, 20 heads, 64 wide: 379 us, 0.97 PFLOP/s, by that way (the tensor unit works 66% of the time)
+//   16 prompts of 5 to 224 tokens, 20 heads, 64 wide: 10 to 11.8 us, two rounds of CTAs
 //     of 1 us to find their rows, 1 us to the first scores, 0.8 us a block and 1 us of results
 //   three pieces of 2 to 300 tokens behind 15000 to 30000, 32 heads on 8, 128 wide,
-//     fp16: 180 to 200 us, 0.95 PFLOP/s, tiles that are not full and the join
+//     fp16: 177 to 200 us, 0.95 PFLOP/s, tiles that are not full and the join
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -51,7 +53,7 @@ struct PromptParams {
 // 64 dims what a tile waits for is the way from a block's weights to its next
 // scores (without any exponentials the case below takes 360 us), so two CTAs
 // share the SM, with blocks of 64 keys, and four tiles' ways overlap.
-//   32 x 1500 frames, 20 heads: 378 us.  One CTA with 128 keys and a third buffer
+//   32 x 1500 frames, 20 heads: 379 us.  One CTA with 128 keys and a third buffer
 //   of scores 442; one with weights beside the scores, so that the next ones are
 //   there when a softmax ends: three tiles and 64 keys 414, two and 128 479.
 template <int D>

@@ -74,10 +74,11 @@ __device__ __forceinline__ float2 rope_angle(int pos, uint64_t turns, float gain
 // are without gaps; or two vectors of dims that do not turn.  A thread keeps its
 // row's cos and sin of one unit in registers and takes that unit of several
 // heads, the next one's loads in flight; a CTA works out each (row, pair)'s angle once.
-//   16384 rows of 40 heads x 128, bf16, neighbours: 60.5 us, 5.5 TB/s; at three CTAs
+//   16384 rows of 40 heads x 128, bf16, neighbours: 61 us, 5.5 TB/s; at three CTAs
 //     an SM (76 registers instead of 64) 68, with two units ahead 71 to 83
 //   6001 rows of 40 heads x 64, fp32, 32 dims turn: 20.7 us, 5.9 TB/s; with one unit ahead 22.7
-//   80 rows of 40 heads x 64, bf16: 5.5 us, the call and two dependent reads
+//   80 rows of 40 heads x 64, bf16: 5.7 us, the call and two dependent reads
+//   (at 64 registers the 16-bit ones keep 12 to 40 bytes of a thread's addresses in memory)
 template <typename T, int VEC, bool kHalf>
 __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_constant__ RopeParams p) {
   using V = RopeVec<T, VEC>;
@@ -256,7 +257,7 @@ wf_status wf_rope(const wf_rope_table *table, const void *d_q, int64_t q_stride,
   const int columns = std::min(p.units, kRopeThreads);
   // Rows of a CTA: rounds of four CTAs an SM, each as long as its rows' bytes and about
   // 12 KB more for a CTA's start; as few of that as can be, of at least one whole round.
-  // (16384 rows of 40 heads, bf16: 128 dims with 4 rows, 7 rounds, 60.5 us, 8 rows, 4 rounds, 63;
+  // (16384 rows of 40 heads, bf16: 128 dims with 4 rows, 7 rounds, 61 us, 8 rows, 4 rounds, 63;
   // 64 dims with 4 rows 37.1, with 8 34.0)
   const int64_t row_bytes = static_cast<int64_t>(p.units) * 2 * vec * size * p.heads;
   constexpr int kRound = kSms * 4;
